@@ -275,6 +275,89 @@ int ll_steer_sweep_topk(const ll_shape* shape, void* workspace, size_t workspace
                         int32_t* out_topk_ids, float* out_topk_p, float* out_target_logp, float* out_entropy,
                         void* stream);
 
+/*
+ * The norms around a block, with its gate and residual scale: what a lens translator (an affine map of an inner layer's rows, added
+ * to them, before the model's own final norm) or a wrapped layer does around its products.  Per row r,
+ *
+ *   u[j]   = gamma_y[j] * y[j] / rms(y)   (gamma_y given: the block's output has a norm of its own),   else y[j]
+ *   x[j]   = hidden[j] + scale * gate[j] * u[j]                                                         (gate NULL: 1)
+ *   out_hidden = bf16(x),   out_normed = bf16(gamma * x / rms(x)),   rms(x) = sqrt(mean_j x[j]^2 + eps)
+ *
+ * x is not rounded before its norm.
+ *
+ *   shape      N and d are used (d a multiple of 8, at most 32768), V is ignored
+ *   hidden, y  bf16 [N, d]
+ *   gate       bf16 [d] (gate_rows 0), bf16 [N, d] (gate_rows 1) or NULL (gate_rows 0)
+ *   gamma_y    bf16 [d] or NULL;  gamma bf16 [d];  scale finite
+ *   out_hidden, out_normed  bf16 [N, d]; either may be `hidden`, `y` or a [N, d] gate itself, no other overlap
+ *
+ * ll_block_norm_grad: the gradient.  From g_hidden (of out_hidden, bf16 [N, d]; NULL: zero) and g_normed (of out_normed), and the
+ * call's own inputs, of which x is formed again (nothing else need be kept),
+ *
+ *   d_hidden, d_y  bf16 [N, d];  d_gate fp32 [d], or bf16 [N, d] where the gate is (iff gate is given)
+ *   d_gamma_y (iff gamma_y is given), d_gamma  fp32 [d]
+ *
+ * Parameters shared by the rows get the sum over them, added in one order (the same bits every time); N == 0 gives them zeros.
+ * d_hidden and d_y may be the buffer of any [N, d] input, but not each other's; no other overlap.
+ * workspace: at least ll_block_norm_grad_workspace_bytes(shape) bytes, 256-byte aligned.
+ */
+int ll_block_norm(const ll_shape* shape, const void* hidden, const void* y, const void* gate, int gate_rows, float scale,
+                  const void* gamma_y, const void* gamma, float eps, void* out_hidden, void* out_normed, void* stream);
+size_t ll_block_norm_grad_workspace_bytes(const ll_shape* shape);
+int ll_block_norm_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* hidden, const void* y,
+                       const void* gate, int gate_rows, float scale, const void* gamma_y, const void* gamma, float eps,
+                       const void* g_hidden, const void* g_normed, void* d_hidden, void* d_y, void* d_gate, float* d_gamma_y,
+                       float* d_gamma, void* stream);
+
+/*
+ * Log-probabilities of listed tokens, and their gradient: what a policy over answer tokens, a learned steering direction or a
+ * trained translator needs of the lens.  With z[r, v] = rows[r, :] . W_U[v, :] / temperature and p = softmax over the vocabulary,
+ *
+ *   out_logp    [N, k] fp32   z[r, ids[r, i]] - logsumexp(z[r, :]);  NaN where the id is outside [0, V)
+ *   out_lse     [N]    fp32   logsumexp(z[r, :])
+ *   out_entropy [N]    fp32   -sum_v p log p, in nats
+ *
+ *   rows  bf16 [N, d], already normalised (out_normed of ll_block_norm, the output of ll_steer_inject)
+ *   W_U   bf16 [V, d];  ids int32 [N, k], 1 <= k <= LL_LIST_MAX, any order, repeats allowed;  temperature positive, finite
+ * d a multiple of 8, at most 65536.  (The most likely tokens besides are ll_project's matter.)
+ *
+ * ll_logp_grad: from lse and entropy as ll_logp returned them (entropy only with g_entropy), g_logp [N, k] and g_entropy [N] or NULL,
+ *
+ *   dz[r, v] = ( sum_{i: ids[r, i] = v} g_logp[r, i] - p (sum_i g_logp[r, i] + g_entropy[r] (log p + entropy[r])) ) / temperature
+ *   out_grad [N, d] bf16 = sum_v dz[r, v] W_U[v, :]
+ *
+ * Entries whose id is outside [0, V) take no part.  A row whose gradients are all zero gets zeros, whatever it holds.
+ * W_U gets no gradient: the lens reuses the model's own.  Rows are processed in passes of at most 2048, for which the
+ * workspace holds dz in bf16 (2 bytes times V a row).
+ * A row that holds NaN or infinity gets NaN; no other row is affected.
+ */
+#define LL_LIST_MAX 64
+size_t ll_logp_workspace_bytes(const ll_shape* shape, int k);
+int ll_logp(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+            const int32_t* ids, float* out_logp, float* out_lse, float* out_entropy, void* stream);
+size_t ll_logp_grad_workspace_bytes(const ll_shape* shape, int k);
+int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+                 const int32_t* ids, const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* out_grad,
+                 void* stream);
+
+/*
+ * Distillation from a teacher's top tokens: loss and gradient in one call.  The teacher is a list of k tokens a row with scores
+ * (logits, or log-probabilities: a constant a row makes no difference), as ll_project lists the last layer's.  Per row, over the
+ * entries whose id is in [0, V) and whose score is not -infinity,
+ *
+ *   t = softmax(teacher_scores / temperature),   p = softmax(rows W_U^T / temperature) over the whole vocabulary
+ *   out_loss[r] = temperature^2 sum_i t[i] (log t[i] - log p[id_i])
+ *   out_grad[r, :] = weight[r] d out_loss[r] / d rows[r, :] = weight[r] temperature sum_v (p[v] - t of v) W_U[v, :]     (bf16 [N, d])
+ *
+ * A row with no such entry has no teacher: loss 0, gradient 0, whatever it holds; so has a row of weight 0 its gradient.
+ *   weight    fp32 [N] or NULL (1)
+ *   out_grad  may be NULL: the loss alone, for about half the time; the workspace may then be of ll_logp_workspace_bytes
+ * Everything else as in ll_logp.
+ */
+size_t ll_distill_workspace_bytes(const ll_shape* shape, int k);
+int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+               const int32_t* teacher_ids, const float* teacher_scores, const float* weight, float* out_loss, void* out_grad, void* stream);
+
 /* Text for an LL_E* code (static storage, never NULL). */
 const char* ll_error_string(int code);
 

@@ -16,6 +16,7 @@ import torch
 LL_OK, LL_EINVAL, LL_EWORKSPACE, LL_EHIP, LL_ESCRATCH = 0, -1, -2, -3, -4
 LL_KMAX = 32
 LL_STATIC_SCRATCH_BYTES = 64 << 20
+LL_LIST_MAX = 64
 LL_FLAG_TOPK_SOFTMAX = 1
 LL_FLAG_REGISTER_STAGED = 2
 
@@ -87,6 +88,25 @@ def lib() -> ctypes.CDLL:
         L.ll_steer_inject_raw.restype = c_int
         L.ll_capture_append.argtypes = [POINTER(ll_capture_shape), c_void_p, c_void_p, c_int64, c_int64, c_void_p]
         L.ll_capture_append.restype = c_int
+        L.ll_block_norm.argtypes = [POINTER(ll_shape), c_void_p, c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p, c_float,
+                                    c_void_p, c_void_p, c_void_p]
+        L.ll_block_norm.restype = c_int
+        L.ll_block_norm_grad_workspace_bytes.argtypes = [POINTER(ll_shape)]
+        L.ll_block_norm_grad_workspace_bytes.restype = c_size_t
+        L.ll_block_norm_grad.argtypes = [POINTER(ll_shape), c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_int, c_float, c_void_p,
+                                         c_void_p, c_float] + [c_void_p] * 8
+        L.ll_block_norm_grad.restype = c_int
+        for name in ("ll_logp", "ll_logp_grad", "ll_distill"):
+            size = getattr(L, name + "_workspace_bytes")
+            size.argtypes = [POINTER(ll_shape), c_int]
+            size.restype = c_size_t
+        lens = [POINTER(ll_shape), c_void_p, c_size_t, c_void_p, c_void_p, c_float, c_int, c_void_p]
+        L.ll_logp.argtypes = lens + [c_void_p] * 4
+        L.ll_logp.restype = c_int
+        L.ll_logp_grad.argtypes = lens + [c_void_p] * 6
+        L.ll_logp_grad.restype = c_int
+        L.ll_distill.argtypes = lens + [c_void_p] * 5
+        L.ll_distill.restype = c_int
         L.ll_error_string.argtypes = [c_int]
         L.ll_error_string.restype = c_char_p
         L.ll_last_hip_error.argtypes = []
@@ -356,3 +376,180 @@ def ll_capture_append(store, slices, t0, *, stream=None):
     if rc != LL_OK:
         raise LLError(rc, "ll_capture_append")
 
+
+def _gate(gate, N, d):
+    """Whether the gate is a row's own: [N, d], against [d] for all rows."""
+    if gate is None:
+        return 0
+    _check(gate, _BF16, "gate", (d,) if gate.dim() == 1 else (N, d))
+    return gate.dim() - 1
+
+
+def _empty(size, dtype, device, stream):
+    """A tensor that a call on `stream` writes: of that stream's own memory, which no earlier work of another stream still uses, and not
+    given back to it before what the current stream has queued until the tensor is dropped."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(size, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(workspace, need, device, stream):
+    if workspace is None:
+        return _empty((max(need(), 256),), torch.uint8, device, stream)
+    if not (isinstance(workspace, _Tensor) and workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace: need a contiguous tensor on the GPU")
+    return workspace
+
+
+def ll_block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None, stream=None, out=None):
+    """The residual and the norms around a block: x = hidden + scale gate u, u = y or gamma_y y / rms(y).
+
+    hidden, y [..., d] bf16, gamma [d] bf16, gate None, [d] or [N, d] bf16, gamma_y None or [d] bf16.
+    Returns (x, gamma x / rms(x)), both bf16 in hidden's shape (`out`: two tensors to hold them).
+    """
+    d = hidden.shape[-1]
+    h2, y2 = _rows(hidden, d), _rows(y, d)
+    N = h2.shape[0]
+    _check(h2, _BF16, "hidden")
+    _check(y2, _BF16, "y", (N, d))
+    _check(gamma, _BF16, "gamma", (d,))
+    if gamma_y is not None:
+        _check(gamma_y, _BF16, "gamma_y", (d,))
+    if out is None:
+        x, n = (_empty((N, d), _BF16, h2.device, stream) for _ in range(2))
+    else:
+        x, n = out
+        for t, name in ((x, "out[0]"), (n, "out[1]")):
+            _check(t, _BF16, name)
+            if t.numel() != N * d:
+                raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(hidden.shape)}")
+    rc = (_lib or lib()).ll_block_norm(_shape(N, d, 0), h2.data_ptr(), y2.data_ptr(), _ptr(gate), _gate(gate, N, d), float(scale),
+                                       _ptr(gamma_y), gamma.data_ptr(), float(eps), x.data_ptr(), n.data_ptr(), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_block_norm")
+    return (x, n) if x.shape == hidden.shape else (x.reshape(hidden.shape), n.reshape(hidden.shape))
+
+
+def ll_block_norm_grad_workspace_bytes(N: int, d: int) -> int:
+    return int(lib().ll_block_norm_grad_workspace_bytes(ll_shape(N, d, 0)))
+
+
+def ll_block_norm_grad(hidden, y, gamma, eps, g_hidden, g_normed, *, gate=None, scale=1.0, gamma_y=None, workspace=None, stream=None):
+    """Gradient of ll_block_norm: from its inputs, g_hidden (of x; None: zero) and g_normed, bf16 in hidden's shape.
+
+    Returns (d_hidden, d_y, d_gate, d_gamma_y, d_gamma): bf16 in hidden's shape, d_gate as the gate is (fp32 [d] or bf16 [N, d]; None without one),
+    fp32 [d] (d_gamma_y None without gamma_y).
+    """
+    size, d = hidden.shape, hidden.shape[-1]
+    h2, y2, gn = _rows(hidden, d), _rows(y, d), _rows(g_normed, d)
+    gh = None if g_hidden is None else _rows(g_hidden, d)
+    N = h2.shape[0]
+    _check(h2, _BF16, "hidden")
+    _check(y2, _BF16, "y", (N, d))
+    _check(gn, _BF16, "g_normed", (N, d))
+    if gh is not None:
+        _check(gh, _BF16, "g_hidden", (N, d))
+    _check(gamma, _BF16, "gamma", (d,))
+    if gamma_y is not None:
+        _check(gamma_y, _BF16, "gamma_y", (d,))
+    gate_rows = _gate(gate, N, d)
+    dev = hidden.device
+    dh, dy = _empty((N, d), _BF16, dev, stream), _empty((N, d), _BF16, dev, stream)
+    dk = None if gate is None else _empty((N, d), _BF16, dev, stream) if gate_rows else _empty((d,), _F32, dev, stream)
+    dgy = None if gamma_y is None else _empty((d,), _F32, dev, stream)
+    dg = _empty((d,), _F32, dev, stream)
+    ws = _workspace(workspace, lambda: ll_block_norm_grad_workspace_bytes(N, d), dev, stream)
+    rc = (_lib or lib()).ll_block_norm_grad(_shape(N, d, 0), ws.data_ptr(), ws.numel() * ws.element_size(), h2.data_ptr(), y2.data_ptr(),
+                                            _ptr(gate), gate_rows, float(scale), _ptr(gamma_y), gamma.data_ptr(), float(eps), _ptr(gh),
+                                            gn.data_ptr(), dh.data_ptr(), dy.data_ptr(), _ptr(dk), _ptr(dgy), dg.data_ptr(), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_block_norm_grad")
+    return dh if dh.shape == size else dh.reshape(size), dy if dy.shape == size else dy.reshape(size), dk, dgy, dg
+
+
+def ll_logp_workspace_bytes(N: int, d: int, V: int, k: int) -> int:
+    return int(lib().ll_logp_workspace_bytes(ll_shape(N, d, V), k))
+
+
+def ll_logp_grad_workspace_bytes(N: int, d: int, V: int, k: int) -> int:
+    return int(lib().ll_logp_grad_workspace_bytes(ll_shape(N, d, V), k))
+
+
+def ll_distill_workspace_bytes(N: int, d: int, V: int, k: int) -> int:
+    return int(lib().ll_distill_workspace_bytes(ll_shape(N, d, V), k))
+
+
+def _lens_rows(rows, W_U, ids, name):
+    """Rows as [N, d], the list as [N, k], and (N, d, V, k)."""
+    d = rows.shape[-1]
+    r2 = _rows(rows, d)
+    N, V = r2.shape[0], W_U.shape[0]
+    _check(r2, _BF16, "rows")
+    _check(W_U, _BF16, "W_U", (V, d))
+    k = ids.shape[-1] if ids.dim() > 1 else 1
+    i2 = ids if ids.dim() == 2 else ids.reshape(-1, k)
+    _check(i2, torch.int32, name, (N, k))
+    return r2, i2, N, d, V, k
+
+
+def ll_logp(rows, W_U, ids, *, temperature=1.0, workspace=None, stream=None):
+    """Log-probabilities of listed tokens: rows [..., d] bf16 (normalised), W_U [V, d] bf16, ids [N, k] int32 (or [N], k = 1).
+
+    Returns (logp [N, k], logsumexp [N], entropy [N]), fp32.
+    """
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids")
+    dev = rows.device
+    logp, lse, ent = _empty((N, k), _F32, dev, stream), _empty((N,), _F32, dev, stream), _empty((N,), _F32, dev, stream)
+    ws = _workspace(workspace, lambda: ll_logp_workspace_bytes(N, d, V, k), dev, stream)
+    rc = (_lib or lib()).ll_logp(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
+                                 float(temperature), k, i2.data_ptr(), logp.data_ptr(), lse.data_ptr(), ent.data_ptr(), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_logp")
+    return logp, lse, ent
+
+
+def ll_logp_grad(rows, W_U, ids, lse, entropy, g_logp, g_entropy=None, *, temperature=1.0, workspace=None, stream=None):
+    """Gradient of ll_logp to its rows, from its own lse and entropy (None without g_entropy), g_logp [N, k] and g_entropy [N] or None.
+
+    Returns it in bf16 in the rows' shape.
+    """
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids")
+    g2 = g_logp if g_logp.dim() == 2 else g_logp.reshape(-1, k)
+    _check(g2, _F32, "g_logp", (N, k))
+    _check(lse, _F32, "lse", (N,))
+    for t, name in ((entropy, "entropy"), (g_entropy, "g_entropy")):
+        if t is not None:
+            _check(t, _F32, name, (N,))
+    out = _empty((N, d), _BF16, rows.device, stream)
+    ws = _workspace(workspace, lambda: ll_logp_grad_workspace_bytes(N, d, V, k), rows.device, stream)
+    rc = (_lib or lib()).ll_logp_grad(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
+                                      float(temperature), k, i2.data_ptr(), lse.data_ptr(), _ptr(entropy), g2.data_ptr(), _ptr(g_entropy),
+                                      out.data_ptr(), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_logp_grad")
+    return out if out.shape == rows.shape else out.reshape(rows.shape)
+
+
+def ll_distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weight=None, grad=True, workspace=None, stream=None):
+    """Distillation from a teacher's top tokens: teacher_ids [N, k] int32 (an id outside the vocabulary: no entry), teacher_scores [N, k]
+    fp32 (logits or log-probabilities, as the logarithm of ll_project's lists), weight [N] fp32 or None (1).
+
+    Returns (loss [N] fp32, gradient of weight . loss in bf16 in the rows' shape, or None with grad=False).
+    """
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, teacher_ids, "teacher_ids")
+    s2 = teacher_scores if teacher_scores.dim() == 2 else teacher_scores.reshape(-1, k)
+    _check(s2, _F32, "teacher_scores", (N, k))
+    if weight is not None:
+        _check(weight, _F32, "weight", (N,))
+    loss = _empty((N,), _F32, rows.device, stream)
+    out = _empty((N, d), _BF16, rows.device, stream) if grad else None
+    ws = _workspace(workspace, lambda: (ll_distill_workspace_bytes if grad else ll_logp_workspace_bytes)(N, d, V, k), rows.device, stream)
+    rc = (_lib or lib()).ll_distill(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
+                                    float(temperature), k, i2.data_ptr(), s2.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(out),
+                                    _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_distill")
+    return loss, out if out is None or out.shape == rows.shape else out.reshape(rows.shape)

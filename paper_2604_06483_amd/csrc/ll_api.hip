@@ -1,5 +1,9 @@
-// Error reporting of the C ABI.
+// Error reporting of the C ABI, and what the launches of several files need once per device.
 #include "ll_common.h"
+
+#include <mutex>
+#include <utility>
+#include <vector>
 
 namespace ll {
 
@@ -9,6 +13,21 @@ int hip_failed(hipError_t e) {
   g_last_hip_error = (int)e;
   (void)hipGetLastError();   // clear the sticky error so that later calls start clean
   return LL_EHIP;
+}
+
+// A kernel that uses more than 64 KB of dynamic LDS has to be told so once per device; remembered
+// here so that the hot path makes no attribute call.
+int allow_dynamic_lds(const void* kern, size_t lds) {
+  static std::mutex mu;
+  static std::vector<std::pair<int, const void*>> done;
+  int dev = -1;
+  LL_HIP_CHECK(hipGetDevice(&dev));
+  std::lock_guard<std::mutex> lock(mu);
+  for (const auto& e : done)
+    if (e.first == dev && e.second == kern) return LL_OK;
+  LL_HIP_CHECK(hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  done.emplace_back(dev, kern);
+  return LL_OK;
 }
 
 }  // namespace ll

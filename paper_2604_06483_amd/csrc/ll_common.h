@@ -17,6 +17,9 @@ int hip_failed(hipError_t e);
     if (e__ != hipSuccess) return ll::hip_failed(e__); \
   } while (0)
 
+// Once per device and kernel: allows `lds` bytes of dynamic LDS (more than 64 KB have to be asked for).
+int allow_dynamic_lds(const void* kern, size_t lds);
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int kWave = 64;

@@ -1,0 +1,679 @@
+// What learns through the lens: log-probabilities of listed tokens, distillation from a teacher's top tokens, and the gradient of
+// either to the (normalised) rows.
+//
+//   z = A W^T / T,  p = softmax(z) over the whole vocabulary,  dA = dz W
+//
+// Forward, the logits stay in MFMA accumulators as in ll_project: the direct-to-LDS kernel (ll_gemm_lds.h) with an epilogue of its
+// own.  A gradient needs every logit a second time, as the left factor of a product over the vocabulary.  Forming them again would be a
+// third product; instead the first one's epilogue leaves e^(z - m), m the row's running maximum, as bf16 behind it (2 bytes a logit,
+// beside 4 d flops), whose relative error is that of any bf16 number however small it is, and the second product reads it with the
+// row's normaliser applied.
+#include "ll_epilogue.h"
+#include "ll_gemm_lds.h"
+
+#include <math.h>
+
+namespace {
+
+constexpr int LIST_MAX = LL_LIST_MAX;      // one lane of a wavefront each
+constexpr int PASS_ROWS = 2048;            // rows of a pass: what the workspace holds of e^(z - m) or dz, 0.6 GB at V = 152 000
+constexpr float LN2 = 0.6931471805599453f;
+
+struct RowTerms {   // of a row's dz: with l = (z log2 e - lse2), dz = 2^l (a + b l)
+  float lse2, a, b, live;
+};
+
+struct LearnArgs : GemmArgs {
+  uint16_t* P;          // [rows, ldp] bf16
+  float* ref;           // [rows, tiles]: what the exponents of a tile are relative to, in powers of two
+  const RowTerms* terms;   // [rows]
+  int64_t ldp;
+  float to_log2;        // log2(e) / T
+};
+
+// Within 64 columns of P the vocabulary is permuted: a lane of the first product holds ids 16 t + 4 g .. + 3 of tiles t, and puts two
+// tiles' side by side, 16 bytes at a time; the second product takes W's rows in the same order.
+__device__ __forceinline__ int64_t place_in_p(int v) {
+  return (v & ~31) + 8 * ((v >> 2) & 3) + 4 * ((v >> 4) & 1) + (v & 3);
+}
+
+enum { STATS, EXPS, GRAD };   // statistics only; and the exponentials; dz where the statistics are known
+template <int WHAT>
+struct LearnEpilogue {
+  struct State {   // of the lane's four rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
+    float m[4], s[4], t[4];
+    RowTerms terms[WHAT == GRAD ? 4 : 1];
+  };
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false;
+  static constexpr int ROWS = BN;
+  static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
+  static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
+  static __device__ __forceinline__ void init(State& st, const GemmArgs& args, int my_row, int) {
+    const LearnArgs& p = static_cast<const LearnArgs&>(args);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      st.m[j] = NEG_BIG;
+      st.s[j] = st.t[j] = 0.f;
+      if (WHAT == GRAD) st.terms[j] = p.terms[min(row_of(my_row, j), p.rows - 1)];
+    }
+  }
+  template <class ACC>
+  static __device__ __forceinline__ void tile(const ACC& acc, State& st, int v0, const GemmArgs& args, int my_row) {
+    const LearnArgs& p = static_cast<const LearnArgs&>(args);
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA's result is in its registers
+    if (v0 + BM <= p.V) rows_of_tile<true>(acc, st, v0, p, my_row);
+    else rows_of_tile<false>(acc, st, v0, p, my_row);
+  }
+  // WHOLE: all of the tile's columns are in the vocabulary.
+  template <bool WHOLE, class ACC>
+  static __device__ __forceinline__ void rows_of_tile(const ACC& acc, State& st, int v0, const LearnArgs& p, int my_row) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const float c = p.to_log2;
+    const int last = p.V - 1 - v0 - 4 * g;   // of the lane's 16 t + i, the last in the vocabulary
+    // Eight values of a row at a time, read from the accumulators as they are needed (twice where the maximum comes first): the
+    // fragments of the next stage hold most of the other registers.
+    const auto eight = [&](int j, int u, float (&x)[8]) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = acc_read(acc[2 * u + (q >> 2)][j][q & 3]) * c;
+      if (!WHOLE) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = 16 * (2 * u + (q >> 2)) + (q & 3) > last ? -INFINITY : x[q];
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = row_of(my_row, j);
+      float m = st.m[j], before = 0.f, keep = 1.f, s = 0.f, t = 0.f;
+      if (WHAT != GRAD) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          float x[8];
+          eight(j, u, x);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) m = fmaxf(m, x[q]);
+          LL_SCHED_FENCE();
+        }
+        if (WHAT == EXPS) {   // the four lanes of a row: one reference
+          const auto most = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
+          m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most));
+        }
+        before = st.m[j] - m;
+        keep = __builtin_amdgcn_exp2f(before);
+      }
+      if (WHAT != STATS && row >= p.rows) continue;
+      uint4* const to = reinterpret_cast<uint4*>(p.P + row * p.ldp + v0 + 8 * g);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        float x[8];
+        eight(j, u, x);
+        if (WHAT == GRAD) {
+          const RowTerms r = st.terms[j];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const float l = x[q] - r.lse2, e = __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a);
+            x[q] = l == -INFINITY || r.live == 0.f ? 0.f : e;
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const float l = x[q] - m;
+            x[q] = __builtin_amdgcn_exp2f(l);
+            s += x[q];
+            if (WHAT == STATS) t += l == -INFINITY ? 0.f : x[q] * l;   // (l is relative to the maximum: nothing large to take away again)
+          }
+        }
+        if (WHAT != STATS)
+          to[4 * u] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        LL_SCHED_FENCE();
+      }
+      if (WHAT != GRAD) {
+        if (WHAT == STATS) st.t[j] = st.s[j] > 0.f ? fmaf(keep, fmaf(before, st.s[j], st.t[j]), t) : t;
+        st.s[j] = fmaf(keep, st.s[j], s);
+        st.m[j] = m;
+        if (WHAT == EXPS && g == 0) p.ref[(int64_t)row * p.tiles + v0 / BM] = m;
+      }
+    }
+  }
+  // Every lane its own (m, S, T): four to a row and split.
+  static __device__ __forceinline__ void store(const GemmArgs& p, const State& st, int my_row, int split) {
+    if (WHAT == GRAD) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = row_of(my_row, j);
+      if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.m[j], st.s[j], st.t[j], 0.f);
+    }
+  }
+};
+
+template <int WHAT, bool TAIL>
+__global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void ll_learn_logits_kernel(const LearnArgs p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  lens_gemm_dma<LearnEpilogue<WHAT>, TAIL>(p, smem);
+}
+
+// Rows of a hidden size that is not a multiple of 64, zero padded to one.
+__global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __restrict__ rows, uint16_t* __restrict__ panel, int d, int64_t lda) {
+  const int64_t row = blockIdx.x;
+  for (int c = threadIdx.x; c < lda / 8; c += 256)
+    reinterpret_cast<uint4*>(panel + row * lda)[c] =
+        8 * c < d ? reinterpret_cast<const uint4*>(rows + row * d)[c] : make_uint4(0, 0, 0, 0);
+}
+
+// Logits of the listed tokens (before the temperature): one wavefront an entry; 0 for an id outside the vocabulary.
+__global__ __launch_bounds__(256) void ll_learn_list_logits_kernel(const uint16_t* __restrict__ rows, const uint16_t* __restrict__ W,
+                                                                   const int32_t* __restrict__ ids, int64_t entries, int k, int d, int V,
+                                                                   float* __restrict__ z) {
+  const int64_t e = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (e >= entries) return;
+  const int lane = threadIdx.x & 63, id = ids[e];
+  float s = 0.f;
+  if (id >= 0 && id < V) {
+    const uint4* a = reinterpret_cast<const uint4*>(rows + e / k * d);
+    const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)id * d);
+    float part[2] = {0.f, 0.f};
+#pragma unroll 4
+    for (int c = lane; c < d / 8; c += 64) {
+      const uint4 x = a[c], y = w[c];
+      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        part[0] = fmaf(bf16_lo(xs[i]), bf16_lo(ys[i]), part[0]);
+        part[1] = fmaf(bf16_hi(xs[i]), bf16_hi(ys[i]), part[1]);
+      }
+    }
+    s = wave_sum(part[0] + part[1]);
+  }
+  if (lane == 0) z[e] = s;
+}
+
+struct RowStats {
+  float lse2, t;   // log2 of the sum of 2^x; sum of p (x - lse2), x = z log2 e: minus the entropy, in powers of two
+};
+// A row's parts joined, by a wavefront.
+__device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats, int parts, int lane) {
+  float m = NEG_BIG;
+  bool nan = false;
+  for (int i = lane; i < parts; i += 64) {
+    m = fmaxf(m, stats[i].x);
+    nan |= stats[i].y != stats[i].y;
+  }
+  m = wave_max(m);
+  float s = 0.f, t = 0.f;
+  for (int i = lane; i < parts; i += 64) {
+    const float4 q = stats[i];
+    const float by = q.x - m, e = __builtin_amdgcn_exp2f(by);
+    s = fmaf(e, q.y, s);
+    t += q.y > 0.f ? e * fmaf(by, q.y, q.z) : 0.f;
+  }
+  s = wave_sum(s);
+  t = wave_sum(t);
+  const float log_s = __builtin_amdgcn_logf(s);
+  RowStats r = {m + log_s, t / s - log_s};
+  if (wave_sum(nan ? 1.f : 0.f) > 0.f) r.lse2 = r.t = NAN;
+  return r;
+}
+
+// A row's statistics from its parts, and its listed tokens' log-probabilities: one wavefront a row, one lane an entry.
+__global__ __launch_bounds__(256) void ll_logp_finish_kernel(const float4* __restrict__ stats, int parts, const float* __restrict__ z,
+                                                             const int32_t* __restrict__ ids, int rows, int k, int V, float to_log2,
+                                                             float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ entropy) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const RowStats r = join_stats(stats + (int64_t)row * parts, parts, lane);
+  if (lane == 0) {
+    lse[row] = r.lse2 * LN2;
+    entropy[row] = -r.t * LN2;
+  }
+  if (lane < k) {
+    const int64_t e = (int64_t)row * k + lane;
+    logp[e] = ids[e] >= 0 && ids[e] < V ? fmaf(z[e], to_log2, -r.lse2) * LN2 : NAN;
+  }
+}
+
+// What the listed entries of a row add to dz: `g` of every lane whose id is this lane's.  Of entries with one id the first has the
+// sum; returns whether the lane is one that has.
+__device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane, float& g) {
+  float sum = 0.f;
+  bool first = valid;
+  for (int j = 0; j < k; ++j) {
+    const int other = __builtin_amdgcn_readlane(valid ? id : -1, j);
+    const float share = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j));
+    if (valid && other == id) {
+      sum += share;
+      if (j < lane) first = false;
+    }
+  }
+  g = sum;
+  return first;
+}
+
+// Teacher, loss, and what dz is made of: one wavefront a row, one lane an entry.  Of a row without a teacher (or of weight 0, as far as
+// the gradient goes) nothing that the row holds matters.
+__global__ __launch_bounds__(256) void ll_distill_rows_kernel(const float4* __restrict__ stats, int parts, const float* __restrict__ z,
+                                                              const int32_t* __restrict__ ids, const float* __restrict__ scores,
+                                                              const float* __restrict__ weight, int rows, int k, int V, float temperature,
+                                                              float to_log2, float* __restrict__ loss, RowTerms* __restrict__ terms,
+                                                              float2* __restrict__ list) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const RowStats r = join_stats(stats + (int64_t)row * parts, parts, lane);
+  const int64_t e = (int64_t)row * k + lane;
+  const int id = lane < k ? ids[e] : -1;
+  const float score = lane < k ? scores[e] : -INFINITY;
+  const bool valid = id >= 0 && id < V && score != -INFINITY;
+  const bool some = __builtin_amdgcn_ballot_w64(valid) != 0;
+  const float most = wave_max(valid ? score : -INFINITY);
+  const float q = valid ? (score - most) / temperature : 0.f;
+  const float share = valid ? expf(q) : 0.f;
+  const float total = wave_sum(share);
+  const float t = some ? share / total : 0.f;
+  const float l = fmaf(lane < k ? z[e] : 0.f, to_log2, -r.lse2);
+  const float term = valid && t != 0.f ? t * ((q - logf(total)) - l * LN2) : 0.f;
+  const float sum = wave_sum(term);
+  if (lane == 0) loss[row] = some ? temperature * temperature * sum : 0.f;
+  if (terms == nullptr) return;
+  const float a = temperature * (weight != nullptr ? weight[row] : 1.f);
+  const bool live = some && a != 0.f;
+  float g = t;
+  const bool first = gather_same(id, valid, k, lane, g);
+  if (lane == 0) terms[row] = {r.lse2, a, 0.f, live ? 1.f : 0.f};
+  if (lane < k) {
+    const float p = __builtin_amdgcn_exp2f(l);
+    list[e] = make_float2(a * (p - g), __int_as_float(live && first ? id : -1));
+  }
+}
+
+// The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
+__global__ __launch_bounds__(256) void ll_logp_terms_kernel(const float* __restrict__ z, const int32_t* __restrict__ ids,
+                                                            const float* __restrict__ lse, const float* __restrict__ entropy,
+                                                            const float* __restrict__ g_logp, const float* __restrict__ g_entropy, int rows,
+                                                            int k, int V, float temperature, float to_log2, RowTerms* __restrict__ terms,
+                                                            float2* __restrict__ list) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const int64_t e = (int64_t)row * k + lane;
+  const int id = lane < k ? ids[e] : -1;
+  const bool valid = id >= 0 && id < V;
+  float g = valid ? g_logp[e] : 0.f;
+  const float total = wave_sum(g), gh = g_entropy != nullptr ? g_entropy[row] : 0.f;
+  const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || gh != 0.f;
+  const float lse2 = lse[row] / LN2, inv_t = 1.f / temperature;
+  const float a = -(total + (g_entropy != nullptr ? gh * entropy[row] : 0.f)) * inv_t, b = -gh * LN2 * inv_t;
+  const float l = fmaf(lane < k ? z[e] : 0.f, to_log2, -lse2);
+  const bool first = gather_same(id, valid, k, lane, g);
+  if (lane == 0) terms[row] = {lse2, a, b, live ? 1.f : 0.f};
+  if (lane < k) {
+    const float p = __builtin_amdgcn_exp2f(l);
+    list[e] = make_float2(fmaf(g, inv_t, p * fmaf(b, l, a)), __int_as_float(live && first ? id : -1));
+  }
+}
+
+// e^(z - m) to dz = a e^(z - lse), in place, eight values a thread.  Rounded to bf16 a second time: the error of a dz is then
+// 2^-9 sqrt(2) of itself in the mean, what the product's bf16 operand has anyway.
+__global__ __launch_bounds__(256) void ll_distill_scale_kernel(uint16_t* __restrict__ P, int64_t ldp, const float* __restrict__ ref, int tiles,
+                                                               const RowTerms* __restrict__ terms) {
+  const int64_t row = blockIdx.y;
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (c >= ldp) return;
+  const RowTerms r = terms[row];
+  uint4* at = reinterpret_cast<uint4*>(P + row * ldp + c);
+  uint4 q = make_uint4(0, 0, 0, 0);
+  if (r.live != 0.f) {
+    q = *at;
+    const float by = r.a * __builtin_amdgcn_exp2f(ref[row * tiles + c / BM] - r.lse2);
+    q = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
+                   pack_bf16(bf16_lo(q.z) * by, bf16_hi(q.z) * by), pack_bf16(bf16_lo(q.w) * by, bf16_hi(q.w) * by));
+  }
+  *at = q;
+}
+
+// The listed tokens' dz, from their fp32 logits and rounded once.
+__global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __restrict__ list, int64_t entries, int k, uint16_t* __restrict__ P,
+                                                                int64_t ldp) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= entries) return;
+  const float2 q = list[e];
+  const int id = __float_as_int(q.y);
+  if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(q.x, 0.f);
+}
+
+// ---------------------------------------------------------------------------------------
+// dA = dz W over one slice of the vocabulary: a workgroup has 128 rows by 128 columns, four wavefronts of 64 by 64, K steps of 32.
+// W comes with the columns in a row; its fragments are read transposed out of LDS.
+// ---------------------------------------------------------------------------------------
+struct BackArgs {
+  const uint16_t* P;      // [rows, ldp]
+  const uint16_t* W;      // [V, d]
+  float* part;            // [splits, rows, d]
+  int64_t ldp;
+  int rows, d, V, splits, steps;   // steps of 32 ids in all
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+__global__ __launch_bounds__(256) void ll_learn_back_kernel(const BackArgs p) {
+  __shared__ __align__(16) uint16_t sP[128][40];     // (rows of 80 bytes: sixteen of them start in different banks)
+  __shared__ __align__(16) uint16_t sW[32][128];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row0 = blockIdx.y * 128, col0 = blockIdx.x * 128, split = blockIdx.z;
+  const int step0 = (int)((int64_t)split * p.steps / p.splits), step1 = (int)((int64_t)(split + 1) * p.steps / p.splits);
+  const int wr = (wave & 1) * 64, wc = (wave >> 1) * 64;
+  const int g = lane >> 4, i16 = lane & 15;
+  f32x4 acc[4][4];   // [columns][rows]
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int step = step0; step < step1; ++step) {
+    uint4 a[2], w[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int ar = min(row0 + (tid >> 2) + 64 * q, p.rows - 1);
+      a[q] = *reinterpret_cast<const uint4*>(p.P + ar * p.ldp + 32 * (int64_t)step + 8 * (tid & 3));
+      const int v = min(32 * step + (tid >> 4) + 16 * q, p.V - 1), c = min(col0 + 8 * (tid & 15), p.d - 8);
+      w[q] = *reinterpret_cast<const uint4*>(p.W + (int64_t)v * p.d + c);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      *reinterpret_cast<uint4*>(&sP[(tid >> 2) + 64 * q][8 * (tid & 3)]) = a[q];
+      *reinterpret_cast<uint4*>(&sW[(tid >> 4) + 16 * q][8 * (tid & 15)]) = w[q];
+    }
+    __syncthreads();
+    bf16x8 fp[4], fw[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fp[j] = *reinterpret_cast<const bf16x8*>(&sP[wr + 16 * j + i16][8 * g]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      // (place_in_p: the lane group's eight K are ids 4 g .. + 3 and 16 + 4 g .. + 3)
+      s16x4 half[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sW[16 * h + 4 * g + (i16 >> 2)][wc + 16 * t + 4 * (i16 & 3)]);
+      fw[t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[t], fp[j], acc[t][j], 0, 0, 0);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = row0 + wr + 16 * j + i16;
+    if (row >= p.rows) continue;
+    float* to = p.part + ((int64_t)split * p.rows + row) * p.d;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int c = col0 + wc + 16 * t + 4 * g;
+      if (c < p.d) *reinterpret_cast<f32x4*>(to + c) = acc[t][j];
+    }
+  }
+}
+
+// The slices joined, in order; a row that takes no part gets zeros whatever W holds.
+__global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, int d,
+                                                            const RowTerms* __restrict__ terms, uint16_t* __restrict__ out) {
+  const int64_t row = blockIdx.y;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (c >= d) return;
+  float s[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i] = 0.f;
+  if (terms[row].live != 0.f)
+    for (int q = 0; q < splits; ++q) {
+      const float4* from = reinterpret_cast<const float4*>(part + ((int64_t)q * rows + row) * d + c);
+      const float4 lo = from[0], hi = from[1];
+      s[0] += lo.x;
+      s[1] += lo.y;
+      s[2] += lo.z;
+      s[3] += lo.w;
+      s[4] += hi.x;
+      s[5] += hi.y;
+      s[6] += hi.z;
+      s[7] += hi.w;
+    }
+  *reinterpret_cast<uint4*>(out + row * d + c) =
+      make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
+}
+
+// ---------------------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------------------
+constexpr int MAX_LEARN_D = 65536;
+
+bool valid(const ll_shape* s, int k) {
+  return s != nullptr && s->N >= 0 && s->N <= INT32_MAX && s->d > 0 && s->d % 8 == 0 && s->d <= MAX_LEARN_D && s->V > 0 &&
+         s->V <= INT32_MAX - BM && k >= 1 && k <= LL_LIST_MAX;
+}
+
+enum Needs { FORWARD, BACKWARD };
+
+struct LearnPlan {
+  int pass_rows, tiles, splits, row_blocks;
+  int back_splits;
+  int64_t lda, ldp;
+  size_t panel, z, stats, terms, list, ref, P, part, total;
+};
+
+LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
+  LearnPlan l = {};
+  const int64_t N = s->N > 0 ? s->N : 1;
+  const int64_t passes = (N + PASS_ROWS - 1) / PASS_ROWS, each = (N + passes - 1) / passes;
+  l.pass_rows = (int)(passes == 1 ? N : (each + BN - 1) / BN * BN);
+  l.tiles = (s->V + BM - 1) / BM;
+  l.row_blocks = (l.pass_rows + BN - 1) / BN;
+  const int most = NUM_CU / l.row_blocks < l.tiles ? NUM_CU / l.row_blocks : l.tiles;
+  const int per = (l.tiles + most - 1) / most;
+  l.splits = (l.tiles + per - 1) / per;
+  l.lda = (s->d + DK - 1) / DK * DK;
+  l.ldp = (int64_t)l.tiles * BM;
+  const int64_t blocks = (int64_t)((l.pass_rows + 127) / 128) * ((s->d + 127) / 128), steps = (s->V + 31) / 32;
+  int64_t back = (1024 + blocks - 1) / blocks;
+  if (back > 64) back = 64;
+  if (back > steps) back = steps;
+  l.back_splits = (int)back;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return at;
+  };
+  const size_t rows = (size_t)l.pass_rows;
+  l.z = take(rows * k * sizeof(float));
+  l.stats = take(rows * l.splits * 4 * sizeof(float4));
+  l.panel = take(l.lda != s->d ? rows * l.lda * 2 : 0);
+  if (needs == BACKWARD) {
+    l.terms = take(rows * sizeof(RowTerms));
+    l.list = take(rows * k * sizeof(float2));
+    l.ref = take(rows * l.tiles * sizeof(float));
+    l.P = take(rows * l.ldp * 2);
+    l.part = take(rows * l.back_splits * s->d * sizeof(float));
+  }
+  l.total = off;
+  return l;
+}
+
+template <class T>
+T* at(void* workspace, size_t offset) {
+  return reinterpret_cast<T*>(static_cast<unsigned char*>(workspace) + offset);
+}
+
+bool misaligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+int check(const ll_shape* shape, void* workspace, size_t workspace_bytes, size_t need, const void* rows, const void* W_U, float temperature,
+          const int32_t* ids) {
+  if (rows == nullptr || W_U == nullptr || ids == nullptr || !(temperature > 0.f) || isinf(temperature)) return LL_EINVAL;
+  if (!(LOG2E / temperature > 0.f) || isinf(LOG2E / temperature)) return LL_EINVAL;
+  if (misaligned(rows, 16) || misaligned(W_U, 16) || misaligned(ids, 4)) return LL_EINVAL;
+  if (workspace == nullptr || workspace_bytes < need || misaligned(workspace, 256)) return LL_EWORKSPACE;
+  return LL_OK;
+}
+
+struct Pass {
+  const ll_shape* shape;
+  const LearnPlan& l;
+  void* ws;
+  const uint16_t* rows;
+  const uint16_t* W;
+  float to_log2;
+  int n, k;
+  hipStream_t stream;
+
+  int list_logits(const int32_t* ids) const {
+    const int64_t entries = (int64_t)n * k;
+    hipLaunchKernelGGL(ll_learn_list_logits_kernel, dim3((unsigned)((entries + 3) / 4)), dim3(256), 0, stream, rows, W, ids, entries, k, shape->d,
+                       shape->V, at<float>(ws, l.z));
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  }
+
+  template <int WHAT>
+  int logits() const {
+    LearnArgs p = {};
+    p.A = rows;
+    if (l.lda != shape->d) {
+      hipLaunchKernelGGL(ll_learn_pad_kernel, dim3(n), dim3(256), 0, stream, rows, at<uint16_t>(ws, l.panel), shape->d, l.lda);
+      LL_HIP_CHECK(hipGetLastError());
+      p.A = at<uint16_t>(ws, l.panel);
+    }
+    p.W = W;
+    p.stats = at<float4>(ws, l.stats);
+    p.lda = l.lda;
+    p.rows = n;
+    p.d = shape->d;
+    p.V = shape->V;
+    p.splits = l.splits;
+    p.tiles = l.tiles;
+    p.row_blocks = (n + BN - 1) / BN;
+    p.last_row = n - 1;
+    p.group_rows = group_rows(p.row_blocks, p.splits);
+    p.to_log2 = to_log2;
+    if (WHAT != STATS) {
+      p.P = at<uint16_t>(ws, l.P);
+      p.ldp = l.ldp;
+      p.ref = at<float>(ws, l.ref);
+      p.terms = at<RowTerms>(ws, l.terms);
+    }
+    const auto kernel = l.lda != shape->d ? ll_learn_logits_kernel<WHAT, true> : ll_learn_logits_kernel<WHAT, false>;
+    const size_t lds = (size_t)SLOTS * SLOT_BYTES;
+    if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
+    const unsigned groups = (unsigned)((p.row_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  }
+
+  // P to the gradient of the rows
+  int back(uint16_t* out) const {
+    const int64_t entries = (int64_t)n * k;
+    hipLaunchKernelGGL(ll_learn_put_list_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, at<float2>(ws, l.list), entries, k,
+                       at<uint16_t>(ws, l.P), l.ldp);
+    LL_HIP_CHECK(hipGetLastError());
+    BackArgs p = {};
+    p.P = at<uint16_t>(ws, l.P);
+    p.W = W;
+    p.part = at<float>(ws, l.part);
+    p.ldp = l.ldp;
+    p.rows = n;
+    p.d = shape->d;
+    p.V = shape->V;
+    p.splits = l.back_splits;
+    p.steps = (shape->V + 31) / 32;
+    hipLaunchKernelGGL(ll_learn_back_kernel, dim3((shape->d + 127) / 128, (n + 127) / 128, p.splits), dim3(256), 0, stream, p);
+    LL_HIP_CHECK(hipGetLastError());
+    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 2047) / 2048, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
+                       at<RowTerms>(ws, l.terms), out);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  }
+};
+
+template <class F>
+int for_passes(const ll_shape* shape, const LearnPlan& l, void* ws, const void* rows, const void* W, float temperature, int k, void* stream, F f) {
+  for (int64_t r0 = 0; r0 < shape->N; r0 += l.pass_rows) {
+    const int n = (int)(shape->N - r0 < l.pass_rows ? shape->N - r0 : l.pass_rows);
+    const Pass pass = {shape, l, ws, (const uint16_t*)rows + r0 * shape->d, (const uint16_t*)W, LOG2E / temperature, n, k, (hipStream_t)stream};
+    if (const int rc = f(pass, r0); rc != LL_OK) return rc;
+  }
+  return LL_OK;
+}
+
+#define LL_TRY(expr) \
+  if (const int rc__ = (expr); rc__ != LL_OK) return rc__
+
+}  // namespace
+
+extern "C" {
+
+size_t ll_logp_workspace_bytes(const ll_shape* shape, int k) { return valid(shape, k) ? plan_for(shape, k, FORWARD).total : 0; }
+
+int ll_logp(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+            const int32_t* ids, float* out_logp, float* out_lse, float* out_entropy, void* stream) {
+  if (!valid(shape, k)) return LL_EINVAL;
+  if (shape->N == 0) return LL_OK;
+  if (out_logp == nullptr || out_lse == nullptr || out_entropy == nullptr) return LL_EINVAL;
+  if (misaligned(out_logp, 4) || misaligned(out_lse, 4) || misaligned(out_entropy, 4)) return LL_EINVAL;
+  const LearnPlan l = plan_for(shape, k, FORWARD);
+  LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
+  return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
+    LL_TRY(p.list_logits(ids + r0 * k));
+    LL_TRY(p.logits<STATS>());
+    hipLaunchKernelGGL(ll_logp_finish_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float4>(workspace, l.stats), 4 * l.splits,
+                       at<float>(workspace, l.z), ids + r0 * k, p.n, k, shape->V, p.to_log2, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  });
+}
+
+size_t ll_logp_grad_workspace_bytes(const ll_shape* shape, int k) { return valid(shape, k) ? plan_for(shape, k, BACKWARD).total : 0; }
+
+int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+                 const int32_t* ids, const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* out_grad,
+                 void* stream) {
+  if (!valid(shape, k)) return LL_EINVAL;
+  if (shape->N == 0) return LL_OK;
+  if (lse == nullptr || g_logp == nullptr || out_grad == nullptr || (g_entropy != nullptr && entropy == nullptr)) return LL_EINVAL;
+  if (misaligned(lse, 4) || misaligned(entropy, 4) || misaligned(g_logp, 4) || misaligned(g_entropy, 4) || misaligned(out_grad, 16)) return LL_EINVAL;
+  const LearnPlan l = plan_for(shape, k, BACKWARD);
+  LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
+  return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
+    LL_TRY(p.list_logits(ids + r0 * k));
+    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float>(workspace, l.z), ids + r0 * k, lse + r0,
+                       entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, p.n, k,
+                       shape->V, temperature, p.to_log2, at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list));
+    LL_HIP_CHECK(hipGetLastError());
+    LL_TRY(p.logits<GRAD>());
+    return p.back((uint16_t*)out_grad + r0 * shape->d);
+  });
+}
+
+size_t ll_distill_workspace_bytes(const ll_shape* shape, int k) { return ll_logp_grad_workspace_bytes(shape, k); }
+
+int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
+               const int32_t* teacher_ids, const float* teacher_scores, const float* weight, float* out_loss, void* out_grad, void* stream) {
+  if (!valid(shape, k)) return LL_EINVAL;
+  if (shape->N == 0) return LL_OK;
+  if (teacher_scores == nullptr || out_loss == nullptr) return LL_EINVAL;
+  if (misaligned(teacher_scores, 4) || misaligned(weight, 4) || misaligned(out_loss, 4) || misaligned(out_grad, 16)) return LL_EINVAL;
+  const LearnPlan l = plan_for(shape, k, out_grad != nullptr ? BACKWARD : FORWARD);
+  LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, teacher_ids));
+  return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
+    const bool grad = out_grad != nullptr;
+    LL_TRY(p.list_logits(teacher_ids + r0 * k));
+    LL_TRY(grad ? p.logits<EXPS>() : p.logits<STATS>());
+    hipLaunchKernelGGL(ll_distill_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float4>(workspace, l.stats), 4 * l.splits,
+                       at<float>(workspace, l.z), teacher_ids + r0 * k, teacher_scores + r0 * k, weight != nullptr ? weight + r0 : nullptr, p.n, k,
+                       shape->V, temperature, p.to_log2, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
+                       grad ? at<float2>(workspace, l.list) : nullptr);
+    LL_HIP_CHECK(hipGetLastError());
+    if (!grad) return LL_OK;
+    hipLaunchKernelGGL(ll_distill_scale_kernel, dim3((unsigned)((l.ldp + 2047) / 2048), p.n), dim3(256), 0, p.stream,
+                       at<uint16_t>(workspace, l.P), l.ldp, at<float>(workspace, l.ref), l.tiles, at<RowTerms>(workspace, l.terms));
+    LL_HIP_CHECK(hipGetLastError());
+    return p.back((uint16_t*)out_grad + r0 * shape->d);
+  });
+}
+
+}  // extern "C"

@@ -789,21 +789,6 @@ void (*few_kernel(int nj, int mu))(const FewArgs) {
   return nullptr;
 }
 
-// A kernel that uses more than 64 KB of dynamic LDS has to be told so once per device; remembered
-// here so that the hot path makes no attribute call.
-int allow_dynamic_lds(const void* kern, size_t lds) {
-  static std::mutex mu;
-  static std::vector<std::pair<int, const void*>> done;
-  int dev = -1;
-  LL_HIP_CHECK(hipGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  for (const auto& e : done)
-    if (e.first == dev && e.second == kern) return LL_OK;
-  LL_HIP_CHECK(hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  done.emplace_back(dev, kern);
-  return LL_OK;
-}
-
 // Most tiles a workgroup for which the kernel of short calls is taken, with the classes of splits and without (half tiles only).
 // Whole calls, us, long | short (d, V, rows, k: tiles a workgroup).  With classes: 256, 4096, 1500, 10 (1, in halves): 50 | 30; 1608,
 // 50257, 777, 3 with a bias (4): 197 | 187; 1024, 50257, 1500, 20 (5): 229 | 189; 4096, 128256, 957, 10 (8): 847 | 830; 1024,
