@@ -319,7 +319,7 @@ int ll_block_norm_grad(const ll_shape* shape, void* workspace, size_t workspace_
  *
  *   rows  bf16 [N, d], already normalised (out_normed of ll_block_norm, the output of ll_steer_inject)
  *   W_U   bf16 [V, d];  ids int32 [N, k], 1 <= k <= LL_LIST_MAX, any order, repeats allowed;  temperature positive, finite
- * d a multiple of 8, at most 65536.  (The most likely tokens besides are ll_project's matter.)
+ * d a multiple of 8, at most 65536, V at most 2^22.  (The most likely tokens besides are ll_project's matter.)
  *
  * ll_logp_grad: from lse and entropy as ll_logp returned them (entropy only with g_entropy), g_logp [N, k] and g_entropy [N] or NULL,
  *

@@ -60,6 +60,13 @@ struct GemmArgs {
   float alpha_most;         // largest |alpha|
 };
 
+// The product backwards, A W with A [rows, V] (see ll_gemm_lds.h): A, W, lda, rows, V, splits (slices of the vocabulary), row_blocks and
+// last_row as above, d the product's columns.
+struct BackArgs : GemmArgs {
+  float* part;              // [splits, rows, d]: the slices' products
+  int col_blocks;           // of 256 columns
+};
+
 using GemmKernel = void (*)(const GemmArgs);
 
 // The direct-to-LDS kernels for a d that is not a multiple of 64 (ll_project_tail.hip); nullptr where there is none (the longest
@@ -613,7 +620,7 @@ __device__ __forceinline__ void epilogue_store(const GemmArgs& p, const RowState
 template <int KR, bool BIAS = false, bool SHORT = false>
 struct TopKEpilogue {   // a5..a7: softmax statistics, k best logits, target logit (BIAS: Eq. 1's b added to every logit first)
   using State = RowState<KR>;
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false;
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false;
   static constexpr int ROWS = BN;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ void init(State& st, const GemmArgs& p, int my_row, int split) {

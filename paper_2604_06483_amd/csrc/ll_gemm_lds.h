@@ -61,6 +61,15 @@ namespace {
 // again).  In code of its own: one body with branches around the slices that a half tile leaves out makes the register allocator
 // copy accumulators to memory.  A half tile takes 0.6 of a whole one's time (d = 1608: 49 000 cycles, and 82 000).  197 tiles over 64
 // splits are four a workgroup; 393 half tiles are seven.
+//
+// EPI::BACK: the product backwards, C [rows, d] = A W with A [rows, V] (the gradient of the logits) and K over the vocabulary.  A is loaded
+// as above.  A stage of W is 64 vocabulary rows by the tile's 256 columns, [64 rows][512 B] in its slot, and K goes down its columns:
+// the fragments are read with ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows, two of them a fragment.  A
+// lane group's eight K are rows 4 g .. + 3 and 16 + 4 g .. + 3 of a half's 32, and A's columns stand in that order within every 32
+// (place_in_p in ll_learn.hip), so that both halves of a read are whole rows apart.  The 32-byte pieces of a row are XOR-swizzled with the
+// row's last three bits: the eight rows that half a wavefront reads from, all at one multiple of 512 bytes, then lie in different banks.
+// A workgroup has one tile, of 256 rows by 256 columns, and one slice of the vocabulary.  Rows of W past the last are the last one's
+// again, where A holds zeros; columns past the last chunk are its own again, and are not stored.
 // ---------------------------------------------------------------------------------------
 constexpr int DK = 64;
 constexpr int W_SLOTS = 3, A_SLOTS = 2, SLOTS = W_SLOTS + A_SLOTS;
@@ -70,6 +79,8 @@ constexpr int LOADS_PER_TILE = 8;    // per wavefront: 8 segments of 1 KB of one
 constexpr int waitcnt_imm(int vmcnt, int lgkmcnt) { return (vmcnt & 0xF) | ((vmcnt >> 4) << 14) | 0x70 | (lgkmcnt << 8); }
 
 typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
 // One global_load_lds_dwordx4: every lane fetches 16 bytes from base + off + IMM and the
@@ -109,16 +120,40 @@ __device__ __forceinline__ f32x4 mfma16_from_zero(bf16x8 a, bf16x8 b) {
   return c;
 }
 
+// One column of four rows a lane, twice: 16 rows apart.
+__device__ __forceinline__ bf16x8 read_transposed(const unsigned char* from) {
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)from);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + 16 * (BM * 2)));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// BACK: slice by slice, of a slice column block by column block, of a column block row block by row block: the 32 workgroups that an
+// XCD runs at a time are a rectangle of up to eight row blocks, and share A's and W's tiles in its L2.
+__device__ __forceinline__ int back_col_blocks(const GemmArgs& p) { return static_cast<const BackArgs&>(p).col_blocks; }
+__device__ __forceinline__ Place place_back(unsigned logical, const GemmArgs& p) {
+  const unsigned rows = p.row_blocks;
+  return {(int)(logical % rows), (int)(logical / (rows * back_col_blocks(p)))};
+}
+__device__ __forceinline__ int column_block(unsigned logical, const GemmArgs& p) { return (int)(logical / p.row_blocks % back_col_blocks(p)); }
+
 template <class EPI, bool TAIL, bool SHORT = false>
 __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* const smem) {
 
   const int logical = xcd_logical_block();
-  if (__builtin_expect(logical >= p.row_blocks * p.splits || EPI::skip(p), 0)) return;
-  const Place at = place_of(logical, p);
+  if (__builtin_expect(logical >= p.row_blocks * p.splits * (EPI::BACK ? back_col_blocks(p) : 1) || EPI::skip(p), 0)) return;
+  constexpr bool BACK = EPI::BACK;
+  const Place at = BACK ? place_back(logical, p) : place_of(logical, p);
   const int split = at.split, rb = at.row_block;
   // the split's tiles; SHORT: counted from its first vocabulary row, row0, up to row_end
   int tile0 = (int)((int64_t)split * p.tiles / p.splits);
   int tile1 = (int)((int64_t)(split + 1) * p.tiles / p.splits);
+  // BACK: the one tile of columns, and the slice's K stages
+  const int stages = BACK ? (p.V + DK - 1) / DK : 0;
+  const int stage0 = BACK ? (int)((int64_t)split * stages / p.splits) : 0;
+  if (BACK) {
+    tile0 = column_block(logical, p);
+    tile1 = tile0 + 1;
+  }
   int row0 = 0, row_end = p.V;
   bool ends_in_half = false;
   if (SHORT) {
@@ -139,7 +174,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d = p.d;
   const int lda = (int)p.lda;
-  const int KT = lda / DK;
+  const int KT = BACK ? (int)((int64_t)(split + 1) * stages / p.splits) - stage0 : lda / DK;
 
   // --- DMA map.  One load instruction fills 8 rows x 128 B; lane l lands at row l/8, physical
   // chunk l%8.  Wavefront w fills rows [64w, 64w+64) of a tile in 8 segments; segment s holds
@@ -176,6 +211,16 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
     for (int s = 0; s < 8; ++s) w_off[s] -= (s & 1) ? odd : even;
   };
   auto set_w_rows = [&](int tile) {
+    if constexpr (BACK) {   // (tile: the stage; of the last one the rows past the vocabulary are its last again)
+      const int w_last = p.V - 1 - tile * DK;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const int row = 16 * wave + 2 * s + (lane >> 5);
+        const int chunk = ((lane & 31) ^ (2 * (row & 7))) + tile0 * (BM / 8);
+        w_off[s] = (unsigned)(min(row, w_last) * d + min(chunk * 8, d - 8)) * 2u + (7168u - 1024u * s);
+      }
+      return;
+    }
     const int w_last = row_end - 1 - row0 - tile * BM;
     int l = lane;
     if (EPI::RELOAD_FRAGMENTS) asm volatile("" : "+v"(l));   // (made anew for every tile: 18 registers less to keep)
@@ -197,8 +242,9 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   const unsigned lds_mid = (unsigned)(uintptr_t)(lptr_t)smem + wave * (64 * DK * 2) + 4096;
   const unsigned w_lds_wrap = lds_mid + W_SLOTS * SLOT_BYTES;
   const unsigned a_lds_flip = (2 * W_SLOTS + 1) * SLOT_BYTES + 2 * lds_mid;   // slot 3 <-> slot 4
-  const unsigned char* const a_base0 = reinterpret_cast<const unsigned char*>(p.A + (int64_t)rb * ROWS * lda) - IMM_BIAS;
+  const unsigned char* const a_base0 = reinterpret_cast<const unsigned char*>(p.A + (int64_t)rb * ROWS * lda + (BACK ? (int64_t)stage0 * DK : 0)) - IMM_BIAS;
   auto w_tile_base = [&](int tile) {
+    if constexpr (BACK) return reinterpret_cast<const unsigned char*>(p.W + (int64_t)tile * DK * d) - IMM_BIAS;
     return reinterpret_cast<const unsigned char*>(p.W + ((int64_t)tile * BM + row0) * d) - IMM_BIAS;
   };
   // (LL_PIN_S: the value is computed where the statement stands; without it the compiler gathers
@@ -206,12 +252,21 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #define LL_PIN_S(x) asm volatile("" : "+s"(x))
   int w_tile = tile0, w_kt = 0;
   unsigned w_lds = lds_mid, a_lds = lds_mid + W_SLOTS * SLOT_BYTES;   // M0 value of the stream's next tile
-  const unsigned char* w_base = w_tile_base(tile0);
+  const unsigned char* w_base = w_tile_base(BACK ? stage0 : tile0);
   const unsigned char* a_base = a_base0;
-  set_w_rows(tile0);
+  set_w_rows(BACK ? stage0 : tile0);
   auto advance_w = [&]() {
     w_lds += SLOT_BYTES;
     if (w_lds >= w_lds_wrap) w_lds -= W_SLOTS * SLOT_BYTES;
+    if constexpr (BACK) {   // the next 64 vocabulary rows; past the slice's end its last ones again
+      if (++w_kt < KT) {
+        w_base += (int64_t)DK * 2 * d;
+        if (stage0 + w_kt == stages - 1) set_w_rows(stage0 + w_kt);
+      }
+      LL_PIN_S(w_lds);
+      LL_PIN_S(w_base);
+      return;
+    }
     w_base += DK * 2;
     if (++w_kt == KT) {   // next vocabulary tile; past the end of the sweep the ring refetches the last one
       w_kt = 0;
@@ -246,6 +301,13 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   int f_off[2];
 #pragma unroll
   for (int hk = 0; hk < 2; ++hk) f_off[hk] = f_row * (DK * 2) + (((4 * hk + f_grp) ^ f_swz) * 16);
+  // BACK: where the lane's four columns of row 4 (lane / 16) + lane % 16 / 4 are, of column tile 0 of a 256-byte piece; of tile t this ^ 32 t
+  const int b_off = BACK ? (4 * f_grp + (f_row >> 2)) * (BM * 2) + ((4 * f_grp + (f_row >> 2)) & 7) * 32 + (f_row & 3) * 8 : 0;
+#define LL_LDS_FRAG(ptr) (*reinterpret_cast<const bf16x8*>(ptr))
+  // Fragment of 16 vocabulary rows (BACK: columns) and one K half of the stage at LDS offset `tile_off`.
+#define LL_W_FRAG(tile_off, t, hk)                                                                  \
+  (BACK ? read_transposed(smem + tile_off + (hk) * 32 * (BM * 2) + ((t) >> 3) * 256 + (b_off ^ ((t) & 7) * 32)) \
+        : LL_LDS_FRAG(smem + tile_off + (t) * 16 * (DK * 2) + f_off[hk]))
   const int a_wave_off = (wave * 64) * (DK * 2);
 
   const int my_row = ROWS == BN || tid < ROWS ? rb * ROWS + tid : INT_MAX;
@@ -280,7 +342,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #pragma unroll
       for (int j = 0; j < 4; ++j) fa[hk][j] = *reinterpret_cast<const bf16x8*>(smem + a_tile_off + j * 16 * (DK * 2) + f_off[hk]);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) fw0[q] = *reinterpret_cast<const bf16x8*>(smem + w_tile_off + (q >> 1) * 16 * (DK * 2) + f_off[q & 1]);
+    for (int q = 0; q < 8; ++q) fw0[q] = LL_W_FRAG(w_tile_off, q >> 1, q & 1);
   };
   read_fragments(0, W_SLOTS * SLOT_BYTES + a_wave_off);
 
@@ -305,7 +367,6 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   // has not come back by then; measured 0.4 to 1.9 % per launch over the spread placement.  (The
   // same move in slice 3, whose fragments the next stage's slice 0 needs as early, measured
   // nothing: that slice's gaps already hold the eight A fragment reads.)
-#define LL_LDS_FRAG(ptr) (*reinterpret_cast<const bf16x8*>(ptr))
   // Written as an instruction so that the 64 accumulator tiles stay in AGPRs: given the builtin,
   // the register allocator keeps some of them in VGPRs and copies them in and out around the MFMA.
   // (Operands come from LDS reads, whose waits the compiler still places; nothing reads an
@@ -326,8 +387,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   acc[4 * S + LL_T(JO, P)][LL_J(JO, P)] =                                                                            \
       LL_MFMA16(fw[2 * LL_T(JO, P) + 1], fa[1][LL_J(JO, P)], acc[4 * S + LL_T(JO, P)][LL_J(JO, P)]);                 \
   if (RD(P) >= 0) { /* fragment q = RD(P): vocabulary tile 4 NS + q / 2, K half q % 2 */                            \
-    nw[RD(P) >= 0 ? RD(P) : 0] =                                                                                     \
-        LL_LDS_FRAG(smem + tW + (4 * NS + (RD(P) >= 0 ? RD(P) : 0) / 2) * 16 * (DK * 2) + f_off[(RD(P) >= 0 ? RD(P) : 0) & 1]); \
+    nw[RD(P) >= 0 ? RD(P) : 0] = LL_W_FRAG(tW, 4 * NS + (RD(P) >= 0 ? RD(P) : 0) / 2, (RD(P) >= 0 ? RD(P) : 0) & 1);     \
   }                                                                                                                  \
   HOOK(P);                                                                                                           \
   AOUT(P);                                                                                                           \
@@ -495,6 +555,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #undef LL_MFMA16_Z
 #undef LL_MFMA16
 #undef LL_LDS_FRAG
+#undef LL_W_FRAG
 #undef LL_DMA_TILE
 #undef LL_HOOK_S3
 #undef LL_HOOK_HALF

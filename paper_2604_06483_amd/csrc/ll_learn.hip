@@ -44,7 +44,7 @@ struct LearnEpilogue {
     float m[4], s[4], t[4];
     RowTerms terms[WHAT == GRAD ? 4 : 1];
   };
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false;
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false;
   static constexpr int ROWS = BN;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
@@ -338,78 +338,40 @@ __global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __
   if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(q.x, 0.f);
 }
 
-// ---------------------------------------------------------------------------------------
-// dA = dz W over one slice of the vocabulary: a workgroup has 128 rows by 128 columns, four wavefronts of 64 by 64, K steps of 32.
-// W comes with the columns in a row; its fragments are read transposed out of LDS.
-// ---------------------------------------------------------------------------------------
-struct BackArgs {
-  const uint16_t* P;      // [rows, ldp]
-  const uint16_t* W;      // [V, d]
-  float* part;            // [splits, rows, d]
-  int64_t ldp;
-  int rows, d, V, splits, steps;   // steps of 32 ids in all
+// dA = dz W over one slice of the vocabulary: the tile as it is.  A lane has four columns of a row in each 16.
+struct BackEpilogue {
+  struct State {
+    int split;
+  };
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = true;
+  static constexpr int ROWS = BN;
+  static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
+  static __device__ __forceinline__ void init(State& st, const GemmArgs&, int, int split) { st.split = split; }
+  template <class ACC>
+  static __device__ __forceinline__ void tile(const ACC& acc, State& st, int c0, const GemmArgs& args, int my_row) {
+    const BackArgs& p = static_cast<const BackArgs&>(args);
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA's result is in its registers
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = my_row - lane + 16 * j + (lane & 15);
+      if (row >= p.rows) continue;
+      const int c = c0 + 4 * (lane >> 4);
+      float* const to = p.part + ((int64_t)st.split * p.rows + row) * p.d + c;
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        if (c + 16 * t < p.d)
+          *reinterpret_cast<float4*>(to + 16 * t) = make_float4(acc_read(acc[t][j][0]), acc_read(acc[t][j][1]), acc_read(acc[t][j][2]), acc_read(acc[t][j][3]));
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(const GemmArgs&, const State&, int, int) {}
 };
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-
-__global__ __launch_bounds__(256) void ll_learn_back_kernel(const BackArgs p) {
-  __shared__ __align__(16) uint16_t sP[128][40];     // (rows of 80 bytes: sixteen of them start in different banks)
-  __shared__ __align__(16) uint16_t sW[32][128];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row0 = blockIdx.y * 128, col0 = blockIdx.x * 128, split = blockIdx.z;
-  const int step0 = (int)((int64_t)split * p.steps / p.splits), step1 = (int)((int64_t)(split + 1) * p.steps / p.splits);
-  const int wr = (wave & 1) * 64, wc = (wave >> 1) * 64;
-  const int g = lane >> 4, i16 = lane & 15;
-  f32x4 acc[4][4];   // [columns][rows]
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int step = step0; step < step1; ++step) {
-    uint4 a[2], w[2];
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int ar = min(row0 + (tid >> 2) + 64 * q, p.rows - 1);
-      a[q] = *reinterpret_cast<const uint4*>(p.P + ar * p.ldp + 32 * (int64_t)step + 8 * (tid & 3));
-      const int v = min(32 * step + (tid >> 4) + 16 * q, p.V - 1), c = min(col0 + 8 * (tid & 15), p.d - 8);
-      w[q] = *reinterpret_cast<const uint4*>(p.W + (int64_t)v * p.d + c);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      *reinterpret_cast<uint4*>(&sP[(tid >> 2) + 64 * q][8 * (tid & 3)]) = a[q];
-      *reinterpret_cast<uint4*>(&sW[(tid >> 4) + 16 * q][8 * (tid & 15)]) = w[q];
-    }
-    __syncthreads();
-    bf16x8 fp[4], fw[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) fp[j] = *reinterpret_cast<const bf16x8*>(&sP[wr + 16 * j + i16][8 * g]);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      // (place_in_p: the lane group's eight K are ids 4 g .. + 3 and 16 + 4 g .. + 3)
-      s16x4 half[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)&sW[16 * h + 4 * g + (i16 >> 2)][wc + 16 * t + 4 * (i16 & 3)]);
-      fw[t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[t], fp[j], acc[t][j], 0, 0, 0);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = row0 + wr + 16 * j + i16;
-    if (row >= p.rows) continue;
-    float* to = p.part + ((int64_t)split * p.rows + row) * p.d;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int c = col0 + wc + 16 * t + 4 * g;
-      if (c < p.d) *reinterpret_cast<f32x4*>(to + c) = acc[t][j];
-    }
-  }
+__global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void ll_learn_back_kernel(const BackArgs p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  lens_gemm_dma<BackEpilogue, false>(p, smem);
 }
 
 // The slices joined, in order; a row that takes no part gets zeros whatever W holds.
@@ -441,21 +403,37 @@ __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restr
 // ---------------------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------------------
-constexpr int MAX_LEARN_D = 65536;
+constexpr int LEARN_MAX_D = 65536, LEARN_MAX_V = 1 << 22;   // (a lane's offsets within 256 rows of P, or of W, fit 32 bits)
 
 bool valid(const ll_shape* s, int k) {
-  return s != nullptr && s->N >= 0 && s->N <= INT32_MAX && s->d > 0 && s->d % 8 == 0 && s->d <= MAX_LEARN_D && s->V > 0 &&
-         s->V <= INT32_MAX - BM && k >= 1 && k <= LL_LIST_MAX;
+  return s != nullptr && s->N >= 0 && s->N <= INT32_MAX && s->d > 0 && s->d % 8 == 0 && s->d <= LEARN_MAX_D && s->V > 0 &&
+         s->V <= LEARN_MAX_V && k >= 1 && k <= LL_LIST_MAX;
 }
 
 enum Needs { FORWARD, BACKWARD };
 
 struct LearnPlan {
   int pass_rows, tiles, splits, row_blocks;
-  int back_splits;
+  int col_blocks, back_splits;
   int64_t lda, ldp;
   size_t panel, z, stats, terms, list, ref, P, part, total;
 };
+
+// Slices of the vocabulary for the product backwards: one workgroup a compute unit at a time, so that `tiles` of it take whole rounds,
+// of a stage's 1.5 us each (and three to fill and empty the ring); a slice more is written and read, at some 4 TB/s.
+int slices(int64_t tiles, int stages, int rows, int d) {
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 64 && s <= stages; ++s) {
+    const double rounds = (double)((tiles * s + NUM_CU - 1) / NUM_CU);
+    const double us = rounds * ((stages + s - 1) / s + 3) * 1.5 + s * (double)rows * d * 8 / 4e6;
+    if (us < least) {
+      least = us;
+      best = s;
+    }
+  }
+  return best;
+}
 
 LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
   LearnPlan l = {};
@@ -469,11 +447,8 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
   l.splits = (l.tiles + per - 1) / per;
   l.lda = (s->d + DK - 1) / DK * DK;
   l.ldp = (int64_t)l.tiles * BM;
-  const int64_t blocks = (int64_t)((l.pass_rows + 127) / 128) * ((s->d + 127) / 128), steps = (s->V + 31) / 32;
-  int64_t back = (1024 + blocks - 1) / blocks;
-  if (back > 64) back = 64;
-  if (back > steps) back = steps;
-  l.back_splits = (int)back;
+  l.col_blocks = (s->d + BM - 1) / BM;
+  l.back_splits = slices(l.row_blocks * l.col_blocks, (s->V + DK - 1) / DK, l.pass_rows, s->d);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -572,16 +547,21 @@ struct Pass {
                        at<uint16_t>(ws, l.P), l.ldp);
     LL_HIP_CHECK(hipGetLastError());
     BackArgs p = {};
-    p.P = at<uint16_t>(ws, l.P);
+    p.A = at<uint16_t>(ws, l.P);
     p.W = W;
     p.part = at<float>(ws, l.part);
-    p.ldp = l.ldp;
+    p.lda = l.ldp;
     p.rows = n;
+    p.last_row = n - 1;
     p.d = shape->d;
     p.V = shape->V;
     p.splits = l.back_splits;
-    p.steps = (shape->V + 31) / 32;
-    hipLaunchKernelGGL(ll_learn_back_kernel, dim3((shape->d + 127) / 128, (n + 127) / 128, p.splits), dim3(256), 0, stream, p);
+    p.row_blocks = (n + BN - 1) / BN;
+    p.col_blocks = l.col_blocks;
+    const size_t lds = (size_t)SLOTS * SLOT_BYTES;
+    if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(ll_learn_back_kernel), lds); rc != LL_OK) return rc;
+    const unsigned groups = (unsigned)((p.row_blocks * p.col_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
+    hipLaunchKernelGGL(ll_learn_back_kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 2047) / 2048, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
                        at<RowTerms>(ws, l.terms), out);

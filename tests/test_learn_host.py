@@ -84,7 +84,7 @@ def test_lens_calls(name, names, required, aligned):
         assert call(**{n: fake((1 << 20) + 8)}) == LL.LL_EINVAL, n
     for n in set(names) - {"shape", "ws", "wsb", "temperature", "k", "stream"}:
         assert call(**{n: fake((1 << 20) + 2)}) == LL.LL_EINVAL, n
-    for N, d, V in ((-1, 64, 300), (2 ** 31, 64, 300), (16, 0, 300), (16, 60, 300), (16, 65544, 300), (16, 64, 0), (16, 64, -5), (16, 64, 2 ** 31 - 1)):
+    for N, d, V in ((-1, 64, 300), (2 ** 31, 64, 300), (16, 0, 300), (16, 60, 300), (16, 65544, 300), (16, 64, 0), (16, 64, -5), (16, 64, 2 ** 22 + 1), (16, 64, 2 ** 31 - 1)):
         assert call(shape=LL.ll_shape(N, d, V)) == LL.LL_EINVAL, (N, d, V)
         assert getattr(LL, name + "_workspace_bytes")(N, d, V, 4) == 0
     for k in (0, -1, LL.LL_LIST_MAX + 1):
