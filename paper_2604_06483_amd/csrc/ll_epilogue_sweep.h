@@ -938,7 +938,7 @@ template <int KS, bool GENERAL, bool OWN>
 struct AnySweepEpilogue {
   using State = SweepState<KS, GENERAL>;
   static constexpr bool RELOAD_FRAGMENTS = true, OWN_U = OWN, BACK = false;
-  static constexpr int ROWS = OWN_U ? SWEEP_OWN_ROWS : BN;
+  static constexpr int ROWS = OWN_U ? SWEEP_OWN_ROWS : BN, ROW_TILES = 4;
   static __device__ __forceinline__ bool skip(const GemmArgs& p) {
     if (OWN_U) {
       if (p.only_general) return false;   // (the host launches no other)

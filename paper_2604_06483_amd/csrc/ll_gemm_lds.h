@@ -62,6 +62,10 @@ namespace {
 // copy accumulators to memory.  A half tile takes 0.6 of a whole one's time (d = 1608: 49 000 cycles, and 82 000).  197 tiles over 64
 // splits are four a workgroup; 393 half tiles are seven.
 //
+// EPI::ROW_TILES below 4: a wavefront has that many tiles of 16 lens rows, a workgroup 64 times that many rows.  Everything goes on as with
+// four but for the matrix instructions, A's loads and A's fragments of the others: for calls of few rows, or whose rows
+// fill blocks of 256 badly.
+//
 // EPI::BACK: the product backwards, C [rows, d] = A W with A [rows, V] (the gradient of the logits) and K over the vocabulary.  A is loaded
 // as above.  A stage of W is 64 vocabulary rows by the tile's 256 columns, [64 rows][512 B] in its slot, and K goes down its columns:
 // the fragments are read with ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows, two of them a fragment.  A
@@ -142,6 +146,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   const int logical = xcd_logical_block();
   if (__builtin_expect(logical >= p.row_blocks * p.splits * (EPI::BACK ? back_col_blocks(p) : 1) || EPI::skip(p), 0)) return;
   constexpr bool BACK = EPI::BACK;
+  constexpr int RT = EPI::ROW_TILES, A_LOADS = LOADS_PER_TILE / 4 * RT;
   const Place at = BACK ? place_back(logical, p) : place_of(logical, p);
   const int split = at.split, rb = at.row_block;
   // the split's tiles; SHORT: counted from its first vocabulary row, row0, up to row_end
@@ -195,7 +200,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   unsigned a_off[8], w_off[8];
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
-    int row = min(seg_row + 8 * s, a_last);
+    int row = min((RT < 4 ? 16 * RT * wave + (lane >> 3) : seg_row) + 8 * s, a_last);
     if (EPI::OWN_U && seg_row + 8 * s >= ROWS) row = a_last + 1 - ROWS + seg_row + 8 * s;   // the direction's, behind the row of zeros
     a_off[s] = (unsigned)(row * lda + ((s & 1) ? seg_koff1 : seg_koff0)) * 2u + (7168u - 1024u * s);
   }
@@ -289,7 +294,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
     LL_PIN_S(a_base);
   };
 #define LL_DMA_W(S) load_to_lds_16<((S) - 4) * 1024>(w_base, w_off[S])
-#define LL_DMA_A(S) load_to_lds_16<((S) - 4) * 1024>(a_base, a_off[S])
+#define LL_DMA_A(S) if constexpr ((S) < A_LOADS) load_to_lds_16<((S) - 4) * 1024>(a_base, a_off[S])
 #define LL_DMA_TILE(DMA) DMA(0); DMA(1); DMA(2); DMA(3); DMA(4); DMA(5); DMA(6); DMA(7)
 
   // --- MFMA fragment map (v_mfma_f32_16x16x32_bf16): lane reads row (lane % 16) of each 16-row
@@ -310,7 +315,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
         : LL_LDS_FRAG(smem + tile_off + (t) * 16 * (DK * 2) + f_off[hk]))
   const int a_wave_off = (wave * 64) * (DK * 2);
 
-  const int my_row = ROWS == BN || tid < ROWS ? rb * ROWS + tid : INT_MAX;
+  const int my_row = RT < 4 ? rb * ROWS + 16 * RT * wave + lane : ROWS == BN || tid < ROWS ? rb * ROWS + tid : INT_MAX;
   typename EPI::State st;
   EPI::init(st, p, my_row, split);
   if constexpr (SHORT) EPI::settle(st);
@@ -330,7 +335,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   advance_a();
   set_lds_dma_base(w_lds);
   LL_DMA_W(0); LL_DMA_W(1); LL_DMA_W(2); LL_DMA_W(3);
-  __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * LOADS_PER_TILE + 4, 15));   // W0 and A0 landed
+  __builtin_amdgcn_s_waitcnt(waitcnt_imm(LOADS_PER_TILE + A_LOADS + 4, 15));   // W0 and A0 landed
   if (TAIL && KT == 1) zero_tail(0);
   __syncthreads();
   // A: the four row tiles of both K halves of the stage.  W: two sets of eight fragments, each the
@@ -340,7 +345,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #pragma unroll
     for (int hk = 0; hk < 2; ++hk)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) fa[hk][j] = *reinterpret_cast<const bf16x8*>(smem + a_tile_off + j * 16 * (DK * 2) + f_off[hk]);
+      for (int j = 0; j < RT; ++j) fa[hk][j] = *reinterpret_cast<const bf16x8*>(smem + a_tile_off + j * 16 * (DK * 2) + f_off[hk]);
 #pragma unroll
     for (int q = 0; q < 8; ++q) fw0[q] = LL_W_FRAG(w_tile_off, q >> 1, q & 1);
   };
@@ -380,12 +385,14 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #define LL_RD_SPREAD(P) ((P) % 2 == 0 ? (P) / 2 : -1)
 #define LL_RD_AHEAD(P) ((P) <= 8 ? ((P) % 2 == 0 ? (P) / 2 : -1) : ((P) <= 11 ? (P) - 4 : -1))
 #define LL_PAIR(MF0, P, S, JO, fw, nw, tW, NS, AIN, AOUT, HOOK, RD)                                                 \
-  acc[4 * S + LL_T(JO, P)][LL_J(JO, P)] =                                                                            \
-      MF0(fw[2 * LL_T(JO, P)], fa[0][LL_J(JO, P)], acc[4 * S + LL_T(JO, P)][LL_J(JO, P)]);                           \
+  if constexpr (LL_J(JO, P) < RT)                                                                                    \
+    acc[4 * S + LL_T(JO, P)][LL_J(JO, P)] =                                                                          \
+        MF0(fw[2 * LL_T(JO, P)], fa[0][LL_J(JO, P)], acc[4 * S + LL_T(JO, P)][LL_J(JO, P)]);                         \
   AIN(P);                                                                                                            \
   LL_SCHED_FENCE();                                                                                                  \
-  acc[4 * S + LL_T(JO, P)][LL_J(JO, P)] =                                                                            \
-      LL_MFMA16(fw[2 * LL_T(JO, P) + 1], fa[1][LL_J(JO, P)], acc[4 * S + LL_T(JO, P)][LL_J(JO, P)]);                 \
+  if constexpr (LL_J(JO, P) < RT)                                                                                    \
+    acc[4 * S + LL_T(JO, P)][LL_J(JO, P)] =                                                                          \
+        LL_MFMA16(fw[2 * LL_T(JO, P) + 1], fa[1][LL_J(JO, P)], acc[4 * S + LL_T(JO, P)][LL_J(JO, P)]);               \
   if (RD(P) >= 0) { /* fragment q = RD(P): vocabulary tile 4 NS + q / 2, K half q % 2 */                            \
     nw[RD(P) >= 0 ? RD(P) : 0] = LL_W_FRAG(tW, 4 * NS + (RD(P) >= 0 ? RD(P) : 0) / 2, (RD(P) >= 0 ? RD(P) : 0) & 1);     \
   }                                                                                                                  \
@@ -416,11 +423,11 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   // after the first MFMA of its last pair, the K half 1 fragment after the second; both are read
   // for the next stage from its A tile (the wavefront's own rows), at LDS offset nA
 #define LL_AIN_S3(P)                                                                                   \
-  if ((P) % 4 == 3) fa[0][(P) / 4] = LL_LDS_FRAG(smem + nA + ((P) / 4) * 16 * (DK * 2) + f_off[0]);    \
-  if ((P) % 4 == 0 && (P) > 0) fa[1][((P) / 4 + 3) % 4] = LL_LDS_FRAG(smem + nA + (((P) / 4 + 3) % 4) * 16 * (DK * 2) + f_off[1])
+  if constexpr ((P) % 4 == 3 && (P) / 4 < RT) fa[0][(P) / 4] = LL_LDS_FRAG(smem + nA + ((P) / 4) * 16 * (DK * 2) + f_off[0]); \
+  if constexpr ((P) % 4 == 0 && (P) > 0 && ((P) / 4 + 3) % 4 < RT) fa[1][((P) / 4 + 3) % 4] = LL_LDS_FRAG(smem + nA + (((P) / 4 + 3) % 4) * 16 * (DK * 2) + f_off[1])
 #define LL_AOUT_S3(P)                                                                                  \
   if ((P) == 15) {                                                                                     \
-    fa[1][3] = LL_LDS_FRAG(smem + nA + 3 * 16 * (DK * 2) + f_off[1]);                                  \
+    if constexpr (RT == 4) fa[1][3] = LL_LDS_FRAG(smem + nA + 3 * 16 * (DK * 2) + f_off[1]);           \
     nA = a_flip - nA;   /* LDS reads return in order: the tile read from just now is the wavefront's to refill */ \
   }
   // (hooks: what goes behind pair P of the slice, besides a fragment read)
@@ -487,7 +494,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
     LL_SLICE(MF0, 1, 0, fw1, fw0, cW, 2, LL_A_NONE, LL_A_NONE, LL_HOOK_S1, LL_RD_SPREAD)               \
     LL_SLICE(MF0, 2, 0, fw0, fw1, cW, 3, LL_A_NONE, LL_A_NONE, LL_HOOK_S2, LL_RD_AHEAD)                \
     /* stage g+1 landed (W(g+2) and A(g+2) may still be out); all my reads of W(g) are done */         \
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * LOADS_PER_TILE, 0));                                    \
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(LOADS_PER_TILE + A_LOADS, 0));                                    \
     if (TAIL && (KT == 1 || (KTILE) == KT - 2)) zero_tail(nW);   /* stage g+1 is a row's last */        \
     __syncthreads();                                                                                   \
     LL_SLICE(MF0, 3, 1, fw1, fw0, nW, 0, LL_AIN_S3, LL_AOUT_S3, LL_HOOK_S3, LL_RD_SPREAD)
@@ -498,13 +505,13 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   // The same of half a tile: vocabulary rows 0 .. 127 of it.
 #define LL_HALF_STAGE(MF0, KTILE)                                                                      \
     LL_SLICE(MF0, 0, 1, fw0, fw1, cW, 1, LL_A_NONE, LL_A_NONE, LL_HOOK_HALF, LL_RD_AHEAD)              \
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * LOADS_PER_TILE, 0));                                    \
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(LOADS_PER_TILE + A_LOADS, 0));                                    \
     if (TAIL && (KT == 1 || (KTILE) == KT - 2)) zero_tail(nW);                                         \
     __syncthreads();                                                                                   \
     LL_SLICE(MF0, 1, 1, fw1, fw0, nW, 0, LL_AIN_S3, LL_AOUT_S3, LL_HOOK_S3, LL_RD_SPREAD)
   const int end = SHORT && ends_in_half ? tile1 - 1 : tile1;
   for (int tile = tile0; tile < end; ++tile) {
-    f32x4 acc[16][4];   // first written by the K half 0 MFMAs of stage 0, with C = 0
+    f32x4 acc[16][RT];   // first written by the K half 0 MFMAs of stage 0, with C = 0
     LL_STAGE(LL_MFMA16_Z, 0)
     // (The loop's place in the 64-byte instruction lines, which a change anywhere before it would move.  In the projections of whole
     // stages without a bias, which most long calls run, its first MFMA is at byte 44: a pass of 8192 rows takes 0.7 % less there at d = 2560
@@ -529,7 +536,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   }
   if constexpr (SHORT) {
     if (ends_in_half) {
-      f32x4 acc[8][4];
+      f32x4 acc[8][RT];
       LL_HALF_STAGE(LL_MFMA16_Z, 0)
       for (int kt = 1; kt < KT; ++kt) {
         LL_HALF_STAGE(LL_MFMA16, kt)

@@ -38,20 +38,20 @@ __device__ __forceinline__ int64_t place_in_p(int v) {
 }
 
 enum { STATS, EXPS, GRAD };   // statistics only; and the exponentials; dz where the statistics are known
-template <int WHAT>
+template <int WHAT, int RT>
 struct LearnEpilogue {
-  struct State {   // of the lane's four rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
-    float m[4], s[4], t[4];
-    RowTerms terms[WHAT == GRAD ? 4 : 1];
+  struct State {   // of the lane's rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
+    float m[RT], s[RT], t[RT];
+    RowTerms terms[WHAT == GRAD ? RT : 1];
   };
   static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false;
-  static constexpr int ROWS = BN;
+  static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
   static __device__ __forceinline__ void init(State& st, const GemmArgs& args, int my_row, int) {
     const LearnArgs& p = static_cast<const LearnArgs&>(args);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < RT; ++j) {
       st.m[j] = NEG_BIG;
       st.s[j] = st.t[j] = 0.f;
       if (WHAT == GRAD) st.terms[j] = p.terms[min(row_of(my_row, j), p.rows - 1)];
@@ -81,7 +81,7 @@ struct LearnEpilogue {
       }
     };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
       float m = st.m[j], before = 0.f, keep = 1.f, s = 0.f, t = 0.f;
       if (WHAT != GRAD) {
@@ -138,18 +138,18 @@ struct LearnEpilogue {
   static __device__ __forceinline__ void store(const GemmArgs& p, const State& st, int my_row, int split) {
     if (WHAT == GRAD) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
       if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.m[j], st.s[j], st.t[j], 0.f);
     }
   }
 };
 
-template <int WHAT, bool TAIL>
+template <int WHAT, bool TAIL, int RT>
 __global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void ll_learn_logits_kernel(const LearnArgs p) {
   extern __shared__ __align__(16) unsigned char smem[];
-  lens_gemm_dma<LearnEpilogue<WHAT>, TAIL>(p, smem);
+  lens_gemm_dma<LearnEpilogue<WHAT, RT>, TAIL>(p, smem);
 }
 
 // Rows of a hidden size that is not a multiple of 64, zero padded to one.
@@ -160,31 +160,33 @@ __global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __res
         8 * c < d ? reinterpret_cast<const uint4*>(rows + row * d)[c] : make_uint4(0, 0, 0, 0);
 }
 
-// Logits of the listed tokens (before the temperature): one wavefront an entry; 0 for an id outside the vocabulary.
-__global__ __launch_bounds__(256) void ll_learn_list_logits_kernel(const uint16_t* __restrict__ rows, const uint16_t* __restrict__ W,
-                                                                   const int32_t* __restrict__ ids, int64_t entries, int k, int d, int V,
-                                                                   float* __restrict__ z) {
-  const int64_t e = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (e >= entries) return;
-  const int lane = threadIdx.x & 63, id = ids[e];
-  float s = 0.f;
-  if (id >= 0 && id < V) {
-    const uint4* a = reinterpret_cast<const uint4*>(rows + e / k * d);
-    const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)id * d);
-    float part[2] = {0.f, 0.f};
+// Logits of a row's listed tokens (before the temperature), a wavefront an entry at a time; 0 for an id outside the vocabulary.  The
+// whole workgroup comes here.  Bound by the gathered rows of W: 1500 x 20 of 16 KB in 95 us, 5.2 TB/s.
+__device__ __forceinline__ void list_logits(const uint16_t* __restrict__ row, const uint16_t* __restrict__ W, const int32_t* __restrict__ ids, int k,
+                                            int d, int V, float* z) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const uint4* a = reinterpret_cast<const uint4*>(row);
+  for (int i = threadIdx.x >> 6; i < k; i += waves) {
+    const int id = ids[i];
+    float s = 0.f;
+    if (id >= 0 && id < V) {
+      const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)id * d);
+      float part[2] = {0.f, 0.f};
 #pragma unroll 4
-    for (int c = lane; c < d / 8; c += 64) {
-      const uint4 x = a[c], y = w[c];
-      const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+      for (int c = lane; c < d / 8; c += 64) {
+        const uint4 x = a[c], y = w[c];
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        part[0] = fmaf(bf16_lo(xs[i]), bf16_lo(ys[i]), part[0]);
-        part[1] = fmaf(bf16_hi(xs[i]), bf16_hi(ys[i]), part[1]);
+        for (int q = 0; q < 4; ++q) {
+          part[0] = fmaf(bf16_lo(xs[q]), bf16_lo(ys[q]), part[0]);
+          part[1] = fmaf(bf16_hi(xs[q]), bf16_hi(ys[q]), part[1]);
+        }
       }
+      s = wave_sum(part[0] + part[1]);
     }
-    s = wave_sum(part[0] + part[1]);
+    if (lane == 0) z[i] = s;
   }
-  if (lane == 0) z[e] = s;
+  __syncthreads();
 }
 
 struct RowStats {
@@ -214,20 +216,34 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   return r;
 }
 
-// A row's statistics from its parts, and its listed tokens' log-probabilities: one wavefront a row, one lane an entry.
-__global__ __launch_bounds__(256) void ll_logp_finish_kernel(const float4* __restrict__ stats, int parts, const float* __restrict__ z,
-                                                             const int32_t* __restrict__ ids, int rows, int k, int V, float to_log2,
-                                                             float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ entropy) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= rows) return;
-  const RowStats r = join_stats(stats + (int64_t)row * parts, parts, lane);
+// A row a workgroup: what its listed tokens' logits are, then (the first wavefront, one lane an entry) what is made of them.
+struct ListArgs {
+  const uint16_t* rows;
+  const uint16_t* W;
+  const int32_t* ids;
+  int k, d, V;
+  float to_log2;
+  __device__ __forceinline__ void logits(float* z) const {
+    list_logits(rows + (int64_t)blockIdx.x * d, W, ids + (int64_t)blockIdx.x * k, k, d, V, z);
+  }
+};
+
+// A row's statistics from its parts, and its listed tokens' log-probabilities.
+__global__ __launch_bounds__(1024) void ll_logp_finish_kernel(const ListArgs p, const float4* __restrict__ stats, int parts,
+                                                              float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ entropy) {
+  __shared__ float z[LIST_MAX];
+  p.logits(z);
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x;
+  if (lane >= 64) return;
+  const RowStats r = join_stats(stats + row * parts, parts, lane);
   if (lane == 0) {
     lse[row] = r.lse2 * LN2;
     entropy[row] = -r.t * LN2;
   }
-  if (lane < k) {
-    const int64_t e = (int64_t)row * k + lane;
-    logp[e] = ids[e] >= 0 && ids[e] < V ? fmaf(z[e], to_log2, -r.lse2) * LN2 : NAN;
+  if (lane < p.k) {
+    const int64_t e = row * p.k + lane;
+    logp[e] = p.ids[e] >= 0 && p.ids[e] < p.V ? fmaf(z[lane], p.to_log2, -r.lse2) * LN2 : NAN;
   }
 }
 
@@ -248,27 +264,28 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
   return first;
 }
 
-// Teacher, loss, and what dz is made of: one wavefront a row, one lane an entry.  Of a row without a teacher (or of weight 0, as far as
-// the gradient goes) nothing that the row holds matters.
-__global__ __launch_bounds__(256) void ll_distill_rows_kernel(const float4* __restrict__ stats, int parts, const float* __restrict__ z,
-                                                              const int32_t* __restrict__ ids, const float* __restrict__ scores,
-                                                              const float* __restrict__ weight, int rows, int k, int V, float temperature,
-                                                              float to_log2, float* __restrict__ loss, RowTerms* __restrict__ terms,
-                                                              float2* __restrict__ list) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= rows) return;
+// Teacher, loss, and what dz is made of.  Of a row without a teacher (or of weight 0, as far as the gradient goes) nothing that the row
+// holds matters.
+__global__ __launch_bounds__(1024) void ll_distill_rows_kernel(const ListArgs p, const float4* __restrict__ stats, int parts,
+                                                               const float* __restrict__ scores, const float* __restrict__ weight,
+                                                               float temperature, float* __restrict__ loss, RowTerms* __restrict__ terms,
+                                                               float2* __restrict__ list) {
+  __shared__ float z[LIST_MAX];
+  p.logits(z);
+  const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
+  if (lane >= 64) return;
   const RowStats r = join_stats(stats + (int64_t)row * parts, parts, lane);
   const int64_t e = (int64_t)row * k + lane;
-  const int id = lane < k ? ids[e] : -1;
+  const int id = lane < k ? p.ids[e] : -1;
   const float score = lane < k ? scores[e] : -INFINITY;
-  const bool valid = id >= 0 && id < V && score != -INFINITY;
+  const bool valid = id >= 0 && id < p.V && score != -INFINITY;
   const bool some = __builtin_amdgcn_ballot_w64(valid) != 0;
   const float most = wave_max(valid ? score : -INFINITY);
   const float q = valid ? (score - most) / temperature : 0.f;
   const float share = valid ? expf(q) : 0.f;
   const float total = wave_sum(share);
   const float t = some ? share / total : 0.f;
-  const float l = fmaf(lane < k ? z[e] : 0.f, to_log2, -r.lse2);
+  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -r.lse2);
   const float term = valid && t != 0.f ? t * ((q - logf(total)) - l * LN2) : 0.f;
   const float sum = wave_sum(term);
   if (lane == 0) loss[row] = some ? temperature * temperature * sum : 0.f;
@@ -279,84 +296,118 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const float4* __re
   const bool first = gather_same(id, valid, k, lane, g);
   if (lane == 0) terms[row] = {r.lse2, a, 0.f, live ? 1.f : 0.f};
   if (lane < k) {
-    const float p = __builtin_amdgcn_exp2f(l);
-    list[e] = make_float2(a * (p - g), __int_as_float(live && first ? id : -1));
+    const float prob = __builtin_amdgcn_exp2f(l);
+    list[e] = make_float2(a * (prob - g), __int_as_float(live && first ? id : -1));
   }
 }
 
 // The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
-__global__ __launch_bounds__(256) void ll_logp_terms_kernel(const float* __restrict__ z, const int32_t* __restrict__ ids,
-                                                            const float* __restrict__ lse, const float* __restrict__ entropy,
-                                                            const float* __restrict__ g_logp, const float* __restrict__ g_entropy, int rows,
-                                                            int k, int V, float temperature, float to_log2, RowTerms* __restrict__ terms,
-                                                            float2* __restrict__ list) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= rows) return;
+__global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
+                                                             const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
+                                                             float temperature, RowTerms* __restrict__ terms, float2* __restrict__ list) {
+  __shared__ float z[LIST_MAX];
+  p.logits(z);
+  const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
+  if (lane >= 64) return;
   const int64_t e = (int64_t)row * k + lane;
-  const int id = lane < k ? ids[e] : -1;
-  const bool valid = id >= 0 && id < V;
+  const int id = lane < k ? p.ids[e] : -1;
+  const bool valid = id >= 0 && id < p.V;
   float g = valid ? g_logp[e] : 0.f;
   const float total = wave_sum(g), gh = g_entropy != nullptr ? g_entropy[row] : 0.f;
   const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || gh != 0.f;
   const float lse2 = lse[row] / LN2, inv_t = 1.f / temperature;
   const float a = -(total + (g_entropy != nullptr ? gh * entropy[row] : 0.f)) * inv_t, b = -gh * LN2 * inv_t;
-  const float l = fmaf(lane < k ? z[e] : 0.f, to_log2, -lse2);
+  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -lse2);
   const bool first = gather_same(id, valid, k, lane, g);
   if (lane == 0) terms[row] = {lse2, a, b, live ? 1.f : 0.f};
-  if (lane < k) {
-    const float p = __builtin_amdgcn_exp2f(l);
-    list[e] = make_float2(fmaf(g, inv_t, p * fmaf(b, l, a)), __int_as_float(live && first ? id : -1));
-  }
-}
-
-// e^(z - m) to dz = a e^(z - lse), in place, eight values a thread.  Rounded to bf16 a second time: the error of a dz is then
-// 2^-9 sqrt(2) of itself in the mean, what the product's bf16 operand has anyway.
-__global__ __launch_bounds__(256) void ll_distill_scale_kernel(uint16_t* __restrict__ P, int64_t ldp, const float* __restrict__ ref, int tiles,
-                                                               const RowTerms* __restrict__ terms) {
-  const int64_t row = blockIdx.y;
-  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (c >= ldp) return;
-  const RowTerms r = terms[row];
-  uint4* at = reinterpret_cast<uint4*>(P + row * ldp + c);
-  uint4 q = make_uint4(0, 0, 0, 0);
-  if (r.live != 0.f) {
-    q = *at;
-    const float by = r.a * __builtin_amdgcn_exp2f(ref[row * tiles + c / BM] - r.lse2);
-    q = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
-                   pack_bf16(bf16_lo(q.z) * by, bf16_hi(q.z) * by), pack_bf16(bf16_lo(q.w) * by, bf16_hi(q.w) * by));
-  }
-  *at = q;
+  if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(b, l, a)), __int_as_float(live && first ? id : -1));
 }
 
 // The listed tokens' dz, from their fp32 logits and rounded once.
+__device__ __forceinline__ void put_entry(uint16_t* __restrict__ row_of_p, const float2 entry) {
+  row_of_p[place_in_p(__float_as_int(entry.y))] = (uint16_t)pack_bf16(entry.x, 0.f);
+}
 __global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __restrict__ list, int64_t entries, int k, uint16_t* __restrict__ P,
                                                                 int64_t ldp) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= entries) return;
-  const float2 q = list[e];
-  const int id = __float_as_int(q.y);
-  if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(q.x, 0.f);
+  if (e < entries && __float_as_int(list[e].y) >= 0) put_entry(P + e / k * ldp, list[e]);
 }
 
-// dA = dz W over one slice of the vocabulary: the tile as it is.  A lane has four columns of a row in each 16.
+// e^(z - m) to dz = a e^(z - lse), in place: a workgroup has SCALE_COLS of a row, and puts its listed tokens behind.  Rounded to bf16 a
+// second time: the error of a dz is then sqrt(2) that of one rounding in the mean, what the product's bf16 operand has anyway.
+constexpr int SCALE_COLS = 8192;
+__global__ __launch_bounds__(256) void ll_distill_scale_kernel(uint16_t* __restrict__ P, int64_t ldp, const float* __restrict__ ref, int tiles,
+                                                               const RowTerms* __restrict__ terms, const float2* __restrict__ list, int k) {
+  const int64_t row = blockIdx.y;
+  const int first = blockIdx.x * SCALE_COLS;
+  uint16_t* const at = P + row * ldp;
+  const RowTerms r = terms[row];
+  uint4 q[SCALE_COLS / 2048];
+  float by[SCALE_COLS / 2048];
+#pragma unroll
+  for (int i = 0; i < SCALE_COLS / 2048; ++i) {
+    const int c = first + 2048 * i + 8 * (int)threadIdx.x;
+    q[i] = make_uint4(0, 0, 0, 0);
+    by[i] = 0.f;
+    if (c < ldp && r.live != 0.f) {
+      q[i] = *reinterpret_cast<const uint4*>(at + c);
+      by[i] = r.a * __builtin_amdgcn_exp2f(ref[row * tiles + c / BM] - r.lse2);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < SCALE_COLS / 2048; ++i) {
+    const int c = first + 2048 * i + 8 * (int)threadIdx.x;
+    if (c < ldp)
+      *reinterpret_cast<uint4*>(at + c) = make_uint4(
+          pack_bf16(bf16_lo(q[i].x) * by[i], bf16_hi(q[i].x) * by[i]), pack_bf16(bf16_lo(q[i].y) * by[i], bf16_hi(q[i].y) * by[i]),
+          pack_bf16(bf16_lo(q[i].z) * by[i], bf16_hi(q[i].z) * by[i]), pack_bf16(bf16_lo(q[i].w) * by[i], bf16_hi(q[i].w) * by[i]));
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < k) {
+    const float2 entry = list[row * k + threadIdx.x];
+    const int id = __float_as_int(entry.y);
+    if (id >= first && id < first + SCALE_COLS) put_entry(at, entry);
+  }
+}
+
+struct LearnBackArgs : BackArgs {
+  uint16_t* out;           // one slice: the gradient itself, [rows, d] bf16
+  const RowTerms* terms;
+};
+
+// dA = dz W over one slice of the vocabulary: the tile as it is, for ll_learn_join_kernel, or rounded where the slice is the whole.  A
+// lane has four columns of a row in each 16.
+template <int RT>
 struct BackEpilogue {
   struct State {
     int split;
   };
   static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = true;
-  static constexpr int ROWS = BN;
+  static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ void init(State& st, const GemmArgs&, int, int split) { st.split = split; }
   template <class ACC>
   static __device__ __forceinline__ void tile(const ACC& acc, State& st, int c0, const GemmArgs& args, int my_row) {
-    const BackArgs& p = static_cast<const BackArgs&>(args);
+    const LearnBackArgs& p = static_cast<const LearnBackArgs&>(args);
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA's result is in its registers
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < RT; ++j) {
       const int row = my_row - lane + 16 * j + (lane & 15);
       if (row >= p.rows) continue;
       const int c = c0 + 4 * (lane >> 4);
+      if (p.splits == 1) {
+        const bool live = p.terms[row].live != 0.f;
+        uint16_t* const to = p.out + (int64_t)row * p.d + c;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          if (c + 16 * t < p.d)
+            *reinterpret_cast<uint2*>(to + 16 * t) = live ? make_uint2(pack_bf16(acc_read(acc[t][j][0]), acc_read(acc[t][j][1])),
+                                                                       pack_bf16(acc_read(acc[t][j][2]), acc_read(acc[t][j][3])))
+                                                          : make_uint2(0, 0);
+        }
+        continue;
+      }
       float* const to = p.part + ((int64_t)st.split * p.rows + row) * p.d + c;
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
@@ -368,10 +419,11 @@ struct BackEpilogue {
   static __device__ __forceinline__ void store(const GemmArgs&, const State&, int, int) {}
 };
 
+template <int RT>
 __global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void ll_learn_back_kernel(const BackArgs p) {
+void ll_learn_back_kernel(const LearnBackArgs p) {
   extern __shared__ __align__(16) unsigned char smem[];
-  lens_gemm_dma<BackEpilogue, false>(p, smem);
+  lens_gemm_dma<BackEpilogue<RT>, false>(p, smem);
 }
 
 // The slices joined, in order; a row that takes no part gets zeros whatever W holds.
@@ -413,20 +465,48 @@ bool valid(const ll_shape* s, int k) {
 enum Needs { FORWARD, BACKWARD };
 
 struct LearnPlan {
-  int pass_rows, tiles, splits, row_blocks;
+  int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
-  size_t panel, z, stats, terms, list, ref, P, part, total;
+  size_t panel, stats, terms, list, ref, P, part, total;
 };
 
+// Tiles of 16 rows a wavefront (64 rows a workgroup each): the fewest that hold all rows, else what costs least.  A row block costs 0.47,
+// 0.6, 0.79 and 1 of one of 256 rows (1500 rows in 24, 12, 8 and 6: d = 4096, V = 128256, ll_logp 2057, 1320, 1168, 1098 us).  Whole
+// calls, us, with 1 | 2 | 3 | 4, ll_logp and ll_distill: d = 2560, V = 151936, 37 rows 161 | 181 | 202 | 228 and 325 | 344 | 367 | 400, 111 rows
+// 203 | 175 | 185 | 198 and 454 | 368 | 374 | 393, 192 rows 256 | 223 | 193 | 201 and 565 | 490 | 414 | 427, 348 rows 453 | 301 | 270 | 301 and
+// 967 | 682 | 586 | 661, 500 rows 567 | 406 | 355 | 313 and 1225 | 888 | 777 | 688; d = 1608, V = 50257, 777 rows 228 | 164 | 143 | 162 and 513 | 350
+// | 328 | 343; d = 8192, V = 128256, 37 rows 427 | 428 | 411 | 456 and 776 | 772 | 759 | 868, 777 rows 2204 | 1513 | 1446 | 1428 and 4545 |
+// 3247 | 2990 | 2900.
+constexpr double BLOCK_COST[4] = {0.47, 0.6, 0.79, 1.0};
+int row_tiles(int rows) {
+  if (rows <= BN) return (rows + 63) / 64;
+  int best = 4;
+  double least = 1e30;
+  for (int rt = 4; rt >= 1; --rt) {
+    const double c = (rows + 64 * rt - 1) / (64 * rt) * BLOCK_COST[rt - 1];
+    if (c < least) {
+      least = c;
+      best = rt;
+    }
+  }
+  return best;
+}
+
+template <class F>
+auto with_row_tiles(int rt, F f) {
+  using std::integral_constant;
+  return rt == 1 ? f(integral_constant<int, 1>{}) : rt == 2 ? f(integral_constant<int, 2>{}) : rt == 3 ? f(integral_constant<int, 3>{}) : f(integral_constant<int, 4>{});
+}
+
 // Slices of the vocabulary for the product backwards: one workgroup a compute unit at a time, so that `tiles` of it take whole rounds,
-// of a stage's 1.5 us each (and three to fill and empty the ring); a slice more is written and read, at some 4 TB/s.
-int slices(int64_t tiles, int stages, int rows, int d) {
+// of a stage's time each (and three to fill and empty the ring); a slice more is written and read, at some 4 TB/s, by a launch of some 5 us.
+int slices(int64_t tiles, int stages, int rows, int d, double stage_us) {
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= 64 && s <= stages; ++s) {
     const double rounds = (double)((tiles * s + NUM_CU - 1) / NUM_CU);
-    const double us = rounds * ((stages + s - 1) / s + 3) * 1.5 + s * (double)rows * d * 8 / 4e6;
+    const double us = rounds * ((stages + s - 1) / s + 3) * stage_us + (s > 1 ? s * (double)rows * d * 8 / 4e6 + 5 : 0);
     if (us < least) {
       least = us;
       best = s;
@@ -441,14 +521,16 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
   const int64_t passes = (N + PASS_ROWS - 1) / PASS_ROWS, each = (N + passes - 1) / passes;
   l.pass_rows = (int)(passes == 1 ? N : (each + BN - 1) / BN * BN);
   l.tiles = (s->V + BM - 1) / BM;
-  l.row_blocks = (l.pass_rows + BN - 1) / BN;
+  l.row_tiles = row_tiles(l.pass_rows);
+  l.block_rows = 64 * l.row_tiles;
+  l.row_blocks = (l.pass_rows + l.block_rows - 1) / l.block_rows;
   const int most = NUM_CU / l.row_blocks < l.tiles ? NUM_CU / l.row_blocks : l.tiles;
   const int per = (l.tiles + most - 1) / most;
   l.splits = (l.tiles + per - 1) / per;
   l.lda = (s->d + DK - 1) / DK * DK;
   l.ldp = (int64_t)l.tiles * BM;
   l.col_blocks = (s->d + BM - 1) / BM;
-  l.back_splits = slices(l.row_blocks * l.col_blocks, (s->V + DK - 1) / DK, l.pass_rows, s->d);
+  l.back_splits = slices(l.row_blocks * l.col_blocks, (s->V + DK - 1) / DK, l.pass_rows, s->d, l.row_blocks == 1 ? 1.5 : 1.5 * BLOCK_COST[l.row_tiles - 1]);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -456,7 +538,6 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     return at;
   };
   const size_t rows = (size_t)l.pass_rows;
-  l.z = take(rows * k * sizeof(float));
   l.stats = take(rows * l.splits * 4 * sizeof(float4));
   l.panel = take(l.lda != s->d ? rows * l.lda * 2 : 0);
   if (needs == BACKWARD) {
@@ -464,7 +545,7 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     l.list = take(rows * k * sizeof(float2));
     l.ref = take(rows * l.tiles * sizeof(float));
     l.P = take(rows * l.ldp * 2);
-    l.part = take(rows * l.back_splits * s->d * sizeof(float));
+    l.part = take(l.back_splits > 1 ? rows * l.back_splits * s->d * sizeof(float) : 0);
   }
   l.total = off;
   return l;
@@ -496,13 +577,8 @@ struct Pass {
   int n, k;
   hipStream_t stream;
 
-  int list_logits(const int32_t* ids) const {
-    const int64_t entries = (int64_t)n * k;
-    hipLaunchKernelGGL(ll_learn_list_logits_kernel, dim3((unsigned)((entries + 3) / 4)), dim3(256), 0, stream, rows, W, ids, entries, k, shape->d,
-                       shape->V, at<float>(ws, l.z));
-    LL_HIP_CHECK(hipGetLastError());
-    return LL_OK;
-  }
+  ListArgs list(const int32_t* ids) const { return {rows, W, ids, k, shape->d, shape->V, to_log2}; }
+  dim3 list_threads() const { return dim3(64 * (k < 16 ? k : 16)); }   // a wavefront an entry
 
   template <int WHAT>
   int logits() const {
@@ -521,7 +597,7 @@ struct Pass {
     p.V = shape->V;
     p.splits = l.splits;
     p.tiles = l.tiles;
-    p.row_blocks = (n + BN - 1) / BN;
+    p.row_blocks = (n + l.block_rows - 1) / l.block_rows;
     p.last_row = n - 1;
     p.group_rows = group_rows(p.row_blocks, p.splits);
     p.to_log2 = to_log2;
@@ -531,7 +607,9 @@ struct Pass {
       p.ref = at<float>(ws, l.ref);
       p.terms = at<RowTerms>(ws, l.terms);
     }
-    const auto kernel = l.lda != shape->d ? ll_learn_logits_kernel<WHAT, true> : ll_learn_logits_kernel<WHAT, false>;
+    const auto kernel = with_row_tiles(l.row_tiles, [&](auto rt) {
+      return l.lda != shape->d ? ll_learn_logits_kernel<WHAT, true, rt()> : ll_learn_logits_kernel<WHAT, false, rt()>;
+    });
     const size_t lds = (size_t)SLOTS * SLOT_BYTES;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
     const unsigned groups = (unsigned)((p.row_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
@@ -542,11 +620,7 @@ struct Pass {
 
   // P to the gradient of the rows
   int back(uint16_t* out) const {
-    const int64_t entries = (int64_t)n * k;
-    hipLaunchKernelGGL(ll_learn_put_list_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, at<float2>(ws, l.list), entries, k,
-                       at<uint16_t>(ws, l.P), l.ldp);
-    LL_HIP_CHECK(hipGetLastError());
-    BackArgs p = {};
+    LearnBackArgs p = {};
     p.A = at<uint16_t>(ws, l.P);
     p.W = W;
     p.part = at<float>(ws, l.part);
@@ -556,13 +630,17 @@ struct Pass {
     p.d = shape->d;
     p.V = shape->V;
     p.splits = l.back_splits;
-    p.row_blocks = (n + BN - 1) / BN;
+    p.row_blocks = (n + l.block_rows - 1) / l.block_rows;
     p.col_blocks = l.col_blocks;
+    p.out = out;
+    p.terms = at<RowTerms>(ws, l.terms);
     const size_t lds = (size_t)SLOTS * SLOT_BYTES;
-    if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(ll_learn_back_kernel), lds); rc != LL_OK) return rc;
+    const auto kernel = with_row_tiles(l.row_tiles, [](auto rt) { return ll_learn_back_kernel<rt()>; });
+    if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
     const unsigned groups = (unsigned)((p.row_blocks * p.col_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
-    hipLaunchKernelGGL(ll_learn_back_kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
+    if (p.splits == 1) return LL_OK;
     hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 2047) / 2048, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
                        at<RowTerms>(ws, l.terms), out);
     LL_HIP_CHECK(hipGetLastError());
@@ -598,10 +676,9 @@ int ll_logp(const ll_shape* shape, void* workspace, size_t workspace_bytes, cons
   const LearnPlan l = plan_for(shape, k, FORWARD);
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
-    LL_TRY(p.list_logits(ids + r0 * k));
     LL_TRY(p.logits<STATS>());
-    hipLaunchKernelGGL(ll_logp_finish_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float4>(workspace, l.stats), 4 * l.splits,
-                       at<float>(workspace, l.z), ids + r0 * k, p.n, k, shape->V, p.to_log2, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
+    hipLaunchKernelGGL(ll_logp_finish_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), at<float4>(workspace, l.stats),
+                       4 * l.splits, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   });
@@ -619,12 +696,15 @@ int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes,
   const LearnPlan l = plan_for(shape, k, BACKWARD);
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
-    LL_TRY(p.list_logits(ids + r0 * k));
-    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float>(workspace, l.z), ids + r0 * k, lse + r0,
-                       entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, p.n, k,
-                       shape->V, temperature, p.to_log2, at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list));
+    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), lse + r0,
+                       entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, temperature,
+                       at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list));
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(p.logits<GRAD>());
+    const int64_t entries = (int64_t)p.n * k;
+    hipLaunchKernelGGL(ll_learn_put_list_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, p.stream, at<float2>(workspace, l.list),
+                       entries, k, at<uint16_t>(workspace, l.P), l.ldp);
+    LL_HIP_CHECK(hipGetLastError());
     return p.back((uint16_t*)out_grad + r0 * shape->d);
   });
 }
@@ -641,16 +721,16 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, teacher_ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
     const bool grad = out_grad != nullptr;
-    LL_TRY(p.list_logits(teacher_ids + r0 * k));
     LL_TRY(grad ? p.logits<EXPS>() : p.logits<STATS>());
-    hipLaunchKernelGGL(ll_distill_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, p.stream, at<float4>(workspace, l.stats), 4 * l.splits,
-                       at<float>(workspace, l.z), teacher_ids + r0 * k, teacher_scores + r0 * k, weight != nullptr ? weight + r0 : nullptr, p.n, k,
-                       shape->V, temperature, p.to_log2, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
+    hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(teacher_ids + r0 * k),
+                       at<float4>(workspace, l.stats), 4 * l.splits, teacher_scores + r0 * k, weight != nullptr ? weight + r0 : nullptr,
+                       temperature, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
                        grad ? at<float2>(workspace, l.list) : nullptr);
     LL_HIP_CHECK(hipGetLastError());
     if (!grad) return LL_OK;
-    hipLaunchKernelGGL(ll_distill_scale_kernel, dim3((unsigned)((l.ldp + 2047) / 2048), p.n), dim3(256), 0, p.stream,
-                       at<uint16_t>(workspace, l.P), l.ldp, at<float>(workspace, l.ref), l.tiles, at<RowTerms>(workspace, l.terms));
+    hipLaunchKernelGGL(ll_distill_scale_kernel, dim3((unsigned)((l.ldp + SCALE_COLS - 1) / SCALE_COLS), p.n), dim3(256), 0, p.stream,
+                       at<uint16_t>(workspace, l.P), l.ldp, at<float>(workspace, l.ref), l.tiles, at<RowTerms>(workspace, l.terms),
+                       at<float2>(workspace, l.list), k);
     LL_HIP_CHECK(hipGetLastError());
     return p.back((uint16_t*)out_grad + r0 * shape->d);
   });
