@@ -5,9 +5,8 @@
 //
 // Forward, the logits stay in MFMA accumulators as in ll_project: the direct-to-LDS kernel (ll_gemm_lds.h) with an epilogue of its
 // own.  A gradient needs every logit a second time, as the left factor of a product over the vocabulary.  Forming them again would be a
-// third product; instead the first one's epilogue leaves e^(z - m), m the row's running maximum, as bf16 behind it (2 bytes a logit,
-// beside 4 d flops), whose relative error is that of any bf16 number however small it is, and the second product reads it with the
-// row's normaliser applied.
+// third product; instead the first one's epilogue leaves P, e^z relative to a reference, as bf16 behind it (2 bytes a logit, beside 4 d
+// flops), whose relative error is that of any bf16 number however small it is, and the second product reads that.
 #include "ll_epilogue.h"
 #include "ll_gemm_lds.h"
 
@@ -19,13 +18,14 @@ constexpr int LIST_MAX = LL_LIST_MAX;      // one lane of a wavefront each
 constexpr int PASS_ROWS = 2048;            // rows of a pass: what the workspace holds of e^(z - m) or dz, 0.6 GB at V = 152 000
 constexpr float LN2 = 0.6931471805599453f;
 
-struct RowTerms {   // of a row's dz: with l = (z log2 e - lse2), dz = 2^l (a + b l)
-  float lse2, a, b, live;
+struct RowTerms {   // of a row's dz: with l = z log2 e - lse2, dz = 2^l (a + b l); its gradient is `factor` times P's product, zeros where that is 0
+  float lse2, a, b, factor;
 };
 
 struct LearnArgs : GemmArgs {
   uint16_t* P;          // [rows, ldp] bf16
-  float* ref;           // [rows, tiles]: what the exponents of a tile are relative to, in powers of two
+  float* moved;         // [rows, tiles]: what the exponents of a tile are relative to, in powers of two
+  const float* ref;     // [rows]: what they start from
   const RowTerms* terms;   // [rows]
   int64_t ldp;
   float to_log2;        // log2(e) / T
@@ -37,24 +37,35 @@ __device__ __forceinline__ int64_t place_in_p(int v) {
   return (v & ~31) + 8 * ((v >> 2) & 3) + 4 * ((v >> 4) & 1) + (v & 3);
 }
 
-enum { STATS, EXPS, GRAD };   // statistics only; and the exponentials; dz where the statistics are known
+// STATS: statistics only; EXPS: and the exponentials; GRAD: dz where the statistics are known.
+//
+// Exponents are relative to a reference that is no maximum: with fp32's range a sum of 2^(x - ref) does as well for any ref that is
+// not far from it, and so does bf16 for the exponentials, so that a tile takes one look at its accumulators and not two.  The reference
+// moves, to the tile's maximum, where the lane's sum over a tile leaves `MOST` behind (or has overflowed), and the tile is taken again.
+// STATS starts from below everything, so that the first tile sets it, and moves it early, for the sake of T, whose terms are 2^l l.
+// EXPS starts from the largest listed logit, one for all splits of a row, and so near the row's maximum that hardly any row ever moves:
+// then all of P's row is relative to one number, which the product backwards need not know (see ll_distill_rows_kernel).
+enum { STATS, EXPS, GRAD };
+constexpr float MASKED = -1e30f;   // an exponent that stands for a column past the vocabulary: 2^l is 0, and l no infinity for what multiplies it
 template <int WHAT, int RT>
 struct LearnEpilogue {
   struct State {   // of the lane's rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
-    float m[RT], s[RT], t[RT];
+    float ref[RT], s[RT], t[RT];
     RowTerms terms[WHAT == GRAD ? RT : 1];
   };
   static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false;
   static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
+  static constexpr float MOST = WHAT == EXPS ? 0x1p60f : 0x1p16f;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
   static __device__ __forceinline__ void init(State& st, const GemmArgs& args, int my_row, int) {
     const LearnArgs& p = static_cast<const LearnArgs&>(args);
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
-      st.m[j] = NEG_BIG;
+      const int row = min(row_of(my_row, j), p.rows - 1);
+      st.ref[j] = WHAT == EXPS ? p.ref[row] : NEG_BIG;
       st.s[j] = st.t[j] = 0.f;
-      if (WHAT == GRAD) st.terms[j] = p.terms[min(row_of(my_row, j), p.rows - 1)];
+      if (WHAT == GRAD) st.terms[j] = p.terms[row];
     }
   }
   template <class ACC>
@@ -64,83 +75,77 @@ struct LearnEpilogue {
     if (v0 + BM <= p.V) rows_of_tile<true>(acc, st, v0, p, my_row);
     else rows_of_tile<false>(acc, st, v0, p, my_row);
   }
-  // WHOLE: all of the tile's columns are in the vocabulary.
+  // Whether column q of the lane's eight of columns 32 u .. is in the vocabulary.
+  static __device__ __forceinline__ bool inside(int u, int q, int last) { return 16 * (2 * u + (q >> 2)) + (q & 3) <= last; }
+  // One row tile, eight values at a time: what they add to the sums, and what goes to P.  WHOLE: all columns are in the vocabulary.
+  template <bool WHOLE, class ACC>
+  static __device__ __forceinline__ float2 sums_of_tile(const ACC& acc, const State& st, int j, int last, float c, uint4* to, bool present) {
+    float s = 0.f, t = 0.f;
+    const float ref = WHAT == GRAD ? st.terms[j].lse2 : st.ref[j];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      float x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        float l = fmaf(acc_read(acc[2 * u + (q >> 2)][j][q & 3]), c, -ref);
+        if (!WHOLE) l = inside(u, q, last) ? l : MASKED;
+        x[q] = __builtin_amdgcn_exp2f(l);
+        if (WHAT == GRAD) x[q] *= fmaf(st.terms[j].b, l, st.terms[j].a);
+        else s += x[q];
+        if (WHAT == STATS) t = fmaf(x[q], l, t);
+      }
+      if (WHAT != STATS && present)
+        to[4 * u] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+      LL_SCHED_FENCE();
+    }
+    return make_float2(s, t);
+  }
   template <bool WHOLE, class ACC>
   static __device__ __forceinline__ void rows_of_tile(const ACC& acc, State& st, int v0, const LearnArgs& p, int my_row) {
     const int g = (threadIdx.x & 63) >> 4;
     const float c = p.to_log2;
     const int last = p.V - 1 - v0 - 4 * g;   // of the lane's 16 t + i, the last in the vocabulary
-    // Eight values of a row at a time, read from the accumulators as they are needed (twice where the maximum comes first): the
-    // fragments of the next stage hold most of the other registers.
-    const auto eight = [&](int j, int u, float (&x)[8]) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] = acc_read(acc[2 * u + (q >> 2)][j][q & 3]) * c;
-      if (!WHOLE) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) x[q] = 16 * (2 * u + (q >> 2)) + (q & 3) > last ? -INFINITY : x[q];
-      }
-    };
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
-      float m = st.m[j], before = 0.f, keep = 1.f, s = 0.f, t = 0.f;
-      if (WHAT != GRAD) {
+      const bool present = row < p.rows;
+      uint4* const to = reinterpret_cast<uint4*>(p.P + row * p.ldp + v0 + 8 * g);
+      float2 add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
+      if (WHAT == GRAD) continue;
+      if (__builtin_amdgcn_ballot_w64(add.x > MOST) != 0) {
+        float m = NEG_BIG;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          float x[8];
-          eight(j, u, x);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) m = fmaxf(m, x[q]);
+          for (int q = 0; q < 8; ++q) {
+            const float z = acc_read(acc[2 * u + (q >> 2)][j][q & 3]);
+            m = WHOLE || inside(u, q, last) ? fmaxf(m, z) : m;
+          }
           LL_SCHED_FENCE();
         }
-        if (WHAT == EXPS) {   // the four lanes of a row: one reference
-          const auto most = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
-          m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most));
-        }
-        before = st.m[j] - m;
-        keep = __builtin_amdgcn_exp2f(before);
+        const auto most = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
+        const auto any = [](uint32_t a, uint32_t b) { return a | b; };
+        // the four lanes of a row together
+        m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most)) * c;
+        const bool move = with_lane_xor<32>(with_lane_xor<16>(add.x > MOST ? 1u : 0u, any), any) != 0;
+        const float to_ref = move ? fmaxf(m, st.ref[j]) : st.ref[j], before = st.ref[j] - to_ref, keep = __builtin_amdgcn_exp2f(before);
+        st.t[j] = keep * fmaf(before, st.s[j], st.t[j]);
+        st.s[j] *= keep;
+        st.ref[j] = to_ref;
+        add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
       }
-      if (WHAT != STATS && row >= p.rows) continue;
-      uint4* const to = reinterpret_cast<uint4*>(p.P + row * p.ldp + v0 + 8 * g);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        float x[8];
-        eight(j, u, x);
-        if (WHAT == GRAD) {
-          const RowTerms r = st.terms[j];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const float l = x[q] - r.lse2, e = __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a);
-            x[q] = l == -INFINITY || r.live == 0.f ? 0.f : e;
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const float l = x[q] - m;
-            x[q] = __builtin_amdgcn_exp2f(l);
-            s += x[q];
-            if (WHAT == STATS) t += l == -INFINITY ? 0.f : x[q] * l;   // (l is relative to the maximum: nothing large to take away again)
-          }
-        }
-        if (WHAT != STATS)
-          to[4 * u] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        LL_SCHED_FENCE();
-      }
-      if (WHAT != GRAD) {
-        if (WHAT == STATS) st.t[j] = st.s[j] > 0.f ? fmaf(keep, fmaf(before, st.s[j], st.t[j]), t) : t;
-        st.s[j] = fmaf(keep, st.s[j], s);
-        st.m[j] = m;
-        if (WHAT == EXPS && g == 0) p.ref[(int64_t)row * p.tiles + v0 / BM] = m;
-      }
+      st.s[j] += add.x;
+      st.t[j] += add.y;
+      if (WHAT == EXPS && g == 0 && present) p.moved[(int64_t)row * p.tiles + v0 / BM] = st.ref[j];
     }
   }
-  // Every lane its own (m, S, T): four to a row and split.
+  // Every lane its own (ref, S, T): four to a row and split.
   static __device__ __forceinline__ void store(const GemmArgs& p, const State& st, int my_row, int split) {
     if (WHAT == GRAD) return;
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
-      if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.m[j], st.s[j], st.t[j], 0.f);
+      if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.ref[j], st.s[j], st.t[j], 0.f);
     }
   }
 };
@@ -197,7 +202,7 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   float m = NEG_BIG;
   bool nan = false;
   for (int i = lane; i < parts; i += 64) {
-    m = fmaxf(m, stats[i].x);
+    m = fmaxf(m, stats[i].y > 0.f ? stats[i].x : NEG_BIG);
     nan |= stats[i].y != stats[i].y;
   }
   m = wave_max(m);
@@ -205,7 +210,7 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   for (int i = lane; i < parts; i += 64) {
     const float4 q = stats[i];
     const float by = q.x - m, e = __builtin_amdgcn_exp2f(by);
-    s = fmaf(e, q.y, s);
+    s += q.y > 0.f ? e * q.y : 0.f;
     t += q.y > 0.f ? e * fmaf(by, q.y, q.z) : 0.f;
   }
   s = wave_sum(s);
@@ -264,41 +269,87 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
   return first;
 }
 
-// Teacher, loss, and what dz is made of.  Of a row without a teacher (or of weight 0, as far as the gradient goes) nothing that the row
-// holds matters.
-__global__ __launch_bounds__(1024) void ll_distill_rows_kernel(const ListArgs p, const float4* __restrict__ stats, int parts,
-                                                               const float* __restrict__ scores, const float* __restrict__ weight,
-                                                               float temperature, float* __restrict__ loss, RowTerms* __restrict__ terms,
-                                                               float2* __restrict__ list) {
+// Before the first product: the listed tokens' logits, and the largest in powers of two (of a row without any: 0).
+__global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref) {
   __shared__ float z[LIST_MAX];
   p.logits(z);
-  const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
+  const int lane = threadIdx.x;
   if (lane >= 64) return;
-  const RowStats r = join_stats(stats + (int64_t)row * parts, parts, lane);
-  const int64_t e = (int64_t)row * k + lane;
-  const int id = lane < k ? p.ids[e] : -1;
-  const float score = lane < k ? scores[e] : -INFINITY;
-  const bool valid = id >= 0 && id < p.V && score != -INFINITY;
-  const bool some = __builtin_amdgcn_ballot_w64(valid) != 0;
-  const float most = wave_max(valid ? score : -INFINITY);
-  const float q = valid ? (score - most) / temperature : 0.f;
-  const float share = valid ? expf(q) : 0.f;
-  const float total = wave_sum(share);
-  const float t = some ? share / total : 0.f;
-  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -r.lse2);
-  const float term = valid && t != 0.f ? t * ((q - logf(total)) - l * LN2) : 0.f;
-  const float sum = wave_sum(term);
-  if (lane == 0) loss[row] = some ? temperature * temperature * sum : 0.f;
-  if (terms == nullptr) return;
-  const float a = temperature * (weight != nullptr ? weight[row] : 1.f);
-  const bool live = some && a != 0.f;
-  float g = t;
-  const bool first = gather_same(id, valid, k, lane, g);
-  if (lane == 0) terms[row] = {r.lse2, a, 0.f, live ? 1.f : 0.f};
-  if (lane < k) {
-    const float prob = __builtin_amdgcn_exp2f(l);
-    list[e] = make_float2(a * (prob - g), __int_as_float(live && first ? id : -1));
+  const int64_t row = blockIdx.x, e = row * p.k + lane;
+  float most = NEG_BIG;
+  if (lane < p.k) {
+    z_out[e] = z[lane];
+    if (p.ids[e] >= 0 && p.ids[e] < p.V) most = z[lane] * p.to_log2;
   }
+  most = wave_max(most);
+  if (lane == 0) ref[row] = fabsf(most) < 1e30f ? most : 0.f;
+}
+
+// Teacher, loss, and what the gradient is made of: a row a workgroup, the first wavefront one lane an entry.  With P = 2^(x - base) over the
+// whole row, dz = a (p - t) is a 2^(base - lse2) (P - t 2^(lse2 - base)): the listed tokens' entries are put into P, from their fp32 logits
+// and rounded once, and the rest is the row's factor of the gradient.  A row whose reference has moved in some tile first has its tiles
+// brought to one base, lse2, here.  Of a row without a teacher (or of weight 0, as far as the gradient goes) nothing that the row holds
+// matters.
+__global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __restrict__ ids, const float* __restrict__ z, int k, int V,
+                                                              float to_log2, const float4* __restrict__ stats, int parts,
+                                                              const float* __restrict__ scores, const float* __restrict__ weight,
+                                                              float temperature, float* __restrict__ loss, RowTerms* __restrict__ terms,
+                                                              const float* __restrict__ ref, const float* __restrict__ moved, int tiles,
+                                                              uint16_t* __restrict__ P, int64_t ldp) {
+  __shared__ float shared_lse2;
+  __shared__ int shared_moved;
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  const bool first_wave = threadIdx.x < 64;
+  int id = -1;
+  bool first = false, live = false;
+  float l = 0.f, t = 0.f;
+  if (first_wave) {
+    const RowStats r = join_stats(stats + row * parts, parts, lane);
+    const int64_t e = row * k + lane;
+    id = lane < k ? ids[e] : -1;
+    const float score = lane < k ? scores[e] : -INFINITY;
+    const bool valid = id >= 0 && id < V && score != -INFINITY;
+    const bool some = __builtin_amdgcn_ballot_w64(valid) != 0;
+    const float most = wave_max(valid ? score : -INFINITY);
+    const float q = valid ? (score - most) / temperature : 0.f;
+    const float share = valid ? expf(q) : 0.f;
+    const float total = wave_sum(share);
+    t = some ? share / total : 0.f;
+    l = fmaf(lane < k ? z[e] : 0.f, to_log2, -r.lse2);
+    const float term = valid && t != 0.f ? t * ((q - logf(total)) - l * LN2) : 0.f;
+    const float sum = wave_sum(term);
+    if (lane == 0) loss[row] = some ? temperature * temperature * sum : 0.f;
+    if (terms != nullptr) {
+      const float a = temperature * (weight != nullptr ? weight[row] : 1.f);
+      live = some && a != 0.f;
+      first = gather_same(id, valid, k, lane, t);
+      bool other = false;
+      for (int i = lane; i < parts; i += 64) other |= stats[row * parts + i].x != ref[row];
+      other = __builtin_amdgcn_ballot_w64(other) != 0;
+      const float base = other ? r.lse2 : ref[row];
+      if (lane == 0) {
+        terms[row] = {r.lse2, 0.f, 0.f, live ? a * __builtin_amdgcn_exp2f(base - r.lse2) : 0.f};
+        shared_moved = live && other;
+        shared_lse2 = r.lse2;
+      }
+      t *= __builtin_amdgcn_exp2f(r.lse2 - base);
+      l += r.lse2 - base;
+    }
+  }
+  if (terms == nullptr) return;
+  __syncthreads();
+  uint16_t* const at = P + row * ldp;
+  if (shared_moved) {
+    for (int64_t c = 8 * (int)threadIdx.x; c < ldp; c += 8 * 256) {
+      const uint4 q = *reinterpret_cast<const uint4*>(at + c);
+      const float by = __builtin_amdgcn_exp2f(moved[row * tiles + c / BM] - shared_lse2);
+      *reinterpret_cast<uint4*>(at + c) = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
+                                                     pack_bf16(bf16_lo(q.z) * by, bf16_hi(q.z) * by), pack_bf16(bf16_lo(q.w) * by, bf16_hi(q.w) * by));
+    }
+    __syncthreads();
+  }
+  if (first_wave && live && first) at[place_in_p(id)] = (uint16_t)pack_bf16(__builtin_amdgcn_exp2f(l) - t, 0.f);
 }
 
 // The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
@@ -323,51 +374,14 @@ __global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, c
   if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(b, l, a)), __int_as_float(live && first ? id : -1));
 }
 
-// The listed tokens' dz, from their fp32 logits and rounded once.
-__device__ __forceinline__ void put_entry(uint16_t* __restrict__ row_of_p, const float2 entry) {
-  row_of_p[place_in_p(__float_as_int(entry.y))] = (uint16_t)pack_bf16(entry.x, 0.f);
-}
+// ll_logp_grad: the listed tokens' dz, from their fp32 logits and rounded once.
 __global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __restrict__ list, int64_t entries, int k, uint16_t* __restrict__ P,
                                                                 int64_t ldp) {
   const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e < entries && __float_as_int(list[e].y) >= 0) put_entry(P + e / k * ldp, list[e]);
-}
-
-// e^(z - m) to dz = a e^(z - lse), in place: a workgroup has SCALE_COLS of a row, and puts its listed tokens behind.  Rounded to bf16 a
-// second time: the error of a dz is then sqrt(2) that of one rounding in the mean, what the product's bf16 operand has anyway.
-constexpr int SCALE_COLS = 8192;
-__global__ __launch_bounds__(256) void ll_distill_scale_kernel(uint16_t* __restrict__ P, int64_t ldp, const float* __restrict__ ref, int tiles,
-                                                               const RowTerms* __restrict__ terms, const float2* __restrict__ list, int k) {
-  const int64_t row = blockIdx.y;
-  const int first = blockIdx.x * SCALE_COLS;
-  uint16_t* const at = P + row * ldp;
-  const RowTerms r = terms[row];
-  uint4 q[SCALE_COLS / 2048];
-  float by[SCALE_COLS / 2048];
-#pragma unroll
-  for (int i = 0; i < SCALE_COLS / 2048; ++i) {
-    const int c = first + 2048 * i + 8 * (int)threadIdx.x;
-    q[i] = make_uint4(0, 0, 0, 0);
-    by[i] = 0.f;
-    if (c < ldp && r.live != 0.f) {
-      q[i] = *reinterpret_cast<const uint4*>(at + c);
-      by[i] = r.a * __builtin_amdgcn_exp2f(ref[row * tiles + c / BM] - r.lse2);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < SCALE_COLS / 2048; ++i) {
-    const int c = first + 2048 * i + 8 * (int)threadIdx.x;
-    if (c < ldp)
-      *reinterpret_cast<uint4*>(at + c) = make_uint4(
-          pack_bf16(bf16_lo(q[i].x) * by[i], bf16_hi(q[i].x) * by[i]), pack_bf16(bf16_lo(q[i].y) * by[i], bf16_hi(q[i].y) * by[i]),
-          pack_bf16(bf16_lo(q[i].z) * by[i], bf16_hi(q[i].z) * by[i]), pack_bf16(bf16_lo(q[i].w) * by[i], bf16_hi(q[i].w) * by[i]));
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < k) {
-    const float2 entry = list[row * k + threadIdx.x];
-    const int id = __float_as_int(entry.y);
-    if (id >= first && id < first + SCALE_COLS) put_entry(at, entry);
-  }
+  if (e >= entries) return;
+  const float2 entry = list[e];
+  const int id = __float_as_int(entry.y);
+  if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(entry.x, 0.f);
 }
 
 struct LearnBackArgs : BackArgs {
@@ -397,14 +411,14 @@ struct BackEpilogue {
       if (row >= p.rows) continue;
       const int c = c0 + 4 * (lane >> 4);
       if (p.splits == 1) {
-        const bool live = p.terms[row].live != 0.f;
+        const float f = p.terms[row].factor;
         uint16_t* const to = p.out + (int64_t)row * p.d + c;
 #pragma unroll
         for (int t = 0; t < 16; ++t) {
           if (c + 16 * t < p.d)
-            *reinterpret_cast<uint2*>(to + 16 * t) = live ? make_uint2(pack_bf16(acc_read(acc[t][j][0]), acc_read(acc[t][j][1])),
-                                                                       pack_bf16(acc_read(acc[t][j][2]), acc_read(acc[t][j][3])))
-                                                          : make_uint2(0, 0);
+            *reinterpret_cast<uint2*>(to + 16 * t) = f != 0.f ? make_uint2(pack_bf16(f * acc_read(acc[t][j][0]), f * acc_read(acc[t][j][1])),
+                                                                           pack_bf16(f * acc_read(acc[t][j][2]), f * acc_read(acc[t][j][3])))
+                                                              : make_uint2(0, 0);
         }
         continue;
       }
@@ -426,30 +440,26 @@ void ll_learn_back_kernel(const LearnBackArgs p) {
   lens_gemm_dma<BackEpilogue<RT>, false>(p, smem);
 }
 
-// The slices joined, in order; a row that takes no part gets zeros whatever W holds.
+// The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)
 __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, int d,
                                                             const RowTerms* __restrict__ terms, uint16_t* __restrict__ out) {
   const int64_t row = blockIdx.y;
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= d) return;
-  float s[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i] = 0.f;
-  if (terms[row].live != 0.f)
+  const float f = terms[row].factor;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (f != 0.f) {
+#pragma unroll 8
     for (int q = 0; q < splits; ++q) {
-      const float4* from = reinterpret_cast<const float4*>(part + ((int64_t)q * rows + row) * d + c);
-      const float4 lo = from[0], hi = from[1];
-      s[0] += lo.x;
-      s[1] += lo.y;
-      s[2] += lo.z;
-      s[3] += lo.w;
-      s[4] += hi.x;
-      s[5] += hi.y;
-      s[6] += hi.z;
-      s[7] += hi.w;
+      const float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)q * rows + row) * d + c);
+      s.x += x.x;
+      s.y += x.y;
+      s.z += x.z;
+      s.w += x.w;
     }
-  *reinterpret_cast<uint4*>(out + row * d + c) =
-      make_uint4(pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3]), pack_bf16(s[4], s[5]), pack_bf16(s[6], s[7]));
+    s = make_float4(f * s.x, f * s.y, f * s.z, f * s.w);
+  }
+  *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
 // ---------------------------------------------------------------------------------------
@@ -468,7 +478,7 @@ struct LearnPlan {
   int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
-  size_t panel, stats, terms, list, ref, P, part, total;
+  size_t stats, z, ref, panel, terms, list, moved, P, part, total;
 };
 
 // Tiles of 16 rows a wavefront (64 rows a workgroup each): the fewest that hold all rows, else what costs least.  A row block costs 0.47,
@@ -539,11 +549,13 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
   };
   const size_t rows = (size_t)l.pass_rows;
   l.stats = take(rows * l.splits * 4 * sizeof(float4));
+  l.z = take(rows * k * sizeof(float));
+  l.ref = take(rows * sizeof(float));
   l.panel = take(l.lda != s->d ? rows * l.lda * 2 : 0);
   if (needs == BACKWARD) {
     l.terms = take(rows * sizeof(RowTerms));
     l.list = take(rows * k * sizeof(float2));
-    l.ref = take(rows * l.tiles * sizeof(float));
+    l.moved = take(rows * l.tiles * sizeof(float));
     l.P = take(rows * l.ldp * 2);
     l.part = take(l.back_splits > 1 ? rows * l.back_splits * s->d * sizeof(float) : 0);
   }
@@ -604,6 +616,7 @@ struct Pass {
     if (WHAT != STATS) {
       p.P = at<uint16_t>(ws, l.P);
       p.ldp = l.ldp;
+      p.moved = at<float>(ws, l.moved);
       p.ref = at<float>(ws, l.ref);
       p.terms = at<RowTerms>(ws, l.terms);
     }
@@ -641,7 +654,7 @@ struct Pass {
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
     if (p.splits == 1) return LL_OK;
-    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 2047) / 2048, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
+    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 1023) / 1024, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
                        at<RowTerms>(ws, l.terms), out);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
@@ -721,17 +734,17 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, teacher_ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
     const bool grad = out_grad != nullptr;
+    hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(teacher_ids + r0 * k), at<float>(workspace, l.z),
+                       at<float>(workspace, l.ref));
+    LL_HIP_CHECK(hipGetLastError());
     LL_TRY(grad ? p.logits<EXPS>() : p.logits<STATS>());
-    hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(teacher_ids + r0 * k),
-                       at<float4>(workspace, l.stats), 4 * l.splits, teacher_scores + r0 * k, weight != nullptr ? weight + r0 : nullptr,
-                       temperature, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
-                       grad ? at<float2>(workspace, l.list) : nullptr);
+    hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), dim3(grad ? 256 : 64), 0, p.stream, teacher_ids + r0 * k, at<float>(workspace, l.z), k,
+                       shape->V, p.to_log2, at<float4>(workspace, l.stats), 4 * l.splits, teacher_scores + r0 * k,
+                       weight != nullptr ? weight + r0 : nullptr, temperature, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
+                       at<float>(workspace, l.ref), grad ? at<float>(workspace, l.moved) : nullptr, l.tiles,
+                       grad ? at<uint16_t>(workspace, l.P) : nullptr, l.ldp);
     LL_HIP_CHECK(hipGetLastError());
     if (!grad) return LL_OK;
-    hipLaunchKernelGGL(ll_distill_scale_kernel, dim3((unsigned)((l.ldp + SCALE_COLS - 1) / SCALE_COLS), p.n), dim3(256), 0, p.stream,
-                       at<uint16_t>(workspace, l.P), l.ldp, at<float>(workspace, l.ref), l.tiles, at<RowTerms>(workspace, l.terms),
-                       at<float2>(workspace, l.list), k);
-    LL_HIP_CHECK(hipGetLastError());
     return p.back((uint16_t*)out_grad + r0 * shape->d);
   });
 }
