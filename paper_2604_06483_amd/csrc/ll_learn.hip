@@ -197,18 +197,19 @@ __device__ __forceinline__ void list_logits(const uint16_t* __restrict__ row, co
 struct RowStats {
   float lse2, t;   // log2 of the sum of 2^x; sum of p (x - lse2), x = z log2 e: minus the entropy, in powers of two
 };
-// A row's parts joined, by a wavefront.
-__device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats, int parts, int lane) {
+// A row's parts, `stride` apart, joined by a wavefront.
+__device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats, int parts, int lane, int stride = 1) {
   float m = NEG_BIG;
   bool nan = false;
   for (int i = lane; i < parts; i += 64) {
-    m = fmaxf(m, stats[i].y > 0.f ? stats[i].x : NEG_BIG);
-    nan |= stats[i].y != stats[i].y;
+    const float4 q = stats[(int64_t)i * stride];
+    m = fmaxf(m, q.y > 0.f ? q.x : NEG_BIG);
+    nan |= q.y != q.y;
   }
   m = wave_max(m);
   float s = 0.f, t = 0.f;
   for (int i = lane; i < parts; i += 64) {
-    const float4 q = stats[i];
+    const float4 q = stats[(int64_t)i * stride];
     const float by = q.x - m, e = __builtin_amdgcn_exp2f(by);
     s += q.y > 0.f ? e * q.y : 0.f;
     t += q.y > 0.f ? e * fmaf(by, q.y, q.z) : 0.f;
@@ -285,13 +286,36 @@ __global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p
   if (lane == 0) ref[row] = fabsf(most) < 1e30f ? most : 0.f;
 }
 
+// A row's teacher, by a wavefront, one lane an entry: t = softmax of the scores / temperature over the entries that there are.
+struct Teacher {
+  bool valid, some;     // the lane's entry is one; the row has one
+  float t, log_t;
+};
+__device__ __forceinline__ Teacher teacher_of(int id, float score, int V, float temperature) {
+  Teacher r;
+  r.valid = id >= 0 && id < V && score != -INFINITY;
+  r.some = __builtin_amdgcn_ballot_w64(r.valid) != 0;
+  const float most = wave_max(r.valid ? score : -INFINITY);
+  const float q = r.valid ? (score - most) / temperature : 0.f;
+  const float share = r.valid ? expf(q) : 0.f;
+  const float total = wave_sum(share);
+  r.t = r.some ? share / total : 0.f;
+  r.log_t = q - logf(total);
+  return r;
+}
+// logp: the student's log-probability of the lane's entry.  (A share that underflows adds nothing.)
+__device__ __forceinline__ float distill_loss(const Teacher& teacher, float logp, float temperature) {
+  const float sum = wave_sum(teacher.valid && teacher.t != 0.f ? teacher.t * (teacher.log_t - logp) : 0.f);
+  return teacher.some ? temperature * temperature * sum : 0.f;
+}
+
 // Teacher, loss, and what the gradient is made of: a row a workgroup, the first wavefront one lane an entry.  With P = 2^(x - base) over the
 // whole row, dz = a (p - t) is a 2^(base - lse2) (P - t 2^(lse2 - base)): the listed tokens' entries are put into P, from their fp32 logits
 // and rounded once, and the rest is the row's factor of the gradient.  A row whose reference has moved in some tile first has its tiles
 // brought to one base, lse2, here.  Of a row without a teacher (or of weight 0, as far as the gradient goes) nothing that the row holds
 // matters.
 __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __restrict__ ids, const float* __restrict__ z, int k, int V,
-                                                              float to_log2, const float4* __restrict__ stats, int parts,
+                                                              float to_log2, const float4* __restrict__ stats, int parts, int stride,
                                                               const float* __restrict__ scores, const float* __restrict__ weight,
                                                               float temperature, float* __restrict__ loss, RowTerms* __restrict__ terms,
                                                               const float* __restrict__ ref, const float* __restrict__ moved, int tiles,
@@ -305,25 +329,18 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   bool first = false, live = false;
   float l = 0.f, t = 0.f;
   if (first_wave) {
-    const RowStats r = join_stats(stats + row * parts, parts, lane);
+    const RowStats r = join_stats(stride == 1 ? stats + row * parts : stats + row, parts, lane, stride);
     const int64_t e = row * k + lane;
     id = lane < k ? ids[e] : -1;
-    const float score = lane < k ? scores[e] : -INFINITY;
-    const bool valid = id >= 0 && id < V && score != -INFINITY;
-    const bool some = __builtin_amdgcn_ballot_w64(valid) != 0;
-    const float most = wave_max(valid ? score : -INFINITY);
-    const float q = valid ? (score - most) / temperature : 0.f;
-    const float share = valid ? expf(q) : 0.f;
-    const float total = wave_sum(share);
-    t = some ? share / total : 0.f;
+    const Teacher teacher = teacher_of(id, lane < k ? scores[e] : -INFINITY, V, temperature);
+    t = teacher.t;
     l = fmaf(lane < k ? z[e] : 0.f, to_log2, -r.lse2);
-    const float term = valid && t != 0.f ? t * ((q - logf(total)) - l * LN2) : 0.f;
-    const float sum = wave_sum(term);
-    if (lane == 0) loss[row] = some ? temperature * temperature * sum : 0.f;
+    const float sum = distill_loss(teacher, l * LN2, temperature);
+    if (lane == 0) loss[row] = sum;
     if (terms != nullptr) {
       const float a = temperature * (weight != nullptr ? weight[row] : 1.f);
-      live = some && a != 0.f;
-      first = gather_same(id, valid, k, lane, t);
+      live = teacher.some && a != 0.f;
+      first = gather_same(id, teacher.valid, k, lane, t);
       bool other = false;
       for (int i = lane; i < parts; i += 64) other |= stats[row * parts + i].x != ref[row];
       other = __builtin_amdgcn_ballot_w64(other) != 0;
@@ -352,6 +369,17 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   if (first_wave && live && first) at[place_in_p(id)] = (uint16_t)pack_bf16(__builtin_amdgcn_exp2f(l) - t, 0.f);
 }
 
+// ll_logp_grad: a and b of a row's dz (see RowTerms), by a wavefront; g: the gradient of the lane's entry, 0 where there is none; gh and h
+// the entropy's gradient and the entropy.
+struct GradTerms {
+  float lse2, a, b;
+  bool live;              // some gradient is not zero
+};
+__device__ __forceinline__ GradTerms grad_terms(float g, float lse, float gh, float h, float inv_t) {
+  const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || gh != 0.f;
+  return {lse / LN2, -(wave_sum(g) + (gh != 0.f ? gh * h : 0.f)) * inv_t, -gh * LN2 * inv_t, live};
+}
+
 // The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
 __global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
                                                              const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
@@ -364,14 +392,12 @@ __global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, c
   const int id = lane < k ? p.ids[e] : -1;
   const bool valid = id >= 0 && id < p.V;
   float g = valid ? g_logp[e] : 0.f;
-  const float total = wave_sum(g), gh = g_entropy != nullptr ? g_entropy[row] : 0.f;
-  const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || gh != 0.f;
-  const float lse2 = lse[row] / LN2, inv_t = 1.f / temperature;
-  const float a = -(total + (g_entropy != nullptr ? gh * entropy[row] : 0.f)) * inv_t, b = -gh * LN2 * inv_t;
-  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -lse2);
+  const float inv_t = 1.f / temperature;
+  const GradTerms r = grad_terms(g, lse[row], g_entropy != nullptr ? g_entropy[row] : 0.f, entropy != nullptr ? entropy[row] : 0.f, inv_t);
+  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -r.lse2);
   const bool first = gather_same(id, valid, k, lane, g);
-  if (lane == 0) terms[row] = {lse2, a, b, live ? 1.f : 0.f};
-  if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(b, l, a)), __int_as_float(live && first ? id : -1));
+  if (lane == 0) terms[row] = {r.lse2, r.a, r.b, r.live ? 1.f : 0.f};
+  if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a)), __int_as_float(r.live && first ? id : -1));
 }
 
 // ll_logp_grad: the listed tokens' dz, from their fp32 logits and rounded once.
@@ -462,6 +488,12 @@ __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restr
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
+}  // namespace
+
+#include "ll_learn_few.h"
+
+namespace {
+
 // ---------------------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------------------
@@ -475,6 +507,8 @@ bool valid(const ll_shape* s, int k) {
 enum Needs { FORWARD, BACKWARD };
 
 struct LearnPlan {
+  bool few;                            // up to eight rows: one read of W (ll_learn_few.h)
+  int few_rows, few_streams, few_parts;
   int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
@@ -507,6 +541,36 @@ template <class F>
 auto with_row_tiles(int rt, F f) {
   using std::integral_constant;
   return rt == 1 ? f(integral_constant<int, 1>{}) : rt == 2 ? f(integral_constant<int, 2>{}) : rt == 3 ? f(integral_constant<int, 3>{}) : f(integral_constant<int, 4>{});
+}
+
+// Calls of so few rows that one read of W does (rows 0: not so): threads to a row of W, chunks a thread, rows as the kernel has them.
+struct FewShape {
+  int rows, tpr, nc;
+};
+FewShape few_shape(const ll_shape* s) {
+  const int n8 = s->d >> 3;
+  FewShape f = {};
+  if (s->N > 8 || s->d > FEW_LEARN_MAX_D) return f;
+  f.tpr = n8 <= 64 ? 64 : n8 <= 128 ? 128 : n8 <= 256 ? 256 : 512;
+  f.nc = n8 <= 512 ? 1 : n8 <= 1024 ? 2 : 4;
+  if (s->N > (f.nc == 1 ? 8 : f.nc == 2 ? 4 : 2)) return f;   // (what the registers hold)
+  f.rows = s->N <= 2 ? (s->N < 2 ? 1 : 2) : s->N <= 4 ? 4 : 8;
+  return f;
+}
+template <int WHAT, int N>
+auto few_kernel(const FewShape& f) -> void (*)(const FewLearnArgs) {
+  if (f.tpr == 64) return ll_learn_few_kernel<WHAT, N, 1, 64>;
+  if (f.tpr == 128) return ll_learn_few_kernel<WHAT, N, 1, 128>;
+  if (f.tpr == 256) return ll_learn_few_kernel<WHAT, N, 1, 256>;
+  if (f.nc == 1) return ll_learn_few_kernel<WHAT, N, 1, 512>;
+  if constexpr (N <= 4)
+    if (f.nc == 2) return ll_learn_few_kernel<WHAT, N, 2, 512>;
+  if constexpr (N <= 2) return ll_learn_few_kernel<WHAT, N, 4, 512>;
+  return nullptr;
+}
+template <int WHAT>
+auto few_kernel(const FewShape& f) {
+  return f.rows == 1 ? few_kernel<WHAT, 1>(f) : f.rows == 2 ? few_kernel<WHAT, 2>(f) : f.rows == 4 ? few_kernel<WHAT, 4>(f) : few_kernel<WHAT, 8>(f);
 }
 
 // Slices of the vocabulary for the product backwards: one workgroup a compute unit at a time, so that `tiles` of it take whole rounds,
@@ -548,6 +612,18 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     return at;
   };
   const size_t rows = (size_t)l.pass_rows;
+  const FewShape few = few_shape(s);
+  l.few = few.rows > 0;
+  if (l.few) {
+    l.few_rows = few.rows;
+    l.few_streams = FEW_LEARN_STREAMS - (int)N;
+    l.few_parts = l.few_streams * (FEW_LEARN_THREADS / few.tpr);
+    l.stats = take((size_t)l.few_parts * few.rows * sizeof(float4));
+    l.z = take(rows * k * sizeof(float));
+    if (needs == BACKWARD) l.part = take((size_t)l.few_parts * few.rows * s->d * sizeof(float));
+    l.total = off;
+    return l;
+  }
   l.stats = take(rows * l.splits * 4 * sizeof(float4));
   l.z = take(rows * k * sizeof(float));
   l.ref = take(rows * sizeof(float));
@@ -591,6 +667,29 @@ struct Pass {
 
   ListArgs list(const int32_t* ids) const { return {rows, W, ids, k, shape->d, shape->V, to_log2}; }
   dim3 list_threads() const { return dim3(64 * (k < 16 ? k : 16)); }   // a wavefront an entry
+
+  // Few rows: the one read of W, as it goes into ll_learn_few_join_kernel and its like.
+  template <int WHAT>
+  int few(const int32_t* ids, FewLearnArgs& p) const {
+    p.list = list(ids);
+    p.n = n;
+    p.streams = l.few_streams;
+    // (as in ll_project: rows of whole lines, and more of them than stay in the Infinity Cache beside other weights)
+    p.past_caches = ((uintptr_t)W | (uintptr_t)shape->d * 2) % 128 == 0 && (int64_t)shape->V * shape->d * 2 > ((int64_t)256 << 20) / 3;
+    p.z = at<float>(ws, l.z);
+    p.stats = at<float4>(ws, l.stats);
+    p.sums = at<float>(ws, l.part);
+    const int lists = WHAT == GRAD ? 0 : n;
+    hipLaunchKernelGGL(few_kernel<WHAT>(few_shape(shape)), dim3(p.streams + lists), dim3(FEW_LEARN_THREADS), 0, stream, p);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  }
+  template <bool DISTILL>
+  int few_join(const FewJoinArgs& p) const {
+    hipLaunchKernelGGL(ll_learn_few_join_kernel<DISTILL>, dim3((shape->d + 63) / 64, n), dim3(256), 0, stream, p);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  }
 
   template <int WHAT>
   int logits() const {
@@ -689,6 +788,14 @@ int ll_logp(const ll_shape* shape, void* workspace, size_t workspace_bytes, cons
   const LearnPlan l = plan_for(shape, k, FORWARD);
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
+    if (l.few) {
+      FewLearnArgs f = {};
+      LL_TRY(p.few<STATS>(ids, f));
+      hipLaunchKernelGGL(ll_logp_few_finish_kernel, dim3(p.n), dim3(64), 0, p.stream, f.list, f.z, f.stats, l.few_parts, l.few_rows, out_logp, out_lse,
+                         out_entropy);
+      LL_HIP_CHECK(hipGetLastError());
+      return LL_OK;
+    }
     LL_TRY(p.logits<STATS>());
     hipLaunchKernelGGL(ll_logp_finish_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), at<float4>(workspace, l.stats),
                        4 * l.splits, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
@@ -709,6 +816,19 @@ int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes,
   const LearnPlan l = plan_for(shape, k, BACKWARD);
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
+    if (l.few) {
+      FewJoinArgs j = {};
+      j.f.lse = lse;
+      j.f.entropy = entropy;
+      j.f.g_logp = g_logp;
+      j.f.g_entropy = g_entropy;
+      j.f.temperature = temperature;
+      LL_TRY(p.few<GRAD>(ids, j.f));
+      j.parts = l.few_parts;
+      j.stride = l.few_rows;
+      j.out = (uint16_t*)out_grad;
+      return p.few_join<false>(j);
+    }
     hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), lse + r0,
                        entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, temperature,
                        at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list));
@@ -734,12 +854,32 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
   LL_TRY(check(shape, workspace, workspace_bytes, l.total, rows, W_U, temperature, teacher_ids));
   return for_passes(shape, l, workspace, rows, W_U, temperature, k, stream, [&](const Pass& p, int64_t r0) -> int {
     const bool grad = out_grad != nullptr;
+    if (l.few && grad) {
+      FewJoinArgs j = {};
+      j.f.temperature = temperature;
+      LL_TRY(p.few<EXPS>(teacher_ids, j.f));
+      j.parts = l.few_parts;
+      j.stride = l.few_rows;
+      j.scores = teacher_scores;
+      j.weight = weight;
+      j.loss = out_loss;
+      j.out = (uint16_t*)out_grad;
+      return p.few_join<true>(j);
+    }
+    if (l.few) {
+      FewLearnArgs f = {};
+      LL_TRY(p.few<STATS>(teacher_ids, f));
+      hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), dim3(64), 0, p.stream, teacher_ids, f.z, k, shape->V, p.to_log2, f.stats, l.few_parts,
+                         l.few_rows, teacher_scores, weight, temperature, out_loss, nullptr, nullptr, nullptr, 0, nullptr, 0);
+      LL_HIP_CHECK(hipGetLastError());
+      return LL_OK;
+    }
     hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(teacher_ids + r0 * k), at<float>(workspace, l.z),
                        at<float>(workspace, l.ref));
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(grad ? p.logits<EXPS>() : p.logits<STATS>());
     hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), dim3(grad ? 256 : 64), 0, p.stream, teacher_ids + r0 * k, at<float>(workspace, l.z), k,
-                       shape->V, p.to_log2, at<float4>(workspace, l.stats), 4 * l.splits, teacher_scores + r0 * k,
+                       shape->V, p.to_log2, at<float4>(workspace, l.stats), 4 * l.splits, 1, teacher_scores + r0 * k,
                        weight != nullptr ? weight + r0 : nullptr, temperature, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
                        at<float>(workspace, l.ref), grad ? at<float>(workspace, l.moved) : nullptr, l.tiles,
                        grad ? at<uint16_t>(workspace, l.P) : nullptr, l.ldp);
