@@ -66,6 +66,8 @@ namespace {
 // four but for the matrix instructions, A's loads and A's fragments of the others: for calls of few rows, or whose rows
 // fill blocks of 256 badly.
 //
+// EPI::PAST_CACHES: W's loads go past the caches, where one row block reads a W that they cannot hold.
+//
 // EPI::BACK: the product backwards, C [rows, d] = A W with A [rows, V] (the gradient of the logits) and K over the vocabulary.  A is loaded
 // as above.  A stage of W is 64 vocabulary rows by the tile's 256 columns, [64 rows][512 B] in its slot, and K goes down its columns:
 // the fragments are read with ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows, two of them a fragment.  A
@@ -95,10 +97,12 @@ typedef __attribute__((address_space(3))) void* lptr_t;
 // explicit s_waitcnt of the main loop.  One instruction per load, with the LDS base set once per
 // tile, matters: a wavefront alone on its SIMD issues one instruction every four cycles or so, and
 // whatever sits between two MFMAs beyond the 16 cycles the first one runs leaves the pipe idle.
-template <int IMM>
+// PAST: the line is not kept in the caches.
+template <int IMM, bool PAST = false>
 __device__ __forceinline__ void load_to_lds_16(const unsigned char* base, unsigned off) {
   static_assert(IMM >= -4096 && IMM < 4096, "13-bit signed immediate");
-  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" : : "v"(off), "s"(base), "n"(IMM) : "memory");
+  if constexpr (PAST) asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2 nt" : : "v"(off), "s"(base), "n"(IMM) : "memory");
+  else asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" : : "v"(off), "s"(base), "n"(IMM) : "memory");
 }
 
 // LDS base of the loads that follow.  M0 is the compiler's own scratch register: it sets it right
@@ -293,7 +297,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
     LL_PIN_S(a_lds);
     LL_PIN_S(a_base);
   };
-#define LL_DMA_W(S) load_to_lds_16<((S) - 4) * 1024>(w_base, w_off[S])
+#define LL_DMA_W(S) load_to_lds_16<((S) - 4) * 1024, EPI::PAST_CACHES>(w_base, w_off[S])
 #define LL_DMA_A(S) if constexpr ((S) < A_LOADS) load_to_lds_16<((S) - 4) * 1024>(a_base, a_off[S])
 #define LL_DMA_TILE(DMA) DMA(0); DMA(1); DMA(2); DMA(3); DMA(4); DMA(5); DMA(6); DMA(7)
 

@@ -7,155 +7,9 @@
 // own.  A gradient needs every logit a second time, as the left factor of a product over the vocabulary.  Forming them again would be a
 // third product; instead the first one's epilogue leaves P, e^z relative to a reference, as bf16 behind it (2 bytes a logit, beside 4 d
 // flops), whose relative error is that of any bf16 number however small it is, and the second product reads that.
-#include "ll_epilogue.h"
-#include "ll_gemm_lds.h"
-
-#include <math.h>
+#include "ll_learn.h"
 
 namespace {
-
-constexpr int LIST_MAX = LL_LIST_MAX;      // one lane of a wavefront each
-constexpr int PASS_ROWS = 2048;            // rows of a pass: what the workspace holds of e^(z - m) or dz, 0.6 GB at V = 152 000
-constexpr float LN2 = 0.6931471805599453f;
-
-struct RowTerms {   // of a row's dz: with l = z log2 e - lse2, dz = 2^l (a + b l); its gradient is `factor` times P's product, zeros where that is 0
-  float lse2, a, b, factor;
-};
-
-struct LearnArgs : GemmArgs {
-  uint16_t* P;          // [rows, ldp] bf16
-  float* moved;         // [rows, tiles]: what the exponents of a tile are relative to, in powers of two
-  const float* ref;     // [rows]: what they start from
-  const RowTerms* terms;   // [rows]
-  int64_t ldp;
-  float to_log2;        // log2(e) / T
-};
-
-// Within 64 columns of P the vocabulary is permuted: a lane of the first product holds ids 16 t + 4 g .. + 3 of tiles t, and puts two
-// tiles' side by side, 16 bytes at a time; the second product takes W's rows in the same order.
-__device__ __forceinline__ int64_t place_in_p(int v) {
-  return (v & ~31) + 8 * ((v >> 2) & 3) + 4 * ((v >> 4) & 1) + (v & 3);
-}
-
-// STATS: statistics only; EXPS: and the exponentials; GRAD: dz where the statistics are known.
-//
-// Exponents are relative to a reference that is no maximum: with fp32's range a sum of 2^(x - ref) does as well for any ref that is
-// not far from it, and so does bf16 for the exponentials, so that a tile takes one look at its accumulators and not two.  The reference
-// moves, to the tile's maximum, where the lane's sum over a tile leaves `MOST` behind (or has overflowed), and the tile is taken again.
-// STATS starts from below everything, so that the first tile sets it, and moves it early, for the sake of T, whose terms are 2^l l.
-// EXPS starts from the largest listed logit, one for all splits of a row, and so near the row's maximum that hardly any row ever moves:
-// then all of P's row is relative to one number, which the product backwards need not know (see ll_distill_rows_kernel).
-enum { STATS, EXPS, GRAD };
-constexpr float MASKED = -1e30f;   // an exponent that stands for a column past the vocabulary: 2^l is 0, and l no infinity for what multiplies it
-template <int WHAT, int RT>
-struct LearnEpilogue {
-  struct State {   // of the lane's rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
-    float ref[RT], s[RT], t[RT];
-    RowTerms terms[WHAT == GRAD ? RT : 1];
-  };
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false;
-  static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
-  static constexpr float MOST = WHAT == EXPS ? 0x1p60f : 0x1p16f;
-  static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
-  static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
-  static __device__ __forceinline__ void init(State& st, const GemmArgs& args, int my_row, int) {
-    const LearnArgs& p = static_cast<const LearnArgs&>(args);
-#pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      const int row = min(row_of(my_row, j), p.rows - 1);
-      st.ref[j] = WHAT == EXPS ? p.ref[row] : NEG_BIG;
-      st.s[j] = st.t[j] = 0.f;
-      if (WHAT == GRAD) st.terms[j] = p.terms[row];
-    }
-  }
-  template <class ACC>
-  static __device__ __forceinline__ void tile(const ACC& acc, State& st, int v0, const GemmArgs& args, int my_row) {
-    const LearnArgs& p = static_cast<const LearnArgs&>(args);
-    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA's result is in its registers
-    if (v0 + BM <= p.V) rows_of_tile<true>(acc, st, v0, p, my_row);
-    else rows_of_tile<false>(acc, st, v0, p, my_row);
-  }
-  // Whether column q of the lane's eight of columns 32 u .. is in the vocabulary.
-  static __device__ __forceinline__ bool inside(int u, int q, int last) { return 16 * (2 * u + (q >> 2)) + (q & 3) <= last; }
-  // One row tile, eight values at a time: what they add to the sums, and what goes to P.  WHOLE: all columns are in the vocabulary.
-  template <bool WHOLE, class ACC>
-  static __device__ __forceinline__ float2 sums_of_tile(const ACC& acc, const State& st, int j, int last, float c, uint4* to, bool present) {
-    float s = 0.f, t = 0.f;
-    const float ref = WHAT == GRAD ? st.terms[j].lse2 : st.ref[j];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      float x[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        float l = fmaf(acc_read(acc[2 * u + (q >> 2)][j][q & 3]), c, -ref);
-        if (!WHOLE) l = inside(u, q, last) ? l : MASKED;
-        x[q] = __builtin_amdgcn_exp2f(l);
-        if (WHAT == GRAD) x[q] *= fmaf(st.terms[j].b, l, st.terms[j].a);
-        else s += x[q];
-        if (WHAT == STATS) t = fmaf(x[q], l, t);
-      }
-      if (WHAT != STATS && present)
-        to[4 * u] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-      LL_SCHED_FENCE();
-    }
-    return make_float2(s, t);
-  }
-  template <bool WHOLE, class ACC>
-  static __device__ __forceinline__ void rows_of_tile(const ACC& acc, State& st, int v0, const LearnArgs& p, int my_row) {
-    const int g = (threadIdx.x & 63) >> 4;
-    const float c = p.to_log2;
-    const int last = p.V - 1 - v0 - 4 * g;   // of the lane's 16 t + i, the last in the vocabulary
-#pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      const int row = row_of(my_row, j);
-      const bool present = row < p.rows;
-      uint4* const to = reinterpret_cast<uint4*>(p.P + row * p.ldp + v0 + 8 * g);
-      float2 add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
-      if (WHAT == GRAD) continue;
-      if (__builtin_amdgcn_ballot_w64(add.x > MOST) != 0) {
-        float m = NEG_BIG;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const float z = acc_read(acc[2 * u + (q >> 2)][j][q & 3]);
-            m = WHOLE || inside(u, q, last) ? fmaxf(m, z) : m;
-          }
-          LL_SCHED_FENCE();
-        }
-        const auto most = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
-        const auto any = [](uint32_t a, uint32_t b) { return a | b; };
-        // the four lanes of a row together
-        m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most)) * c;
-        const bool move = with_lane_xor<32>(with_lane_xor<16>(add.x > MOST ? 1u : 0u, any), any) != 0;
-        const float to_ref = move ? fmaxf(m, st.ref[j]) : st.ref[j], before = st.ref[j] - to_ref, keep = __builtin_amdgcn_exp2f(before);
-        st.t[j] = keep * fmaf(before, st.s[j], st.t[j]);
-        st.s[j] *= keep;
-        st.ref[j] = to_ref;
-        add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
-      }
-      st.s[j] += add.x;
-      st.t[j] += add.y;
-      if (WHAT == EXPS && g == 0 && present) p.moved[(int64_t)row * p.tiles + v0 / BM] = st.ref[j];
-    }
-  }
-  // Every lane its own (ref, S, T): four to a row and split.
-  static __device__ __forceinline__ void store(const GemmArgs& p, const State& st, int my_row, int split) {
-    if (WHAT == GRAD) return;
-#pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      const int row = row_of(my_row, j);
-      if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.ref[j], st.s[j], st.t[j], 0.f);
-    }
-  }
-};
-
-template <int WHAT, bool TAIL, int RT>
-__global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void ll_learn_logits_kernel(const LearnArgs p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  lens_gemm_dma<LearnEpilogue<WHAT, RT>, TAIL>(p, smem);
-}
 
 // Rows of a hidden size that is not a multiple of 64, zero padded to one.
 __global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __restrict__ rows, uint16_t* __restrict__ panel, int d, int64_t lda) {
@@ -163,35 +17,6 @@ __global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __res
   for (int c = threadIdx.x; c < lda / 8; c += 256)
     reinterpret_cast<uint4*>(panel + row * lda)[c] =
         8 * c < d ? reinterpret_cast<const uint4*>(rows + row * d)[c] : make_uint4(0, 0, 0, 0);
-}
-
-// Logits of a row's listed tokens (before the temperature), a wavefront an entry at a time; 0 for an id outside the vocabulary.  The
-// whole workgroup comes here.  Bound by the gathered rows of W: 1500 x 20 of 16 KB in 95 us, 5.2 TB/s.
-__device__ __forceinline__ void list_logits(const uint16_t* __restrict__ row, const uint16_t* __restrict__ W, const int32_t* __restrict__ ids, int k,
-                                            int d, int V, float* z) {
-  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  const uint4* a = reinterpret_cast<const uint4*>(row);
-  for (int i = threadIdx.x >> 6; i < k; i += waves) {
-    const int id = ids[i];
-    float s = 0.f;
-    if (id >= 0 && id < V) {
-      const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)id * d);
-      float part[2] = {0.f, 0.f};
-#pragma unroll 4
-      for (int c = lane; c < d / 8; c += 64) {
-        const uint4 x = a[c], y = w[c];
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          part[0] = fmaf(bf16_lo(xs[q]), bf16_lo(ys[q]), part[0]);
-          part[1] = fmaf(bf16_hi(xs[q]), bf16_hi(ys[q]), part[1]);
-        }
-      }
-      s = wave_sum(part[0] + part[1]);
-    }
-    if (lane == 0) z[i] = s;
-  }
-  __syncthreads();
 }
 
 struct RowStats {
@@ -223,22 +48,11 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
 }
 
 // A row a workgroup: what its listed tokens' logits are, then (the first wavefront, one lane an entry) what is made of them.
-struct ListArgs {
-  const uint16_t* rows;
-  const uint16_t* W;
-  const int32_t* ids;
-  int k, d, V;
-  float to_log2;
-  __device__ __forceinline__ void logits(float* z) const {
-    list_logits(rows + (int64_t)blockIdx.x * d, W, ids + (int64_t)blockIdx.x * k, k, d, V, z);
-  }
-};
-
 // A row's statistics from its parts, and its listed tokens' log-probabilities.
 __global__ __launch_bounds__(1024) void ll_logp_finish_kernel(const ListArgs p, const float4* __restrict__ stats, int parts,
                                                               float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ entropy) {
   __shared__ float z[LIST_MAX];
-  p.logits(z);
+  list_logits(p, blockIdx.x, z);
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x;
   if (lane >= 64) return;
@@ -273,7 +87,7 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
 // Before the first product: the listed tokens' logits, and the largest in powers of two (of a row without any: 0).
 __global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref) {
   __shared__ float z[LIST_MAX];
-  p.logits(z);
+  list_logits(p, blockIdx.x, z);
   const int lane = threadIdx.x;
   if (lane >= 64) return;
   const int64_t row = blockIdx.x, e = row * p.k + lane;
@@ -369,23 +183,12 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   if (first_wave && live && first) at[place_in_p(id)] = (uint16_t)pack_bf16(__builtin_amdgcn_exp2f(l) - t, 0.f);
 }
 
-// ll_logp_grad: a and b of a row's dz (see RowTerms), by a wavefront; g: the gradient of the lane's entry, 0 where there is none; gh and h
-// the entropy's gradient and the entropy.
-struct GradTerms {
-  float lse2, a, b;
-  bool live;              // some gradient is not zero
-};
-__device__ __forceinline__ GradTerms grad_terms(float g, float lse, float gh, float h, float inv_t) {
-  const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || gh != 0.f;
-  return {lse / LN2, -(wave_sum(g) + (gh != 0.f ? gh * h : 0.f)) * inv_t, -gh * LN2 * inv_t, live};
-}
-
 // The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
 __global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
                                                              const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
                                                              float temperature, RowTerms* __restrict__ terms, float2* __restrict__ list) {
   __shared__ float z[LIST_MAX];
-  p.logits(z);
+  list_logits(p, blockIdx.x, z);
   const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
   if (lane >= 64) return;
   const int64_t e = (int64_t)row * k + lane;
@@ -410,62 +213,6 @@ __global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __
   if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(entry.x, 0.f);
 }
 
-struct LearnBackArgs : BackArgs {
-  uint16_t* out;           // one slice: the gradient itself, [rows, d] bf16
-  const RowTerms* terms;
-};
-
-// dA = dz W over one slice of the vocabulary: the tile as it is, for ll_learn_join_kernel, or rounded where the slice is the whole.  A
-// lane has four columns of a row in each 16.
-template <int RT>
-struct BackEpilogue {
-  struct State {
-    int split;
-  };
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = true;
-  static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
-  static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
-  static __device__ __forceinline__ void init(State& st, const GemmArgs&, int, int split) { st.split = split; }
-  template <class ACC>
-  static __device__ __forceinline__ void tile(const ACC& acc, State& st, int c0, const GemmArgs& args, int my_row) {
-    const LearnBackArgs& p = static_cast<const LearnBackArgs&>(args);
-    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMA's result is in its registers
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      const int row = my_row - lane + 16 * j + (lane & 15);
-      if (row >= p.rows) continue;
-      const int c = c0 + 4 * (lane >> 4);
-      if (p.splits == 1) {
-        const float f = p.terms[row].factor;
-        uint16_t* const to = p.out + (int64_t)row * p.d + c;
-#pragma unroll
-        for (int t = 0; t < 16; ++t) {
-          if (c + 16 * t < p.d)
-            *reinterpret_cast<uint2*>(to + 16 * t) = f != 0.f ? make_uint2(pack_bf16(f * acc_read(acc[t][j][0]), f * acc_read(acc[t][j][1])),
-                                                                           pack_bf16(f * acc_read(acc[t][j][2]), f * acc_read(acc[t][j][3])))
-                                                              : make_uint2(0, 0);
-        }
-        continue;
-      }
-      float* const to = p.part + ((int64_t)st.split * p.rows + row) * p.d + c;
-#pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        if (c + 16 * t < p.d)
-          *reinterpret_cast<float4*>(to + 16 * t) = make_float4(acc_read(acc[t][j][0]), acc_read(acc[t][j][1]), acc_read(acc[t][j][2]), acc_read(acc[t][j][3]));
-      }
-    }
-  }
-  static __device__ __forceinline__ void store(const GemmArgs&, const State&, int, int) {}
-};
-
-template <int RT>
-__global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void ll_learn_back_kernel(const LearnBackArgs p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  lens_gemm_dma<BackEpilogue<RT>, false>(p, smem);
-}
-
 // The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)
 __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, int d,
                                                             const RowTerms* __restrict__ terms, uint16_t* __restrict__ out) {
@@ -488,15 +235,118 @@ __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restr
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
-}  // namespace
+// ll_logp of few rows: statistics from the parts, a row a workgroup.
+__global__ __launch_bounds__(64) void ll_logp_few_finish_kernel(const ListArgs p, const float* __restrict__ z, const float4* __restrict__ stats,
+                                                                int parts, int stride, float* __restrict__ logp, float* __restrict__ lse,
+                                                                float* __restrict__ entropy) {
+  const int row = blockIdx.x, lane = threadIdx.x;
+  const RowStats r = join_stats(stats + row, parts, lane, stride);
+  if (lane == 0) {
+    lse[row] = r.lse2 * LN2;
+    entropy[row] = -r.t * LN2;
+  }
+  if (lane < p.k) {
+    const int e = row * p.k + lane;
+    logp[e] = p.ids[e] >= 0 && p.ids[e] < p.V ? fmaf(z[e], p.to_log2, -r.lse2) * LN2 : NAN;
+  }
+}
 
-#include "ll_learn_few.h"
-
-namespace {
+// The parts' sums joined, and the listed tokens' rows of W: block (64 columns, row), sixteen runs of the parts and of the list side by side.
+// DISTILL: parts relative to their references, dA = a (sum p W - sum t W_id), and the loss; else sums of dz W, and g / T W_id.
+struct FewJoinArgs {
+  FewLearnArgs f;
+  int parts, stride;        // stride: rows of a part's sums and statistics
+  const float* scores;
+  const float* weight;
+  float* loss;
+  uint16_t* out;
+};
+template <bool DISTILL>
+__global__ __launch_bounds__(256) void ll_learn_few_join_kernel(const FewJoinArgs p) {
+  __shared__ float scale[DISTILL ? FEW_LEARN_STREAMS : 1];
+  __shared__ float4 red[16][16];
+  __shared__ float share[LIST_MAX];
+  __shared__ int id_of[LIST_MAX];
+  __shared__ float shared_factor, shared_ref;
+  const ListArgs& l = p.f.list;
+  const int row = blockIdx.y, k = l.k, lane = threadIdx.x & 63;
+  const float temperature = p.f.temperature;
+  if (threadIdx.x < 64) {
+    const int e = row * k + lane;
+    const int id = lane < k ? l.ids[e] : -1;
+    if (DISTILL) {
+      const RowStats r = join_stats(p.f.stats + row, p.parts, lane, p.stride);
+      const Teacher teacher = teacher_of(id, lane < k ? p.scores[e] : -INFINITY, l.V, temperature);
+      const float q = fmaf(lane < k ? p.f.z[e] : 0.f, l.to_log2, -r.lse2);
+      const float loss = distill_loss(teacher, q * LN2, temperature);
+      const float a = temperature * (p.weight != nullptr ? p.weight[row] : 1.f);
+      if (lane == 0) {
+        if (blockIdx.x == 0) p.loss[row] = loss;
+        shared_factor = teacher.some ? a : 0.f;
+        shared_ref = r.lse2;
+      }
+      share[lane] = -teacher.t;
+      id_of[lane] = teacher.valid ? id : -1;
+    } else {
+      const bool valid = id >= 0 && id < l.V;
+      const float g = valid ? p.f.g_logp[e] : 0.f;
+      const bool live = __builtin_amdgcn_ballot_w64(g != 0.f) != 0 || (p.f.g_entropy != nullptr && p.f.g_entropy[row] != 0.f);
+      if (lane == 0) shared_factor = live ? 1.f : 0.f;
+      share[lane] = g / temperature;
+      id_of[lane] = valid ? id : -1;
+    }
+  }
+  __syncthreads();
+  if (DISTILL) {
+    for (int i = threadIdx.x; i < p.parts; i += 256) {
+      const float4 q = p.f.stats[(int64_t)i * p.stride + row];
+      scale[i] = q.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(q.x - shared_ref);
+    }
+    __syncthreads();
+  }
+  const int col = threadIdx.x & 15, run = threadIdx.x >> 4, c = blockIdx.x * 64 + col * 4;
+  const float factor = shared_factor;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < l.d && factor != 0.f) {
+    const float* from = p.f.sums + (int64_t)row * l.d + c;
+    const int64_t stride = (int64_t)p.stride * l.d;
+#pragma unroll 8
+    for (int i = run; i < p.parts; i += 16) {
+      const float4 x = *reinterpret_cast<const float4*>(from + i * stride);
+      const float by = DISTILL ? scale[i] : 1.f;
+      s.x = fmaf(by, x.x, s.x);
+      s.y = fmaf(by, x.y, s.y);
+      s.z = fmaf(by, x.z, s.z);
+      s.w = fmaf(by, x.w, s.w);
+    }
+    for (int i = run; i < k; i += 16) {
+      if (id_of[i] < 0) continue;
+      const uint2 w = *reinterpret_cast<const uint2*>(l.W + (int64_t)id_of[i] * l.d + c);
+      const float by = share[i];
+      s.x = fmaf(by, bf16_lo(w.x), s.x);
+      s.y = fmaf(by, bf16_hi(w.x), s.y);
+      s.z = fmaf(by, bf16_lo(w.y), s.z);
+      s.w = fmaf(by, bf16_hi(w.y), s.w);
+    }
+  }
+  red[run][col] = s;
+  __syncthreads();
+  if (run != 0 || c >= l.d) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) {
+    const float4 x = red[i][col];
+    s.x += x.x;
+    s.y += x.y;
+    s.z += x.z;
+    s.w += x.w;
+  }
+  *reinterpret_cast<uint2*>(p.out + (int64_t)row * l.d + c) = make_uint2(pack_bf16(factor * s.x, factor * s.y), pack_bf16(factor * s.z, factor * s.w));
+}
 
 // ---------------------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------------------
+constexpr int64_t INFINITY_CACHE_BYTES = (int64_t)256 << 20;
 constexpr int LEARN_MAX_D = 65536, LEARN_MAX_V = 1 << 22;   // (a lane's offsets within 256 rows of P, or of W, fit 32 bits)
 
 bool valid(const ll_shape* s, int k) {
@@ -507,8 +357,8 @@ bool valid(const ll_shape* s, int k) {
 enum Needs { FORWARD, BACKWARD };
 
 struct LearnPlan {
-  bool few;                            // up to eight rows: one read of W (ll_learn_few.h)
-  int few_rows, few_streams, few_parts;
+  bool few;                            // up to eight rows: one read of W (ll_learn_few.hip)
+  int few_rows, few_parts;
   int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
@@ -537,40 +387,30 @@ int row_tiles(int rows) {
   return best;
 }
 
-template <class F>
-auto with_row_tiles(int rt, F f) {
-  using std::integral_constant;
-  return rt == 1 ? f(integral_constant<int, 1>{}) : rt == 2 ? f(integral_constant<int, 2>{}) : rt == 3 ? f(integral_constant<int, 3>{}) : f(integral_constant<int, 4>{});
-}
-
-// Calls of so few rows that one read of W does (rows 0: not so): threads to a row of W, chunks a thread, rows as the kernel has them.
+// Calls of so few rows that one read of W does (rows 0: not so): rows as the kernel has them, chunks a thread, groups and threads of a
+// workgroup, workgroups that read W.
 struct FewShape {
-  int rows, tpr, nc;
+  int rows, nc, groups, threads, streams;
 };
-FewShape few_shape(const ll_shape* s) {
+// A gradient: up to four rows (two above d = 8192, what the registers hold).  Whole calls, us, so | in two products, ll_distill: d = 256, V =
+// 150 000, 1 row 24 | 56, 4 rows 39 | 56; 1608, 50257: 35 | 76, 49 | 77; 2560, 151936: 139 | 275, 192 | 279; 4096, 128256: 179 | 372, 186 | 374;
+// 8192, 128256: 351 | 760, 363 | 761; 16384, 60000, 1 row 339 | 706.  (Eight rows: 60 | 56, 79 | 79, 360 | 284, 319 | 375 and, in too many registers,
+// 851 | 755.)  Statistics alone: up to eight where a row of W fills the workgroup.  ll_logp, 4 rows and 8: d = 256 23 | 27, 34 | 27; 2560 137 | 145,
+// 185 | 147; 4096 176 | 202, 178 | 205; 8192 342 | 436, 346 | 431.
+FewShape few_shape(const ll_shape* s, Needs needs) {
   const int n8 = s->d >> 3;
   FewShape f = {};
-  if (s->N > 8 || s->d > FEW_LEARN_MAX_D) return f;
-  f.tpr = n8 <= 64 ? 64 : n8 <= 128 ? 128 : n8 <= 256 ? 256 : 512;
+  if (s->d > FEW_LEARN_MAX_D) return f;
   f.nc = n8 <= 512 ? 1 : n8 <= 1024 ? 2 : 4;
-  if (s->N > (f.nc == 1 ? 8 : f.nc == 2 ? 4 : 2)) return f;   // (what the registers hold)
+  f.groups = n8 <= 64 ? 8 : n8 <= 128 ? 4 : n8 <= 256 ? 2 : 1;
+  f.threads = f.groups > 1 ? FEW_LEARN_THREADS : ((n8 + f.nc - 1) / f.nc + kWave - 1) / kWave * kWave;
+  const int most = f.nc == 4 ? 2 : needs == FORWARD && (f.nc == 2 || f.threads == FEW_LEARN_THREADS) && f.groups == 1 ? 8 : 4;
+  if (s->N > most) return f;
   f.rows = s->N <= 2 ? (s->N < 2 ? 1 : 2) : s->N <= 4 ? 4 : 8;
+  const int step = f.groups * few_learn_rows(f.rows, f.nc), steps = (s->V + step - 1) / step;
+  f.streams = NUM_CU - (int)s->N;   // (the listed tokens' logits have a compute unit each at first)
+  if (f.streams > steps) f.streams = steps;
   return f;
-}
-template <int WHAT, int N>
-auto few_kernel(const FewShape& f) -> void (*)(const FewLearnArgs) {
-  if (f.tpr == 64) return ll_learn_few_kernel<WHAT, N, 1, 64>;
-  if (f.tpr == 128) return ll_learn_few_kernel<WHAT, N, 1, 128>;
-  if (f.tpr == 256) return ll_learn_few_kernel<WHAT, N, 1, 256>;
-  if (f.nc == 1) return ll_learn_few_kernel<WHAT, N, 1, 512>;
-  if constexpr (N <= 4)
-    if (f.nc == 2) return ll_learn_few_kernel<WHAT, N, 2, 512>;
-  if constexpr (N <= 2) return ll_learn_few_kernel<WHAT, N, 4, 512>;
-  return nullptr;
-}
-template <int WHAT>
-auto few_kernel(const FewShape& f) {
-  return f.rows == 1 ? few_kernel<WHAT, 1>(f) : f.rows == 2 ? few_kernel<WHAT, 2>(f) : f.rows == 4 ? few_kernel<WHAT, 4>(f) : few_kernel<WHAT, 8>(f);
 }
 
 // Slices of the vocabulary for the product backwards: one workgroup a compute unit at a time, so that `tiles` of it take whole rounds,
@@ -601,10 +441,10 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
   const int most = NUM_CU / l.row_blocks < l.tiles ? NUM_CU / l.row_blocks : l.tiles;
   const int per = (l.tiles + most - 1) / most;
   l.splits = (l.tiles + per - 1) / per;
-  l.lda = (s->d + DK - 1) / DK * DK;
+  l.lda = (s->d + STAGE_K - 1) / STAGE_K * STAGE_K;
   l.ldp = (int64_t)l.tiles * BM;
   l.col_blocks = (s->d + BM - 1) / BM;
-  l.back_splits = slices(l.row_blocks * l.col_blocks, (s->V + DK - 1) / DK, l.pass_rows, s->d, l.row_blocks == 1 ? 1.5 : 1.5 * BLOCK_COST[l.row_tiles - 1]);
+  l.back_splits = slices(l.row_blocks * l.col_blocks, (s->V + STAGE_K - 1) / STAGE_K, l.pass_rows, s->d, l.row_blocks == 1 ? 1.5 : 1.5 * BLOCK_COST[l.row_tiles - 1]);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -612,12 +452,11 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     return at;
   };
   const size_t rows = (size_t)l.pass_rows;
-  const FewShape few = few_shape(s);
+  const FewShape few = few_shape(s, needs);
   l.few = few.rows > 0;
   if (l.few) {
     l.few_rows = few.rows;
-    l.few_streams = FEW_LEARN_STREAMS - (int)N;
-    l.few_parts = l.few_streams * (FEW_LEARN_THREADS / few.tpr);
+    l.few_parts = few.streams;
     l.stats = take((size_t)l.few_parts * few.rows * sizeof(float4));
     l.z = take(rows * k * sizeof(float));
     if (needs == BACKWARD) l.part = take((size_t)l.few_parts * few.rows * s->d * sizeof(float));
@@ -665,22 +504,29 @@ struct Pass {
   int n, k;
   hipStream_t stream;
 
+  int64_t w_bytes() const { return (int64_t)shape->V * shape->d * 2; }
+  bool whole_lines() const { return ((uintptr_t)W | (uintptr_t)shape->d * 2) % 128 == 0; }   // (else W's rows share lines, which the caches keep between two loads)
+  // The products read W past the caches where it is read once, by one row block, and is more than the Infinity Cache holds.  Whole calls
+  // past the caches over through them, ll_logp and ll_distill: d = 2560, V = 151936, 37 rows 0.92 and 0.96, 100 rows 0.95 and 1.01; 4096, 128256:
+  // 0.89 and 0.92, 0.90 and 0.95; 8192, 128256: 0.91 and 0.94, 0.89 and 0.96; two row blocks (348 rows) 0.98 to 1.0; 103 MB of W 1.1 and 1.13.
+  bool past_caches() const { return l.row_blocks == 1 && whole_lines() && w_bytes() > INFINITY_CACHE_BYTES; }
   ListArgs list(const int32_t* ids) const { return {rows, W, ids, k, shape->d, shape->V, to_log2}; }
   dim3 list_threads() const { return dim3(64 * (k < 16 ? k : 16)); }   // a wavefront an entry
 
   // Few rows: the one read of W, as it goes into ll_learn_few_join_kernel and its like.
-  template <int WHAT>
+  template <LearnWhat WHAT>
   int few(const int32_t* ids, FewLearnArgs& p) const {
     p.list = list(ids);
     p.n = n;
-    p.streams = l.few_streams;
-    // (as in ll_project: rows of whole lines, and more of them than stay in the Infinity Cache beside other weights)
-    p.past_caches = ((uintptr_t)W | (uintptr_t)shape->d * 2) % 128 == 0 && (int64_t)shape->V * shape->d * 2 > ((int64_t)256 << 20) / 3;
+    p.streams = l.few_parts;
+    // (as in ll_project: more of W than stays in the Infinity Cache beside other weights)
+    p.past_caches = whole_lines() && w_bytes() > INFINITY_CACHE_BYTES / 3;
     p.z = at<float>(ws, l.z);
     p.stats = at<float4>(ws, l.stats);
     p.sums = at<float>(ws, l.part);
     const int lists = WHAT == GRAD ? 0 : n;
-    hipLaunchKernelGGL(few_kernel<WHAT>(few_shape(shape)), dim3(p.streams + lists), dim3(FEW_LEARN_THREADS), 0, stream, p);
+    const FewShape f = few_shape(shape, WHAT == STATS ? FORWARD : BACKWARD);
+    hipLaunchKernelGGL(few_learn_kernel(WHAT, f.rows, f.nc, f.groups), dim3(p.streams + lists), dim3(f.threads), 0, stream, p);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   }
@@ -691,7 +537,7 @@ struct Pass {
     return LL_OK;
   }
 
-  template <int WHAT>
+  template <LearnWhat WHAT>
   int logits() const {
     LearnArgs p = {};
     p.A = rows;
@@ -719,10 +565,8 @@ struct Pass {
       p.ref = at<float>(ws, l.ref);
       p.terms = at<RowTerms>(ws, l.terms);
     }
-    const auto kernel = with_row_tiles(l.row_tiles, [&](auto rt) {
-      return l.lda != shape->d ? ll_learn_logits_kernel<WHAT, true, rt()> : ll_learn_logits_kernel<WHAT, false, rt()>;
-    });
-    const size_t lds = (size_t)SLOTS * SLOT_BYTES;
+    const LearnKernel kernel = learn_kernel(WHAT, l.lda != shape->d, past_caches(), l.row_tiles);
+    const size_t lds = LEARN_LDS;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
     const unsigned groups = (unsigned)((p.row_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
@@ -746,8 +590,8 @@ struct Pass {
     p.col_blocks = l.col_blocks;
     p.out = out;
     p.terms = at<RowTerms>(ws, l.terms);
-    const size_t lds = (size_t)SLOTS * SLOT_BYTES;
-    const auto kernel = with_row_tiles(l.row_tiles, [](auto rt) { return ll_learn_back_kernel<rt()>; });
+    const size_t lds = LEARN_LDS;
+    const LearnBackKernel kernel = learn_back_kernel(past_caches(), l.row_tiles);
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
     const unsigned groups = (unsigned)((p.row_blocks * p.col_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
