@@ -285,7 +285,7 @@ int ll_steer_sweep_topk(const ll_shape* shape, void* workspace, size_t workspace
  *
  * x is not rounded before its norm.
  *
- *   shape      N and d are used (d a multiple of 8, at most 32768), V is ignored
+ *   shape      N and d are used (d a multiple of 8, at most 16384), V is ignored
  *   hidden, y  bf16 [N, d]
  *   gate       bf16 [d] (gate_rows 0), bf16 [N, d] (gate_rows 1) or NULL (gate_rows 0)
  *   gamma_y    bf16 [d] or NULL;  gamma bf16 [d];  scale finite

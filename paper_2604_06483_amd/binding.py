@@ -396,6 +396,10 @@ def _empty(size, dtype, device, stream):
     return t
 
 
+def _like(t, stream):
+    return torch.empty_like(t) if stream is None else _empty(t.shape, t.dtype, t.device, stream)   # (1.2 us of host time against 1.75)
+
+
 def _workspace(workspace, need, device, stream):
     if workspace is None:
         return _empty((max(need(), 256),), torch.uint8, device, stream)
@@ -419,7 +423,7 @@ def ll_block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None, 
     if gamma_y is not None:
         _check(gamma_y, _BF16, "gamma_y", (d,))
     if out is None:
-        x, n = (_empty((N, d), _BF16, h2.device, stream) for _ in range(2))
+        x, n = _like(h2, stream), _like(h2, stream)
     else:
         x, n = out
         for t, name in ((x, "out[0]"), (n, "out[1]")):
@@ -457,8 +461,8 @@ def ll_block_norm_grad(hidden, y, gamma, eps, g_hidden, g_normed, *, gate=None, 
         _check(gamma_y, _BF16, "gamma_y", (d,))
     gate_rows = _gate(gate, N, d)
     dev = hidden.device
-    dh, dy = _empty((N, d), _BF16, dev, stream), _empty((N, d), _BF16, dev, stream)
-    dk = None if gate is None else _empty((N, d), _BF16, dev, stream) if gate_rows else _empty((d,), _F32, dev, stream)
+    dh, dy = _like(h2, stream), _like(h2, stream)
+    dk = None if gate is None else _like(gate, stream) if gate_rows else _empty((d,), _F32, dev, stream)
     dgy = None if gamma_y is None else _empty((d,), _F32, dev, stream)
     dg = _empty((d,), _F32, dev, stream)
     ws = _workspace(workspace, lambda: ll_block_norm_grad_workspace_bytes(N, d), dev, stream)
@@ -523,7 +527,7 @@ def ll_logp_grad(rows, W_U, ids, lse, entropy, g_logp, g_entropy=None, *, temper
     for t, name in ((entropy, "entropy"), (g_entropy, "g_entropy")):
         if t is not None:
             _check(t, _F32, name, (N,))
-    out = _empty((N, d), _BF16, rows.device, stream)
+    out = _like(r2, stream)
     ws = _workspace(workspace, lambda: ll_logp_grad_workspace_bytes(N, d, V, k), rows.device, stream)
     rc = (_lib or lib()).ll_logp_grad(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
                                       float(temperature), k, i2.data_ptr(), lse.data_ptr(), _ptr(entropy), g2.data_ptr(), _ptr(g_entropy),
@@ -545,7 +549,7 @@ def ll_distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weigh
     if weight is not None:
         _check(weight, _F32, "weight", (N,))
     loss = _empty((N,), _F32, rows.device, stream)
-    out = _empty((N, d), _BF16, rows.device, stream) if grad else None
+    out = _like(r2, stream) if grad else None
     ws = _workspace(workspace, lambda: (ll_distill_workspace_bytes if grad else ll_logp_workspace_bytes)(N, d, V, k), rows.device, stream)
     rc = (_lib or lib()).ll_distill(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
                                     float(temperature), k, i2.data_ptr(), s2.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(out),

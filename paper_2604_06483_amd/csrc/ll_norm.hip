@@ -20,8 +20,7 @@ namespace {
 
 using namespace ll;
 
-constexpr int NORM_MAX_D = 32768;        // four chunks of eight values for each of 1024 threads
-constexpr int GRAD_GROUPS = 1024;        // most workgroups of the gradient, each with its own sums of the parameters' gradients
+constexpr int NORM_MAX_D = 16384;        // two chunks of eight values for each of 1024 threads
 
 struct NormArgs {
   const uint16_t* hidden;     // [rows, d]
@@ -55,19 +54,21 @@ __device__ __forceinline__ uint4 narrow(const Eight& e) {
 __device__ __forceinline__ uint4 load8(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void store8(uint16_t* p, const Eight& e) { *reinterpret_cast<uint4*>(p) = narrow(e); }
 
-// Two sums over the workgroup's threads at once; `red` is this reduction's own place (see the kernels for when it is free again).
+// Two sums over the workgroup's threads at once; `red` is this reduction's own place (see the kernels for when it is free again).  A lane
+// reads one wavefront's pair and the sixteen are summed across lanes: one trip to LDS, not one for every wavefront.
 __device__ __forceinline__ float2 group_sum(float a, float b, float2* red) {
   a = wave_sum(a);
   b = wave_sum(b);
-  const int waves = blockDim.x >> 6;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(a, b);
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  if (waves == 1) return make_float2(a, b);
+  if (lane == 0) red[threadIdx.x >> 6] = make_float2(a, b);
   __syncthreads();
-  float2 t = red[0];
-  for (int w = 1; w < waves; ++w) {
-    t.x += red[w].x;
-    t.y += red[w].y;
-  }
-  return t;
+  const float2 q = (lane & 15) < waves ? red[lane & 15] : make_float2(0.f, 0.f);
+  const auto add = [](uint32_t u, uint32_t v) { return __float_as_uint(__uint_as_float(u) + __uint_as_float(v)); };
+  const auto sixteen = [&](float x) {
+    return __uint_as_float(with_lane_xor<1>(with_lane_xor<2>(with_lane_xor<4>(with_lane_xor<8>(__float_as_uint(x), add), add), add), add));
+  };
+  return make_float2(sixteen(q.x), sixteen(q.y));
 }
 
 // One workgroup a row, NIT chunks of eight values a thread.
@@ -127,61 +128,113 @@ __global__ __launch_bounds__(THREADS) void ll_block_norm_kernel(const NormArgs p
 // belongs to one thread), which are written once, for ll_block_norm_sums_kernel: no atomics, the same bits every time.
 // Places of the reductions alternate between rows: a place is written again two rows on, behind a barrier that every thread reaches
 // only after it has read it.
-template <int NIT, int THREADS, bool POST, bool GATED>
+// The next row's loads go out before this row's sums (AHEAD) and x is kept from its sum on, where the registers hold them: one chunk a
+// thread, d up to 8192; so does what all rows share.  More chunks form x twice and load the shared parameters, and g_hidden, where they
+// are used.  The sums for gate and gamma_y are in LDS (IN_LDS: more chunks; or both of them, which leaves 128 registers and no spill:
+// d = 2560, 55 500 rows 424 us with both in registers).
+enum { NO_GATE, SHARED_GATE, ROWS_GATE };
+constexpr bool sums_in_lds(int nit, bool post, int gate) { return nit > 1 || (post && gate == SHARED_GATE); }
+template <int NIT, int THREADS, bool POST, int GATE>
 __global__ __launch_bounds__(THREADS) void ll_block_norm_grad_kernel(const NormArgs p) {
+  constexpr bool AHEAD = NIT == 1, GATED = GATE != NO_GATE, IN_LDS = sums_in_lds(NIT, POST, GATE);
   __shared__ float2 red[2][3][THREADS / 64];
   const int n8 = p.d >> 3, threads = blockDim.x;
   const float inv_d = 1.f / (float)p.d;
-  const bool shared_gate = GATED && p.gate_stride == 0;
-  Eight sum_gate[GATED ? NIT : 1], sum_y[POST ? NIT : 1], sum[NIT];
-#pragma unroll
-  for (int it = 0; it < NIT; ++it)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sum[it].v[i] = 0.f;
-      if (GATED) sum_gate[it].v[i] = 0.f;
-      if (POST) sum_y[it].v[i] = 0.f;
-    }
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
-    const int64_t at = row * (int64_t)p.d;
+  struct Row {
     uint4 h[NIT], y[NIT], k[NIT], gh[NIT], gn[NIT];
+  };
+  const auto load = [&](int64_t row, Row& q) {
+    const int64_t at = row * (int64_t)p.d;
 #pragma unroll
     for (int it = 0; it < NIT; ++it) {
       const int c = threadIdx.x + threads * it;
-      h[it] = y[it] = k[it] = gh[it] = gn[it] = make_uint4(0, 0, 0, 0);
+      q.h[it] = q.y[it] = q.gh[it] = q.gn[it] = q.k[it] = make_uint4(0, 0, 0, 0);
       if (c < n8) {
-        h[it] = load8(p.hidden + at + 8 * c);
-        y[it] = load8(p.y + at + 8 * c);
-        gn[it] = load8(p.g_normed + at + 8 * c);
-        if (p.g_hidden != nullptr) gh[it] = load8(p.g_hidden + at + 8 * c);
-        if (GATED) k[it] = load8(p.gate + row * p.gate_stride + 8 * c);
+        q.h[it] = load8(p.hidden + at + 8 * c);
+        q.y[it] = load8(p.y + at + 8 * c);
+        q.gn[it] = load8(p.g_normed + at + 8 * c);
+        if (AHEAD && p.g_hidden != nullptr) q.gh[it] = load8(p.g_hidden + at + 8 * c);
+        if (GATE == ROWS_GATE) q.k[it] = load8(p.gate + at + 8 * c);
       }
+    }
+  };
+  uint4 gammas[AHEAD ? NIT : 1], gammas_y[POST && AHEAD ? NIT : 1], gates[GATE == SHARED_GATE && AHEAD ? NIT : 1];
+  const auto shared = [&](const uint4* kept, const uint16_t* from, int it) {
+    const int c = threadIdx.x + threads * it;
+    return AHEAD ? kept[it] : c < n8 ? load8(from + 8 * c) : make_uint4(0, 0, 0, 0);
+  };
+  extern __shared__ __align__(16) float lds_sums[];      // [2][d]: a thread's own columns
+  Eight sum_gate[GATE == SHARED_GATE && !IN_LDS ? NIT : 1], sum_y[POST && !IN_LDS ? NIT : 1], sum[NIT];
+  const auto lds_sum = [&](int which, int it) { return reinterpret_cast<float4*>(lds_sums + which * p.d + 8 * (threadIdx.x + threads * it)); };
+  const auto add = [&](Eight* sums, int which, int it, const Eight& v) {
+    if constexpr (!IN_LDS) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sums[it].v[i] += v.v[i];
+    } else if ((int)threadIdx.x + threads * it < n8) {
+      float4* at = lds_sum(which, it);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float4 x = at[q];
+        at[q] = make_float4(x.x + v.v[4 * q], x.y + v.v[4 * q + 1], x.z + v.v[4 * q + 2], x.w + v.v[4 * q + 3]);
+      }
+    }
+  };
+#pragma unroll
+  for (int it = 0; it < NIT; ++it) {
+    const int c = threadIdx.x + threads * it;
+    if (AHEAD) {
+      gammas[it] = c < n8 ? load8(p.gamma + 8 * c) : make_uint4(0, 0, 0, 0);
+      if (POST) gammas_y[it] = c < n8 ? load8(p.gamma_y + 8 * c) : make_uint4(0, 0, 0, 0);
+      if (GATE == SHARED_GATE) gates[it] = c < n8 ? load8(p.gate + 8 * c) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sum[it].v[i] = 0.f;
+      if (GATE == SHARED_GATE && !IN_LDS) sum_gate[it].v[i] = 0.f;
+      if (POST && !IN_LDS) sum_y[it].v[i] = 0.f;
+    }
+    if (IN_LDS && c < n8)
+      for (int which = 0; which < 2; ++which) lds_sum(which, it)[0] = lds_sum(which, it)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  int turn = 0;
+  Row now, next;
+  if (AHEAD) load(blockIdx.x, next);
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    const int64_t at = row * (int64_t)p.d;
+    if (AHEAD) {
+      now = next;
+      if (row + gridDim.x < p.rows) load(row + gridDim.x, next);
+    } else {
+      load(row, now);
     }
     float inv_y = 1.f;
     if (POST) {
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-      for (int it = 0; it < NIT; ++it) accum_sq(y[it], s0, s1);
+      for (int it = 0; it < NIT; ++it) accum_sq(now.y[it], s0, s1);
       inv_y = inv_rms_from_sumsq(group_sum(s0 + s1, 0.f, red[turn][0]).x, p.d, p.eps);
     }
     // x, and at once the sums of x^2 and of e x
+    const auto stream = [&](int it) {
+      const Eight hv = widen(now.h[it]), yv = widen(now.y[it]);
+      Eight gy, kv;
+      if (POST) gy = widen(shared(gammas_y, p.gamma_y, it));
+      if (GATED) kv = widen(GATE == SHARED_GATE ? shared(gates, p.gate, it) : now.k[it]);
+      Eight v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v.v[i] = fmaf(GATED ? p.scale * kv.v[i] : p.scale, POST ? yv.v[i] * inv_y * gy.v[i] : yv.v[i], hv.v[i]);
+      return v;
+    };
+    Eight x[AHEAD ? NIT : 1];
     float ss = 0.f, ex = 0.f;
 #pragma unroll
     for (int it = 0; it < NIT; ++it) {
-      const int c = threadIdx.x + threads * it;
-      const Eight hv = widen(h[it]), yv = widen(y[it]), kv = widen(k[it]), gv = widen(gn[it]);
-      Eight gy = {{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}}, gamma = gy;
-      if (c < n8) {
-        gamma = widen(load8(p.gamma + 8 * c));
-        if (POST) gy = widen(load8(p.gamma_y + 8 * c));
-      }
+      const Eight v = stream(it), gv = widen(now.gn[it]), gamma = widen(shared(gammas, p.gamma, it));
+      if (AHEAD) x[it] = v;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float u = POST ? yv.v[i] * inv_y * gy.v[i] : yv.v[i];
-        const float x = fmaf(GATED ? p.scale * kv.v[i] : p.scale, u, hv.v[i]);
-        ss = fmaf(x, x, ss);
-        ex = fmaf(gv.v[i] * gamma.v[i], x, ex);
+        ss = fmaf(v.v[i], v.v[i], ss);
+        ex = fmaf(gv.v[i] * gamma.v[i], v.v[i], ex);
       }
     }
     const float2 both = group_sum(ss, ex, red[turn][1]);
@@ -192,32 +245,33 @@ __global__ __launch_bounds__(THREADS) void ll_block_norm_grad_kernel(const NormA
 #pragma unroll
     for (int it = 0; it < NIT; ++it) {
       const int c = threadIdx.x + threads * it;
-      const Eight hv = widen(h[it]), yv = widen(y[it]), kv = widen(k[it]), gv = widen(gn[it]), ghv = widen(gh[it]);
-      Eight gy = {{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}}, gamma = gy, dx, dk;
-      if (c < n8) {
-        gamma = widen(load8(p.gamma + 8 * c));
-        if (POST) gy = widen(load8(p.gamma_y + 8 * c));
-      }
+      if (!AHEAD && p.g_hidden != nullptr && c < n8) now.gh[it] = load8(p.g_hidden + at + 8 * c);
+      const Eight yv = widen(now.y[it]), gv = widen(now.gn[it]), ghv = widen(now.gh[it]), gamma = widen(shared(gammas, p.gamma, it));
+      Eight gy, kv;
+      if (POST) gy = widen(shared(gammas_y, p.gamma_y, it));
+      if (GATED) kv = widen(GATE == SHARED_GATE ? shared(gates, p.gate, it) : now.k[it]);
+      const Eight xv = AHEAD ? x[AHEAD ? it : 0] : stream(it);
+      Eight dx, dk, dgy;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float yh = yv.v[i] * inv_y, u = POST ? yh * gy.v[i] : yv.v[i];
         const float factor = GATED ? p.scale * kv.v[i] : p.scale;
-        const float xh = fmaf(factor, u, hv.v[i]) * inv;
+        const float xh = xv.v[i] * inv;
         dx.v[i] = fmaf(gv.v[i] * gamma.v[i] - xh * mean_exh, inv, ghv.v[i]);
         du[it].v[i] = factor * dx.v[i];
         sum[it].v[i] = fmaf(gv.v[i], xh, sum[it].v[i]);
-        if (GATED) {
-          dk.v[i] = p.scale * u * dx.v[i];
-          sum_gate[it].v[i] += dk.v[i];
-        }
+        if (GATED) dk.v[i] = p.scale * u * dx.v[i];
         if (POST) {
-          sum_y[it].v[i] = fmaf(du[it].v[i], yh, sum_y[it].v[i]);
-          fy = fmaf(du[it].v[i] * gy.v[i], yh, fy);
+          dgy.v[i] = du[it].v[i] * yh;
+          du[it].v[i] *= gy.v[i];
+          fy = fmaf(du[it].v[i], yh, fy);
         }
       }
+      if (GATE == SHARED_GATE) add(sum_gate, 0, it, dk);
+      if (POST) add(sum_y, 1, it, dgy);
       if (c < n8) {
         store8(p.d_hidden + at + 8 * c, dx);
-        if (GATED && !shared_gate) store8(p.d_gate_rows + at + 8 * c, dk);
+        if (GATE == ROWS_GATE) store8(p.d_gate_rows + at + 8 * c, dk);
         if (!POST) store8(p.d_y + at + 8 * c, du[it]);
       }
     }
@@ -227,42 +281,49 @@ __global__ __launch_bounds__(THREADS) void ll_block_norm_grad_kernel(const NormA
       for (int it = 0; it < NIT; ++it) {
         const int c = threadIdx.x + threads * it;
         if (c >= n8) continue;
-        const Eight yv = widen(y[it]), gy = widen(load8(p.gamma_y + 8 * c));
+        const Eight yv = widen(now.y[it]);
         Eight dy;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dy.v[i] = (du[it].v[i] * gy.v[i] - yv.v[i] * inv_y * mean_fyh) * inv_y;
+        for (int i = 0; i < 8; ++i) dy.v[i] = (du[it].v[i] - yv.v[i] * inv_y * mean_fyh) * inv_y;
         store8(p.d_y + at + 8 * c, dy);
       }
     }
   }
-  auto put = [&](int which, const Eight* s) {
+  const auto put = [&](int which, auto&& of) {
     float* to = p.partial + ((int64_t)which * gridDim.x + blockIdx.x) * p.d;
 #pragma unroll
     for (int it = 0; it < NIT; ++it) {
       const int c = threadIdx.x + threads * it;
       if (c >= n8) continue;
-      *reinterpret_cast<float4*>(to + 8 * c) = make_float4(s[it].v[0], s[it].v[1], s[it].v[2], s[it].v[3]);
-      *reinterpret_cast<float4*>(to + 8 * c + 4) = make_float4(s[it].v[4], s[it].v[5], s[it].v[6], s[it].v[7]);
+      const Eight s = of(it);
+      *reinterpret_cast<float4*>(to + 8 * c) = make_float4(s.v[0], s.v[1], s.v[2], s.v[3]);
+      *reinterpret_cast<float4*>(to + 8 * c + 4) = make_float4(s.v[4], s.v[5], s.v[6], s.v[7]);
     }
   };
-  if (shared_gate) put(0, sum_gate);
-  if (POST) put(1, sum_y);
-  put(2, sum);
+  const auto kept = [&](const Eight* sums, int which, int it) {
+    if (!IN_LDS) return sums[it];
+    const float4 lo = lds_sum(which, it)[0], hi = lds_sum(which, it)[1];
+    return Eight{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
+  };
+  if (GATE == SHARED_GATE) put(0, [&](int it) { return kept(sum_gate, 0, it); });
+  if (POST) put(1, [&](int it) { return kept(sum_y, 1, it); });
+  put(2, [&](int it) { return sum[it]; });
 }
 
-// The workgroups' sums joined: block (64 columns, parameter); sixteen runs of the workgroups side by side, then the runs in order.
+// The workgroups' sums joined: block (32 columns, parameter); 32 runs of the workgroups side by side, then the runs in order.
 __global__ __launch_bounds__(256) void ll_block_norm_sums_kernel(const float* __restrict__ partial, int groups, int d,
                                                                  float* __restrict__ d_gate, float* __restrict__ d_gamma_y,
                                                                  float* __restrict__ d_gamma) {
-  __shared__ float4 red[16][16];
+  constexpr int LANES = 8, RUNS = 32;
+  __shared__ float4 red[RUNS][LANES];
   float* out = blockIdx.y == 0 ? d_gate : blockIdx.y == 1 ? d_gamma_y : d_gamma;
   if (out == nullptr) return;
-  const int col = threadIdx.x & 15, run = threadIdx.x >> 4, c = blockIdx.x * 64 + col * 4;
+  const int col = threadIdx.x % LANES, run = threadIdx.x / LANES, c = (blockIdx.x * LANES + col) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < d) {
     const float* from = partial + (int64_t)blockIdx.y * groups * d + c;
-#pragma unroll 4
-    for (int g = run; g < groups; g += 16) {
+#pragma unroll 8
+    for (int g = run; g < groups; g += RUNS) {
       const float4 x = *reinterpret_cast<const float4*>(from + (int64_t)g * d);
       s.x += x.x;
       s.y += x.y;
@@ -274,7 +335,7 @@ __global__ __launch_bounds__(256) void ll_block_norm_sums_kernel(const float* __
   __syncthreads();
   if (run != 0 || c >= d) return;
 #pragma unroll
-  for (int r = 1; r < 16; ++r) {
+  for (int r = 1; r < RUNS; ++r) {
     const float4 x = red[r][col];
     s.x += x.x;
     s.y += x.y;
@@ -284,21 +345,34 @@ __global__ __launch_bounds__(256) void ll_block_norm_sums_kernel(const float* __
   *reinterpret_cast<float4*>(out + c) = s;
 }
 
-// Chunks of eight values a thread and most threads of a workgroup: the fewest chunks that 512 threads hold a row with, up to two,
-// then 1024 threads.
+// Chunks of eight values a thread and most threads of a workgroup: the fewest chunks that 512 threads hold a row with, up to two, then
+// 1024 threads; of the gradient, whose registers are short, 1024 threads before a second chunk.
 template <class F>
-void with_chunks(int d, F f) {
+void with_chunks(int d, bool grad, F f) {
   using std::integral_constant;
   const int n8 = d >> 3;
   if (n8 <= 512) f(integral_constant<int, 1>{}, integral_constant<int, 512>{});
+  else if (n8 <= 1024 && grad) f(integral_constant<int, 1>{}, integral_constant<int, 1024>{});
   else if (n8 <= 1024) f(integral_constant<int, 2>{}, integral_constant<int, 512>{});
-  else if (n8 <= 2048) f(integral_constant<int, 2>{}, integral_constant<int, 1024>{});
-  else f(integral_constant<int, 4>{}, integral_constant<int, 1024>{});
+  else f(integral_constant<int, 2>{}, integral_constant<int, 1024>{});
 }
 unsigned threads_for(int d, int nit) { return (unsigned)(((d >> 3) + nit - 1) / nit + kWave - 1) / kWave * kWave; }
 
-int grad_groups(int64_t rows) { return (int)(rows < GRAD_GROUPS ? rows : GRAD_GROUPS); }
+// Workgroups of the gradient: as many as are on the chip at once (some 16 wavefronts a compute unit), each with its own sums of the
+// parameters' gradients.
+int grad_groups(int64_t rows, int d) {
+  int waves = 0;
+  with_chunks(d, true, [&](auto nit, auto) { waves = (int)threads_for(d, nit()) / kWave; });
+  const int most = 256 * (waves >= 16 ? 1 : 16 / waves);
+  return (int)(rows < most ? rows : most);
+}
 
+template <class F>
+void with_gate(int gate, F f) {
+  if (gate == NO_GATE) f(std::integral_constant<int, NO_GATE>{});
+  else if (gate == SHARED_GATE) f(std::integral_constant<int, SHARED_GATE>{});
+  else f(std::integral_constant<int, ROWS_GATE>{});
+}
 template <class F>
 void with_bool(bool b, F f) {
   if (b) f(std::true_type{});
@@ -344,10 +418,11 @@ int ll_block_norm(const ll_shape* shape, const void* hidden, const void* y, cons
   p.eps = eps;
   p.out_hidden = (uint16_t*)out_hidden;
   p.out_normed = (uint16_t*)out_normed;
-  with_chunks(p.d, [&](auto nit, auto threads) {
+  with_chunks(p.d, false, [&](auto nit, auto threads) {
     with_bool(gamma_y != nullptr, [&](auto post) {
-      hipLaunchKernelGGL((ll_block_norm_kernel<nit(), threads(), post()>), dim3((unsigned)p.rows), dim3(threads_for(p.d, nit())), 0,
-                         (hipStream_t)stream, p);
+      if constexpr (nit() > 1 || threads() == 512)
+        hipLaunchKernelGGL((ll_block_norm_kernel<nit(), threads(), post()>), dim3((unsigned)p.rows), dim3(threads_for(p.d, nit())), 0,
+                           (hipStream_t)stream, p);
     });
   });
   LL_HIP_CHECK(hipGetLastError());
@@ -356,7 +431,7 @@ int ll_block_norm(const ll_shape* shape, const void* hidden, const void* y, cons
 
 size_t ll_block_norm_grad_workspace_bytes(const ll_shape* shape) {
   if (!valid_shape(shape)) return 0;
-  return align_up((size_t)3 * grad_groups(shape->N > 0 ? shape->N : 1) * shape->d * sizeof(float), 256);
+  return align_up((size_t)3 * grad_groups(shape->N > 0 ? shape->N : 1, shape->d) * shape->d * sizeof(float), 256);
 }
 
 int ll_block_norm_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* hidden, const void* y,
@@ -391,20 +466,26 @@ int ll_block_norm_grad(const ll_shape* shape, void* workspace, size_t workspace_
   p.d_y = (uint16_t*)d_y;
   p.d_gate_rows = gate_rows ? (uint16_t*)d_gate : nullptr;
   p.partial = (float*)workspace;
-  const int groups = grad_groups(p.rows);
+  const int groups = grad_groups(p.rows, p.d);
+  int rc = LL_OK;
   if (groups > 0) {
-    with_chunks(p.d, [&](auto nit, auto threads) {
+    with_chunks(p.d, true, [&](auto nit, auto threads) {
       with_bool(gamma_y != nullptr, [&](auto post) {
-        with_bool(gate != nullptr, [&](auto gated) {
-          hipLaunchKernelGGL((ll_block_norm_grad_kernel<nit(), threads(), post(), gated()>), dim3(groups),
-                             dim3(threads_for(p.d, nit())), 0, (hipStream_t)stream, p);
+        with_gate(gate == nullptr ? NO_GATE : gate_rows ? ROWS_GATE : SHARED_GATE, [&](auto gated) {
+          if constexpr (nit() == 1 || threads() == 1024) {
+            const auto kernel = ll_block_norm_grad_kernel<nit(), threads(), post(), gated()>;
+            const size_t lds = sums_in_lds(nit(), post(), gated()) ? (size_t)2 * p.d * sizeof(float) : 0;
+            if (lds > 0) rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), (size_t)2 * NORM_MAX_D * sizeof(float));
+            if (rc == LL_OK) hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads_for(p.d, nit())), lds, (hipStream_t)stream, p);
+          }
         });
       });
     });
+    if (rc != LL_OK) return rc;
     LL_HIP_CHECK(hipGetLastError());
   }
   // (no rows: the sums over none are zeros)
-  hipLaunchKernelGGL(ll_block_norm_sums_kernel, dim3((unsigned)((p.d + 63) / 64), 3), dim3(256), 0, (hipStream_t)stream, p.partial, groups,
+  hipLaunchKernelGGL(ll_block_norm_sums_kernel, dim3((unsigned)((p.d + 31) / 32), 3), dim3(256), 0, (hipStream_t)stream, p.partial, groups,
                      p.d, gate != nullptr && !gate_rows ? (float*)d_gate : nullptr, d_gamma_y, d_gamma);
   LL_HIP_CHECK(hipGetLastError());
   return LL_OK;
