@@ -31,7 +31,7 @@ struct LearnArgs : GemmArgs {
 };
 
 struct LearnBackArgs : BackArgs {
-  uint16_t* out;           // one slice: the gradient itself, [rows, d] bf16
+  uint16_t* out;           // one slice, and nothing to add to it: the gradient itself, [rows, d] bf16; else nullptr
   const RowTerms* terms;
 };
 

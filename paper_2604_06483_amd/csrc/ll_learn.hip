@@ -11,12 +11,15 @@
 
 namespace {
 
-// Rows of a hidden size that is not a multiple of 64, zero padded to one.
-__global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __restrict__ rows, uint16_t* __restrict__ panel, int d, int64_t lda) {
-  const int64_t row = blockIdx.x;
-  for (int c = threadIdx.x; c < lda / 8; c += 256)
+// A row of a hidden size that is not a multiple of 64, zero padded to one, by a workgroup; no panel: the rows are read where they are.
+__device__ __forceinline__ void pad_row(const uint16_t* __restrict__ rows, int64_t row, int d, uint16_t* __restrict__ panel, int64_t lda) {
+  if (panel == nullptr) return;
+  for (int c = threadIdx.x; c < lda / 8; c += (int)blockDim.x)
     reinterpret_cast<uint4*>(panel + row * lda)[c] =
         8 * c < d ? reinterpret_cast<const uint4*>(rows + row * d)[c] : make_uint4(0, 0, 0, 0);
+}
+__global__ __launch_bounds__(256) void ll_learn_pad_kernel(const uint16_t* __restrict__ rows, uint16_t* __restrict__ panel, int d, int64_t lda) {
+  pad_row(rows, blockIdx.x, d, panel, lda);
 }
 
 struct RowStats {
@@ -84,9 +87,11 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
   return first;
 }
 
-// Before the first product: the listed tokens' logits, and the largest in powers of two (of a row without any: 0).
-__global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref) {
+// Before the first product: the rows padded, the listed tokens' logits, and the largest in powers of two (of a row without any: 0).
+__global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref,
+                                                                uint16_t* __restrict__ panel, int64_t lda) {
   __shared__ float z[LIST_MAX];
+  pad_row(p.rows, blockIdx.x, p.d, panel, lda);
   list_logits(p, blockIdx.x, z);
   const int lane = threadIdx.x;
   if (lane >= 64) return;
@@ -183,41 +188,40 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   if (first_wave && live && first) at[place_in_p(id)] = (uint16_t)pack_bf16(__builtin_amdgcn_exp2f(l) - t, 0.f);
 }
 
-// The same of ll_logp_grad: dz = (sum_i g_i [v = id_i] - p (G + gH (log p + H))) / T.
-__global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
-                                                             const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
-                                                             float temperature, RowTerms* __restrict__ terms, float2* __restrict__ list) {
-  __shared__ float z[LIST_MAX];
-  list_logits(p, blockIdx.x, z);
-  const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
+// ll_logp_grad, before the first product: the rows padded, and what a row's dz is made of but for its listed tokens, -p (G + gH (log p + H)) / T.
+__global__ __launch_bounds__(256) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
+                                                            const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
+                                                            float temperature, RowTerms* __restrict__ terms, uint16_t* __restrict__ panel,
+                                                            int64_t lda) {
+  pad_row(p.rows, blockIdx.x, p.d, panel, lda);
+  const int row = blockIdx.x, lane = threadIdx.x;
   if (lane >= 64) return;
-  const int64_t e = (int64_t)row * k + lane;
-  const int id = lane < k ? p.ids[e] : -1;
-  const bool valid = id >= 0 && id < p.V;
-  float g = valid ? g_logp[e] : 0.f;
-  const float inv_t = 1.f / temperature;
-  const GradTerms r = grad_terms(g, lse[row], g_entropy != nullptr ? g_entropy[row] : 0.f, entropy != nullptr ? entropy[row] : 0.f, inv_t);
-  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -r.lse2);
-  const bool first = gather_same(id, valid, k, lane, g);
+  const int64_t e = (int64_t)row * p.k + lane;
+  const int id = lane < p.k ? p.ids[e] : -1;
+  const GradTerms r = grad_terms(id >= 0 && id < p.V ? g_logp[e] : 0.f, lse[row], g_entropy != nullptr ? g_entropy[row] : 0.f,
+                                 entropy != nullptr ? entropy[row] : 0.f, 1.f / temperature);
   if (lane == 0) terms[row] = {r.lse2, r.a, r.b, r.live ? 1.f : 0.f};
-  if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a)), __int_as_float(r.live && first ? id : -1));
 }
 
-// ll_logp_grad: the listed tokens' dz, from their fp32 logits and rounded once.
-__global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __restrict__ list, int64_t entries, int k, uint16_t* __restrict__ P,
-                                                                int64_t ldp) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= entries) return;
-  const float2 entry = list[e];
-  const int id = __float_as_int(entry.y);
-  if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(entry.x, 0.f);
-}
-
-// The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)
-__global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, int d,
-                                                            const RowTerms* __restrict__ terms, uint16_t* __restrict__ out) {
+// The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)  LIST,
+// ll_logp_grad: and g / T times W's row of every listed token, in fp32.
+template <bool LIST>
+__global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, const ListArgs p,
+                                                            const RowTerms* __restrict__ terms, const float* __restrict__ g_logp, float inv_t,
+                                                            uint16_t* __restrict__ out) {
+  __shared__ float share[LIST ? LIST_MAX : 1];
+  __shared__ int id_of[LIST ? LIST_MAX : 1];
   const int64_t row = blockIdx.y;
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const int d = p.d, c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (LIST) {
+    if ((int)threadIdx.x < p.k) {
+      const int64_t e = row * p.k + threadIdx.x;
+      const int id = p.ids[e];
+      id_of[threadIdx.x] = id >= 0 && id < p.V ? id : -1;
+      share[threadIdx.x] = g_logp[e] * inv_t;
+    }
+    __syncthreads();
+  }
   if (c >= d) return;
   const float f = terms[row].factor;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -231,6 +235,18 @@ __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restr
       s.w += x.w;
     }
     s = make_float4(f * s.x, f * s.y, f * s.z, f * s.w);
+    if (LIST) {
+#pragma unroll 4
+      for (int i = 0; i < p.k; ++i) {
+        const int id = id_of[i];
+        const uint2 w = *reinterpret_cast<const uint2*>(p.W + (int64_t)max(id, 0) * d + c);
+        const float by = id >= 0 ? share[i] : 0.f;
+        s.x += id >= 0 ? by * bf16_lo(w.x) : 0.f;
+        s.y += id >= 0 ? by * bf16_hi(w.x) : 0.f;
+        s.z += id >= 0 ? by * bf16_lo(w.y) : 0.f;
+        s.w += id >= 0 ? by * bf16_hi(w.y) : 0.f;
+      }
+    }
   }
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
@@ -362,7 +378,7 @@ struct LearnPlan {
   int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
-  size_t stats, z, ref, panel, terms, list, moved, P, part, total;
+  size_t stats, z, ref, panel, terms, moved, P, part, total;
 };
 
 // Tiles of 16 rows a wavefront (64 rows a workgroup each): the fewest that hold all rows, else what costs least.  A row block costs 0.47,
@@ -463,16 +479,15 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     l.total = off;
     return l;
   }
-  l.stats = take(rows * l.splits * 4 * sizeof(float4));
+  l.stats = take(rows * l.splits * sizeof(float4));
   l.z = take(rows * k * sizeof(float));
   l.ref = take(rows * sizeof(float));
   l.panel = take(l.lda != s->d ? rows * l.lda * 2 : 0);
   if (needs == BACKWARD) {
     l.terms = take(rows * sizeof(RowTerms));
-    l.list = take(rows * k * sizeof(float2));
     l.moved = take(rows * l.tiles * sizeof(float));
     l.P = take(rows * l.ldp * 2);
-    l.part = take(l.back_splits > 1 ? rows * l.back_splits * s->d * sizeof(float) : 0);
+    l.part = take(rows * l.back_splits * s->d * sizeof(float));
   }
   l.total = off;
   return l;
@@ -537,15 +552,13 @@ struct Pass {
     return LL_OK;
   }
 
+  // where the rows are padded to, by a kernel before the first product
+  uint16_t* panel() const { return l.lda != shape->d ? at<uint16_t>(ws, l.panel) : nullptr; }
+
   template <LearnWhat WHAT>
   int logits() const {
     LearnArgs p = {};
-    p.A = rows;
-    if (l.lda != shape->d) {
-      hipLaunchKernelGGL(ll_learn_pad_kernel, dim3(n), dim3(256), 0, stream, rows, at<uint16_t>(ws, l.panel), shape->d, l.lda);
-      LL_HIP_CHECK(hipGetLastError());
-      p.A = at<uint16_t>(ws, l.panel);
-    }
+    p.A = panel() != nullptr ? panel() : rows;
     p.W = W;
     p.stats = at<float4>(ws, l.stats);
     p.lda = l.lda;
@@ -574,8 +587,8 @@ struct Pass {
     return LL_OK;
   }
 
-  // P to the gradient of the rows
-  int back(uint16_t* out) const {
+  // P to the gradient of the rows; g_logp: and of the listed tokens
+  int back(const int32_t* ids, const float* g_logp, float inv_t, uint16_t* out) const {
     LearnBackArgs p = {};
     p.A = at<uint16_t>(ws, l.P);
     p.W = W;
@@ -588,7 +601,7 @@ struct Pass {
     p.splits = l.back_splits;
     p.row_blocks = (n + l.block_rows - 1) / l.block_rows;
     p.col_blocks = l.col_blocks;
-    p.out = out;
+    p.out = g_logp == nullptr && p.splits == 1 ? out : nullptr;
     p.terms = at<RowTerms>(ws, l.terms);
     const size_t lds = LEARN_LDS;
     const LearnBackKernel kernel = learn_back_kernel(past_caches(), l.row_tiles);
@@ -596,9 +609,9 @@ struct Pass {
     const unsigned groups = (unsigned)((p.row_blocks * p.col_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
-    if (p.splits == 1) return LL_OK;
-    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 1023) / 1024, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
-                       at<RowTerms>(ws, l.terms), out);
+    if (p.out != nullptr) return LL_OK;
+    hipLaunchKernelGGL(g_logp != nullptr ? ll_learn_join_kernel<true> : ll_learn_join_kernel<false>, dim3((shape->d + 1023) / 1024, n), dim3(256), 0,
+                       stream, p.part, p.splits, n, list(ids), at<RowTerms>(ws, l.terms), g_logp, inv_t, out);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   }
@@ -640,9 +653,13 @@ int ll_logp(const ll_shape* shape, void* workspace, size_t workspace_bytes, cons
       LL_HIP_CHECK(hipGetLastError());
       return LL_OK;
     }
+    if (p.panel() != nullptr) {
+      hipLaunchKernelGGL(ll_learn_pad_kernel, dim3(p.n), dim3(256), 0, p.stream, p.rows, p.panel(), shape->d, l.lda);
+      LL_HIP_CHECK(hipGetLastError());
+    }
     LL_TRY(p.logits<STATS>());
     hipLaunchKernelGGL(ll_logp_finish_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), at<float4>(workspace, l.stats),
-                       4 * l.splits, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
+                       l.splits, out_logp + r0 * k, out_lse + r0, out_entropy + r0);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   });
@@ -673,16 +690,12 @@ int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes,
       j.out = (uint16_t*)out_grad;
       return p.few_join<false>(j);
     }
-    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), lse + r0,
+    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids + r0 * k), lse + r0,
                        entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, temperature,
-                       at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list));
+                       at<RowTerms>(workspace, l.terms), p.panel(), l.lda);
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(p.logits<GRAD>());
-    const int64_t entries = (int64_t)p.n * k;
-    hipLaunchKernelGGL(ll_learn_put_list_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, p.stream, at<float2>(workspace, l.list),
-                       entries, k, at<uint16_t>(workspace, l.P), l.ldp);
-    LL_HIP_CHECK(hipGetLastError());
-    return p.back((uint16_t*)out_grad + r0 * shape->d);
+    return p.back(ids + r0 * k, g_logp + r0 * k, 1.f / temperature, (uint16_t*)out_grad + r0 * shape->d);
   });
 }
 
@@ -719,17 +732,17 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
       return LL_OK;
     }
     hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(teacher_ids + r0 * k), at<float>(workspace, l.z),
-                       at<float>(workspace, l.ref));
+                       at<float>(workspace, l.ref), p.panel(), l.lda);
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(grad ? p.logits<EXPS>() : p.logits<STATS>());
     hipLaunchKernelGGL(ll_distill_rows_kernel, dim3(p.n), dim3(grad ? 256 : 64), 0, p.stream, teacher_ids + r0 * k, at<float>(workspace, l.z), k,
-                       shape->V, p.to_log2, at<float4>(workspace, l.stats), 4 * l.splits, 1, teacher_scores + r0 * k,
+                       shape->V, p.to_log2, at<float4>(workspace, l.stats), l.splits, 1, teacher_scores + r0 * k,
                        weight != nullptr ? weight + r0 : nullptr, temperature, out_loss + r0, grad ? at<RowTerms>(workspace, l.terms) : nullptr,
                        at<float>(workspace, l.ref), grad ? at<float>(workspace, l.moved) : nullptr, l.tiles,
                        grad ? at<uint16_t>(workspace, l.P) : nullptr, l.ldp);
     LL_HIP_CHECK(hipGetLastError());
     if (!grad) return LL_OK;
-    return p.back((uint16_t*)out_grad + r0 * shape->d);
+    return p.back(teacher_ids + r0 * k, nullptr, 0.f, (uint16_t*)out_grad + r0 * shape->d);
   });
 }
 

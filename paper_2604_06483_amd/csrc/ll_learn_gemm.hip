@@ -108,13 +108,16 @@ struct LearnEpilogue {
       if (WHAT == EXPS && g == 0 && present) p.moved[(int64_t)row * p.tiles + v0 / BM] = st.ref[j];
     }
   }
-  // Every lane its own (ref, S, T): four to a row and split.
+  // The four lanes of a row have one reference.
   static __device__ __forceinline__ void store(const GemmArgs& p, const State& st, int my_row, int split) {
     if (WHAT == GRAD) return;
+    const auto add = [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
+    const auto four = [&](float x) { return __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(x), add), add)); };
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
-      if (row < p.rows) p.stats[((int64_t)row * p.splits + split) * 4 + ((threadIdx.x & 63) >> 4)] = make_float4(st.ref[j], st.s[j], st.t[j], 0.f);
+      const float s = four(st.s[j]), t = four(st.t[j]);
+      if (row < p.rows && (threadIdx.x & 63) < 16) p.stats[(int64_t)row * p.splits + split] = make_float4(st.ref[j], s, t, 0.f);
     }
   }
 };
@@ -147,7 +150,7 @@ struct BackEpilogue {
       const int row = my_row - lane + 16 * j + (lane & 15);
       if (row >= p.rows) continue;
       const int c = c0 + 4 * (lane >> 4);
-      if (p.splits == 1) {
+      if (p.out != nullptr) {
         const float f = p.terms[row].factor;
         uint16_t* const to = p.out + (int64_t)row * p.d + c;
 #pragma unroll
