@@ -418,14 +418,25 @@ int ll_block_norm(const ll_shape* shape, const void* hidden, const void* y, cons
   p.eps = eps;
   p.out_hidden = (uint16_t*)out_hidden;
   p.out_normed = (uint16_t*)out_normed;
-  with_chunks(p.d, false, [&](auto nit, auto threads) {
-    with_bool(gamma_y != nullptr, [&](auto post) {
-      if constexpr (nit() > 1 || threads() == 512)
-        hipLaunchKernelGGL((ll_block_norm_kernel<nit(), threads(), post()>), dim3((unsigned)p.rows), dim3(threads_for(p.d, nit())), 0,
-                           (hipStream_t)stream, p);
+  // (a launch has at most 2^32 threads)
+  constexpr int64_t MOST = (int64_t)1 << 21;
+  for (int64_t left = shape->N; left > 0; left -= MOST) {
+    p.rows = left < MOST ? left : MOST;
+    with_chunks(p.d, false, [&](auto nit, auto threads) {
+      with_bool(gamma_y != nullptr, [&](auto post) {
+        if constexpr (nit() > 1 || threads() == 512)
+          hipLaunchKernelGGL((ll_block_norm_kernel<nit(), threads(), post()>), dim3((unsigned)p.rows), dim3(threads_for(p.d, nit())), 0,
+                             (hipStream_t)stream, p);
+      });
     });
-  });
-  LL_HIP_CHECK(hipGetLastError());
+    LL_HIP_CHECK(hipGetLastError());
+    const int64_t step = MOST * p.d;
+    p.hidden += step;
+    p.y += step;
+    if (gate_rows) p.gate += step;
+    p.out_hidden += step;
+    p.out_normed += step;
+  }
   return LL_OK;
 }
 

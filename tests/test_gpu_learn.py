@@ -130,6 +130,23 @@ def test_logits_far_apart(spread, temperature):
     check_distill(a, W, ids, 5 * torch.randn((N, k), generator=g), None, temperature)
 
 
+@pytest.mark.parametrize("N,d,V", [(1, 256, 3000), (4, 1024, 2000), (3, 5120, 700), (70, 512, 3000), (300, 264, 2000)])
+@pytest.mark.parametrize("gap", [20.0, 300.0])
+def test_lists_far_below_the_most_likely_token(N, d, V, gap):
+    """Every second row has its probability on a token that its list does not name, up to hundreds of nats above those that it does: the
+    exponents' reference, which starts from the list, has to move, in the middle of the vocabulary."""
+    say(f"lists far below N={N} d={d} V={V} gap={gap}")
+    a, W, ids, g = inputs(N, d, V, 5, spread=1.0)
+    top = V // 2 + 7
+    ids = torch.where((ids == top) | (ids < 0) | (ids >= V), (ids.abs() + 1) % (V // 4), ids).to(torch.int32)
+    W[top] = (0.02 * torch.sign(W[top].float())).to(torch.bfloat16)       # of length 0.02 sqrt(d)
+    a = a.float()
+    a[::2] += gap / (0.0004 * d) * W[top].float()                          # its logit: gap and some
+    a = a.to(torch.bfloat16)
+    check_distill(a, W, ids, torch.randn((N, 5), generator=g), torch.rand((N,), generator=g) + 0.1, 1.0)
+    check_logp(a, W, ids, g, 1.0)
+
+
 def test_nothing_of_a_masked_row_matters():
     say("masked rows of NaN and infinities")
     N, d, V, k = 40, 136, 900, 5
@@ -190,6 +207,23 @@ def test_the_same_bits_twice_and_from_any_workspace(N, d, V, k):
     for other in runs[1:]:
         for x, y in zip(runs[0], other):
             assert torch.equal(x.nan_to_num(7.0), y.nan_to_num(7.0))
+
+
+def test_the_last_rows_of_a_pass_of_long_rows():
+    """P of a pass is more than 2^31 bytes apart at its ends: the last rows' gradients are those of a call of them alone, but for the order of
+    the slices' sums."""
+    say("rows far apart in the workspace")
+    N, d, V, k = 1800, 64, 700001, 2
+    g = torch.Generator(device=DEV).manual_seed(2)
+    W = (0.1 * torch.randn((V, d), generator=g, device=DEV)).to(torch.bfloat16)
+    a = torch.randn((N, d), generator=g, device=DEV).to(torch.bfloat16)
+    ids = torch.randint(0, V, (N, k), generator=g, device=DEV, dtype=torch.int32)
+    ids[:, 0] = V - 1
+    scores = torch.randn((N, k), generator=g, device=DEV)
+    loss, grad = LL.ll_distill(a, W, ids, scores)
+    few, rest = LL.ll_distill(a[-20:].contiguous(), W, ids[-20:].contiguous(), scores[-20:].contiguous())
+    torch.testing.assert_close(loss[-20:], few, rtol=1e-5, atol=1e-5)
+    torch.testing.assert_close(grad[-20:].float(), rest.float(), rtol=2 ** -7, atol=2 ** -7 * float(rest.float().abs().mean()))
 
 
 def test_no_rows():

@@ -165,3 +165,20 @@ def test_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(captured, both()):
             assert torch.equal(a, b), turn
+
+
+@pytest.mark.parametrize("N,d", [(270000, 8192), ((1 << 21) + 3, 64)])
+def test_offsets_past_32_bits_and_rows_past_a_launch(N, d):
+    """The last rows of a long call are those of a call of them alone."""
+    say(f"block norm N={N} d={d}")
+    g = torch.Generator(device=DEV).manual_seed(3)
+    normal = lambda *s: torch.randn(s, generator=g, device=DEV, dtype=torch.bfloat16)
+    h, y, k, gn, gamma = normal(N, d), normal(N, d), normal(N, d), normal(N, d), normal(d)
+    x, n = LL.ll_block_norm(h, y, gamma, 1e-5, gate=k)
+    dh, dy, dk, _, _ = LL.ll_block_norm_grad(h, y, gamma, 1e-5, None, gn, gate=k)
+    last = slice(N - 5, N)
+    part = [t[last].contiguous() for t in (h, y, k, gn)]
+    x2, n2 = LL.ll_block_norm(part[0], part[1], gamma, 1e-5, gate=part[2])
+    dh2, dy2, dk2, _, _ = LL.ll_block_norm_grad(part[0], part[1], gamma, 1e-5, None, part[3], gate=part[2])
+    for a, b in ((x, x2), (n, n2), (dh, dh2), (dy, dy2), (dk, dk2)):
+        assert torch.equal(a[last], b)
