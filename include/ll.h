@@ -327,6 +327,8 @@ int ll_block_norm_grad(const ll_shape* shape, void* workspace, size_t workspace_
  *   out_grad [N, d] bf16 = sum_v dz[r, v] W_U[v, :]
  *
  * Entries whose id is outside [0, V) take no part.  A row whose gradients are all zero gets zeros, whatever it holds.
+ * The workspace's size goes up and down with N (whole passes, slices of the vocabulary): ask for each N, or take the largest.  A device's first call
+ * of a kind sets a kernel attribute: make it outside stream capture.
  * W_U gets no gradient: the lens reuses the model's own.  Rows are processed in passes of at most 2048, for which the
  * workspace holds dz in bf16 (2 bytes times V a row).
  * A row that holds NaN or infinity gets NaN; no other row is affected.
@@ -343,7 +345,7 @@ int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes,
 /*
  * Distillation from a teacher's top tokens: loss and gradient in one call.  The teacher is a list of k tokens a row with scores
  * (logits, or log-probabilities: a constant a row makes no difference), as ll_project lists the last layer's.  Per row, over the
- * entries whose id is in [0, V) and whose score is not -infinity,
+ * entries whose id is in [0, V) and whose score is not -infinity (the others finite),
  *
  *   t = softmax(teacher_scores / temperature),   p = softmax(rows W_U^T / temperature) over the whole vocabulary
  *   out_loss[r] = temperature^2 sum_i t[i] (log t[i] - log p[id_i])
