@@ -8,8 +8,9 @@
 // threads; else a row has the workgroup, of just the wavefronts that it needs.  A group takes R rows at a time and has the next 2 R
 // there or in flight, up to 128 KB a compute unit.  The R x N products are summed over a wavefront by halving (each step adds two values' halves
 // across lanes, so that 32 values take some 80 instructions and not 32 sums of six steps), over a group's wavefronts through LDS, one
-// barrier for R rows, and go back to all lanes as scalars.  That is a long chain of waits for the two wavefronts of a SIMD, so the R rows
-// before are added to the sums behind the barrier, while the next R rows' logits come out of LDS.
+// barrier for R rows, and go back to all lanes as scalars.  That is a long chain of waits for the two wavefronts of a SIMD, so from three
+// rows on the R rows before are added to the sums behind the barrier, while the next R rows' logits come out of LDS (d = 2560, V = 151936, 4
+// rows 209 | 192 us, 5120 360 | 330; for one or two rows the third buffer costs 2 to 4 %: d = 8192 341 | 355).
 // Bound by the read of W_U up to four rows, by the fused multiply-adds above: 8 N + 8 instructions for a chunk's part of the sums, and
 // half of 8 N for its logits (v_dot2_f32_bf16: two products a lane, fp32 sums, as exact as two fused multiply-adds).
 #include "ll_learn.h"
@@ -235,28 +236,44 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
     if (WHAT == STATS) t = fmaf(prob, e, t);
     return WHAT == GRAD ? prob * fmaf(term_b, e, term_a) : prob;
   };
-  // Rows of step, step + 1 (both there) and step + 2 (loaded): the first into the sums, the second's weights.
-  float prob = 0.f;
-  const auto advance = [&](int step, const uint4 (&w)[R][NC], const uint4 (&next)[R][NC], uint4 (&far)[R][NC]) {
-    const bool more = step + 1 < step1;
-    load(min(step + 2, step1 - 1), far);
-    float sums[WAVES];
-    if (more) dots_of(next, step + 1, sums);
-    if (WHAT != STATS) add_rows(w, prob);
-    if (more) prob = weigh(sums, step + 1);
-  };
-  uint4 w0[R][NC], w1[R][NC], w2[R][NC];
-  if (step0 < step1) {
-    load(step0, w0);
-    load(min(step0 + 1, step1 - 1), w1);
-    float sums[WAVES];
-    dots_of(w0, step0, sums);
-    prob = weigh(sums, step0);
-  }
-  for (int step = step0; step < step1; step += 3) {
-    advance(step, w0, w1, w2);
-    if (step + 1 < step1) advance(step + 1, w1, w2, w0);
-    if (step + 2 < step1) advance(step + 2, w2, w0, w1);
+  if constexpr (N <= 2) {   // few instructions beside the read: one step after the other
+    const auto take = [&](int step, const uint4 (&w)[R][NC], uint4 (&next)[R][NC]) {
+      load(min(step + 1, step1 - 1), next);
+      float sums[WAVES];
+      dots_of(w, step, sums);
+      const float prob = weigh(sums, step);
+      if (WHAT != STATS) add_rows(w, prob);
+    };
+    uint4 w0[R][NC], w1[R][NC];
+    if (step0 < step1) load(step0, w0);
+    for (int step = step0; step < step1; step += 2) {
+      take(step, w0, w1);
+      if (step + 1 < step1) take(step + 1, w1, w0);
+    }
+  } else {
+    // Rows of step, step + 1 (both there) and step + 2 (loaded): the first into the sums, the second's weights.
+    float prob = 0.f;
+    const auto advance = [&](int step, const uint4 (&w)[R][NC], const uint4 (&next)[R][NC], uint4 (&far)[R][NC]) {
+      const bool more = step + 1 < step1;
+      load(min(step + 2, step1 - 1), far);
+      float sums[WAVES];
+      if (more) dots_of(next, step + 1, sums);
+      if (WHAT != STATS) add_rows(w, prob);
+      if (more) prob = weigh(sums, step + 1);
+    };
+    uint4 w0[R][NC], w1[R][NC], w2[R][NC];
+    if (step0 < step1) {
+      load(step0, w0);
+      load(min(step0 + 1, step1 - 1), w1);
+      float sums[WAVES];
+      dots_of(w0, step0, sums);
+      prob = weigh(sums, step0);
+    }
+    for (int step = step0; step < step1; step += 3) {
+      advance(step, w0, w1, w2);
+      if (step + 1 < step1) advance(step + 1, w1, w2, w0);
+      if (step + 2 < step1) advance(step + 2, w2, w0, w1);
+    }
   }
   const bool speaks = wave % WAVES == 0 && my_r == 0 && (lane & ((1 << VALUE_BIT) - 1)) == 0;   // for a lens row of its group
   if (WHAT != GRAD) {
