@@ -8,7 +8,7 @@
 namespace ll {
 
 constexpr int LIST_MAX = LL_LIST_MAX;      // one lane of a wavefront each
-constexpr int PASS_ROWS = 2048;            // rows of a pass: what the workspace holds of e^(z - m) or dz, 0.6 GB at V = 152 000
+constexpr int PASS_ROWS = 2048;            // rows of a pass: what the workspace holds of P, 0.6 GB at V = 152 000
 constexpr int STAGE_K = 64;                // columns (backwards: ids) of a stage of the products
 constexpr size_t LEARN_LDS = 160 << 10;    // what they take of LDS
 constexpr float LN2 = 0.6931471805599453f;
@@ -31,7 +31,7 @@ struct LearnArgs : GemmArgs {
 };
 
 struct LearnBackArgs : BackArgs {
-  uint16_t* out;           // one slice, and nothing to add to it: the gradient itself, [rows, d] bf16; else nullptr
+  uint16_t* out;           // one slice: the gradient itself, [rows, d] bf16; else nullptr
   const RowTerms* terms;
 };
 
@@ -49,9 +49,9 @@ constexpr int FEW_LEARN_MAX_D = 16384;
 
 struct FewLearnArgs {
   ListArgs list;            // rows, W, ids, k, d, V, to_log2
-  int n, streams;           // rows; workgroups that read W_U (those behind them: the listed tokens' logits)
+  int n, streams;           // rows; workgroups that read W_U (behind them one a row for the listed tokens' logits, but for GRAD)
   int past_caches;          // W's loads go past the caches
-  float* z;                 // [n, k]: the listed tokens' logits (nullptr: not asked for)
+  float* z;                 // [n, k]: the listed tokens' logits (not GRAD)
   float4* stats;            // [streams, N]: (ref, S, T)
   float* sums;              // [streams, N, d]
   // GRAD: what the row's dz is made of
@@ -93,7 +93,7 @@ __device__ __forceinline__ int64_t place_in_p(int v) {
 }
 
 // Logits of a row's listed tokens (before the temperature), a wavefront an entry at a time; 0 for an id outside the vocabulary.  The
-// whole workgroup comes here.  Bound by the gathered rows of W: 1500 x 20 of 16 KB in 95 us, 5.2 TB/s.
+// whole workgroup comes here.  Bound by the gathered rows of W: 1500 x 20 of 16 KB in 103 us, 4.8 TB/s.
 __device__ __forceinline__ void list_logits(const ListArgs& p, int row, float* z) {
   const uint16_t* const W = p.W;
   const int32_t* const ids = p.ids + (int64_t)row * p.k;

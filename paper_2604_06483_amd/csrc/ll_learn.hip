@@ -50,8 +50,8 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   return r;
 }
 
-// A row a workgroup: what its listed tokens' logits are, then (the first wavefront, one lane an entry) what is made of them.
-// A row's statistics from its parts, and its listed tokens' log-probabilities.
+// A row's listed tokens' logits, by the workgroup, then its statistics from their parts and the log-probabilities, by the first wavefront, one
+// lane an entry.
 __global__ __launch_bounds__(1024) void ll_logp_finish_kernel(const ListArgs p, const float4* __restrict__ stats, int parts,
                                                               float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ entropy) {
   __shared__ float z[LIST_MAX];
@@ -188,40 +188,44 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   if (first_wave && live && first) at[place_in_p(id)] = (uint16_t)pack_bf16(__builtin_amdgcn_exp2f(l) - t, 0.f);
 }
 
-// ll_logp_grad, before the first product: the rows padded, and what a row's dz is made of but for its listed tokens, -p (G + gH (log p + H)) / T.
-__global__ __launch_bounds__(256) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
-                                                            const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
-                                                            float temperature, RowTerms* __restrict__ terms, uint16_t* __restrict__ panel,
-                                                            int64_t lda) {
+// ll_logp_grad, before the first product: the rows padded, what a row's dz is made of, -p (G + gH (log p + H)) / T and g / T for a listed token,
+// and the listed tokens' whole dz.  Those are added up here, in fp32, and rounded once: of a likely token the two parts cancel, and the rounding
+// of p alone would be large beside their sum.
+__global__ __launch_bounds__(1024) void ll_logp_terms_kernel(const ListArgs p, const float* __restrict__ lse, const float* __restrict__ entropy,
+                                                             const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
+                                                             float temperature, RowTerms* __restrict__ terms, float2* __restrict__ list,
+                                                             uint16_t* __restrict__ panel, int64_t lda) {
+  __shared__ float z[LIST_MAX];
   pad_row(p.rows, blockIdx.x, p.d, panel, lda);
-  const int row = blockIdx.x, lane = threadIdx.x;
+  list_logits(p, blockIdx.x, z);
+  const int row = blockIdx.x, lane = threadIdx.x, k = p.k;
   if (lane >= 64) return;
-  const int64_t e = (int64_t)row * p.k + lane;
-  const int id = lane < p.k ? p.ids[e] : -1;
-  const GradTerms r = grad_terms(id >= 0 && id < p.V ? g_logp[e] : 0.f, lse[row], g_entropy != nullptr ? g_entropy[row] : 0.f,
-                                 entropy != nullptr ? entropy[row] : 0.f, 1.f / temperature);
+  const int64_t e = (int64_t)row * k + lane;
+  const int id = lane < k ? p.ids[e] : -1;
+  const bool valid = id >= 0 && id < p.V;
+  float g = valid ? g_logp[e] : 0.f;
+  const float inv_t = 1.f / temperature;
+  const GradTerms r = grad_terms(g, lse[row], g_entropy != nullptr ? g_entropy[row] : 0.f, entropy != nullptr ? entropy[row] : 0.f, inv_t);
+  const float l = fmaf(lane < k ? z[lane] : 0.f, p.to_log2, -r.lse2);
+  const bool first = gather_same(id, valid, k, lane, g);
   if (lane == 0) terms[row] = {r.lse2, r.a, r.b, r.live ? 1.f : 0.f};
+  if (lane < k) list[e] = make_float2(fmaf(g, inv_t, __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a)), __int_as_float(r.live && first ? id : -1));
+}
+// And behind it: the listed tokens' dz to their places.
+__global__ __launch_bounds__(256) void ll_learn_put_list_kernel(const float2* __restrict__ list, int64_t entries, int k, uint16_t* __restrict__ P,
+                                                                int64_t ldp) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= entries) return;
+  const float2 entry = list[e];
+  const int id = __float_as_int(entry.y);
+  if (id >= 0) P[e / k * ldp + place_in_p(id)] = (uint16_t)pack_bf16(entry.x, 0.f);
 }
 
-// The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)  LIST,
-// ll_logp_grad: and g / T times W's row of every listed token, in fp32.
-template <bool LIST>
-__global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, const ListArgs p,
-                                                            const RowTerms* __restrict__ terms, const float* __restrict__ g_logp, float inv_t,
-                                                            uint16_t* __restrict__ out) {
-  __shared__ float share[LIST ? LIST_MAX : 1];
-  __shared__ int id_of[LIST ? LIST_MAX : 1];
+// The slices joined, in order; a row that takes no part gets zeros whatever W holds.  (Eight slices' loads in flight at a time.)
+__global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restrict__ part, int splits, int rows, int d,
+                                                            const RowTerms* __restrict__ terms, uint16_t* __restrict__ out) {
   const int64_t row = blockIdx.y;
-  const int d = p.d, c = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (LIST) {
-    if ((int)threadIdx.x < p.k) {
-      const int64_t e = row * p.k + threadIdx.x;
-      const int id = p.ids[e];
-      id_of[threadIdx.x] = id >= 0 && id < p.V ? id : -1;
-      share[threadIdx.x] = g_logp[e] * inv_t;
-    }
-    __syncthreads();
-  }
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= d) return;
   const float f = terms[row].factor;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -235,18 +239,6 @@ __global__ __launch_bounds__(256) void ll_learn_join_kernel(const float* __restr
       s.w += x.w;
     }
     s = make_float4(f * s.x, f * s.y, f * s.z, f * s.w);
-    if (LIST) {
-#pragma unroll 4
-      for (int i = 0; i < p.k; ++i) {
-        const int id = id_of[i];
-        const uint2 w = *reinterpret_cast<const uint2*>(p.W + (int64_t)max(id, 0) * d + c);
-        const float by = id >= 0 ? share[i] : 0.f;
-        s.x += id >= 0 ? by * bf16_lo(w.x) : 0.f;
-        s.y += id >= 0 ? by * bf16_hi(w.x) : 0.f;
-        s.z += id >= 0 ? by * bf16_lo(w.y) : 0.f;
-        s.w += id >= 0 ? by * bf16_hi(w.y) : 0.f;
-      }
-    }
   }
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
@@ -378,7 +370,7 @@ struct LearnPlan {
   int pass_rows, tiles, splits, row_tiles, block_rows, row_blocks;   // row_tiles: of 16 rows a wavefront
   int col_blocks, back_splits;
   int64_t lda, ldp;
-  size_t stats, z, ref, panel, terms, moved, P, part, total;
+  size_t stats, z, ref, panel, terms, list, moved, P, part, total;
 };
 
 // Tiles of 16 rows a wavefront (64 rows a workgroup each): the fewest that hold all rows, else what costs least.  A row block costs 0.47,
@@ -409,8 +401,8 @@ struct FewShape {
   int rows, nc, groups, threads, streams;
 };
 // A gradient: up to four rows (two above d = 8192, what the registers hold).  Whole calls, us, so | in two products, ll_distill: d = 256, V =
-// 150 000, 1 row 24 | 56, 4 rows 39 | 56; 1608, 50257: 35 | 76, 49 | 77; 2560, 151936: 139 | 275, 192 | 279; 4096, 128256: 179 | 372, 186 | 374;
-// 8192, 128256: 351 | 760, 363 | 761; 16384, 60000, 1 row 339 | 706.  (Eight rows: 60 | 56, 79 | 79, 360 | 284, 319 | 375 and, in too many registers,
+// 150 000, 1 row 24 | 56, 4 rows 39 | 56; 1608, 50257: 35 | 76, 49 | 77; 2560, 151936: 136 | 275, 192 | 279; 4096, 128256: 176 | 372, 186 | 374;
+// 8192, 128256: 341 | 760, 363 | 761; 16384, 60000, 1 row 336 | 706.  (Eight rows: 60 | 56, 79 | 79, 360 | 284, 319 | 375 and, in too many registers,
 // 851 | 755.)  Statistics alone: up to eight where a row of W fills the workgroup.  ll_logp, 4 rows and 8: d = 256 23 | 27, 34 | 27; 2560 137 | 145,
 // 185 | 147; 4096 176 | 202, 178 | 205; 8192 342 | 436, 346 | 431.
 FewShape few_shape(const ll_shape* s, Needs needs) {
@@ -487,7 +479,8 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     l.terms = take(rows * sizeof(RowTerms));
     l.moved = take(rows * l.tiles * sizeof(float));
     l.P = take(rows * l.ldp * 2);
-    l.part = take(rows * l.back_splits * s->d * sizeof(float));
+    l.part = take(l.back_splits > 1 ? rows * l.back_splits * s->d * sizeof(float) : 0);
+    l.list = take(rows * k * sizeof(float2));
   }
   l.total = off;
   return l;
@@ -587,8 +580,8 @@ struct Pass {
     return LL_OK;
   }
 
-  // P to the gradient of the rows; g_logp: and of the listed tokens
-  int back(const int32_t* ids, const float* g_logp, float inv_t, uint16_t* out) const {
+  // P to the gradient of the rows
+  int back(uint16_t* out) const {
     LearnBackArgs p = {};
     p.A = at<uint16_t>(ws, l.P);
     p.W = W;
@@ -601,7 +594,7 @@ struct Pass {
     p.splits = l.back_splits;
     p.row_blocks = (n + l.block_rows - 1) / l.block_rows;
     p.col_blocks = l.col_blocks;
-    p.out = g_logp == nullptr && p.splits == 1 ? out : nullptr;
+    p.out = p.splits == 1 ? out : nullptr;
     p.terms = at<RowTerms>(ws, l.terms);
     const size_t lds = LEARN_LDS;
     const LearnBackKernel kernel = learn_back_kernel(past_caches(), l.row_tiles);
@@ -610,8 +603,8 @@ struct Pass {
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
     if (p.out != nullptr) return LL_OK;
-    hipLaunchKernelGGL(g_logp != nullptr ? ll_learn_join_kernel<true> : ll_learn_join_kernel<false>, dim3((shape->d + 1023) / 1024, n), dim3(256), 0,
-                       stream, p.part, p.splits, n, list(ids), at<RowTerms>(ws, l.terms), g_logp, inv_t, out);
+    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 1023) / 1024, n), dim3(256), 0, stream, p.part, p.splits, n, shape->d,
+                       at<RowTerms>(ws, l.terms), out);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   }
@@ -690,12 +683,16 @@ int ll_logp_grad(const ll_shape* shape, void* workspace, size_t workspace_bytes,
       j.out = (uint16_t*)out_grad;
       return p.few_join<false>(j);
     }
-    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids + r0 * k), lse + r0,
+    hipLaunchKernelGGL(ll_logp_terms_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids + r0 * k), lse + r0,
                        entropy != nullptr ? entropy + r0 : nullptr, g_logp + r0 * k, g_entropy != nullptr ? g_entropy + r0 : nullptr, temperature,
-                       at<RowTerms>(workspace, l.terms), p.panel(), l.lda);
+                       at<RowTerms>(workspace, l.terms), at<float2>(workspace, l.list), p.panel(), l.lda);
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(p.logits<GRAD>());
-    return p.back(ids + r0 * k, g_logp + r0 * k, 1.f / temperature, (uint16_t*)out_grad + r0 * shape->d);
+    const int64_t entries = (int64_t)p.n * k;
+    hipLaunchKernelGGL(ll_learn_put_list_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, p.stream, at<float2>(workspace, l.list),
+                       entries, k, at<uint16_t>(workspace, l.P), l.ldp);
+    LL_HIP_CHECK(hipGetLastError());
+    return p.back((uint16_t*)out_grad + r0 * shape->d);
   });
 }
 
@@ -742,7 +739,7 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
                        grad ? at<uint16_t>(workspace, l.P) : nullptr, l.ldp);
     LL_HIP_CHECK(hipGetLastError());
     if (!grad) return LL_OK;
-    return p.back(teacher_ids + r0 * k, nullptr, 0.f, (uint16_t*)out_grad + r0 * shape->d);
+    return p.back((uint16_t*)out_grad + r0 * shape->d);
   });
 }
 

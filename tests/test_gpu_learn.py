@@ -12,11 +12,12 @@ DEV = "cuda:0"
 INT_MIN, INT_MAX = -2 ** 31, 2 ** 31 - 1
 
 # (N, d, V, k): one of everything, less than a tile of it, ragged in each direction, more rows than a pass, more ids than a lane has; up
-# to eight rows of every width that they are dealt by
+# to eight rows of every width that they are dealt by; the gradient's product in one slice
 SIZES = [(1, 8, 1, 1), (1, 64, 5, 2), (3, 72, 257, 3), (64, 256, 4096, 5), (130, 328, 1000, 20), (257, 128, 3001, 64), (300, 1608, 2050, 7),
          (2100, 64, 777, 2), (520, 264, 300, 32), (1, 4096, 33000, 10), (33, 2560, 20000, 10), (17, 200, 70000, 4), (16, 8192, 1500, 1),
          (2, 1000, 3000, 5), (4, 1024, 900, 8), (5, 2048, 700, 3), (8, 4096, 600, 64), (4, 8192, 1000, 4), (3, 5120, 2000, 7), (2, 16384, 500, 2),
-         (6, 512, 9000, 10), (7, 2504, 5001, 6), (8, 4104, 300, 3), (3, 8200, 400, 2), (1, 16392, 300, 3), (2, 8, 70000, 33)]
+         (6, 512, 9000, 10), (7, 2504, 5001, 6), (8, 4104, 300, 3), (3, 8200, 400, 2), (1, 16392, 300, 3), (2, 8, 70000, 33),
+         (20, 72, 60, 3), (600, 520, 60, 5), (2048, 8192, 300, 2)]
 
 
 def inputs(N, d, V, k, spread=8.0, seed=0):
