@@ -19,11 +19,6 @@ namespace {
 
 constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 
-template <int OFF>
-__device__ __forceinline__ float lane_xor(float x) {
-  return __uint_as_float(with_lane_xor<OFF>(__float_as_uint(x), [](uint32_t, uint32_t b) { return b; }));
-}
-
 // v[0 .. M): values of every lane.  Returns one sum over the wavefront a lane, of value (lane >> (6 - log2 M)).
 template <int M, int OFF = 32>
 __device__ __forceinline__ float sum_across(float (&v)[M > 0 ? M : 1]) {
