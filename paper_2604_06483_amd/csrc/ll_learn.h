@@ -15,7 +15,7 @@ constexpr float LN2 = 0.6931471805599453f;
 
 // Statistics only; and the exponentials; dz where the statistics are known.
 enum LearnWhat { STATS, EXPS, GRAD };
-constexpr float MASKED = -1e30f;   // an exponent that stands for a column past the vocabulary: 2^l is 0, and l no infinity for what multiplies it
+constexpr float MASKED = -1024.f;  // an exponent that stands for a column past the vocabulary: 2^l is 0, and l times whatever a gradient is no infinity
 
 struct RowTerms {   // of a row's dz: with l = z log2 e - lse2, dz = 2^l (a + b l); its gradient is `factor` times P's product, zeros where that is 0
   float lse2, a, b, factor;

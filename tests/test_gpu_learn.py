@@ -148,6 +148,23 @@ def test_lists_far_below_the_most_likely_token(N, d, V, gap):
     check_logp(a, W, ids, g, 1.0)
 
 
+@pytest.mark.parametrize("N,d,V,k", [(1, 256, 300, 2), (4, 1024, 777, 3), (3, 5120, 130, 2), (40, 136, 900, 5), (300, 264, 1001, 3)])
+@pytest.mark.parametrize("power", [-60, 40, 100])
+def test_gradients_of_any_size(N, d, V, k, power):
+    """The gradient is linear in what it starts from, and a power of two changes no rounding: the same bits, but for the exponent.  (The
+    columns past the vocabulary meet it too.)"""
+    say(f"gradients times 2^{power} N={N} d={d} V={V}")
+    a, W, ids, g = inputs(N, d, V, k)
+    ca, cW, cids = a.to(DEV), W.to(DEV), ids.to(DEV)
+    _, lse, ent = LL.ll_logp(ca, cW, cids)
+    g_logp, g_ent = torch.randn((N, k), generator=g).to(DEV), torch.randn((N,), generator=g).to(DEV)
+    plain = LL.ll_logp_grad(ca, cW, cids, lse, ent, g_logp, g_ent)
+    scaled = LL.ll_logp_grad(ca, cW, cids, lse, ent, g_logp * 2.0 ** power, g_ent * 2.0 ** power)
+    assert torch.isfinite(plain).all()
+    # (what underflows on its way has no influence on a value of this size)
+    torch.testing.assert_close(scaled.double(), plain.double() * 2.0 ** power, rtol=0, atol=2.0 ** power * 1e-12)
+
+
 def test_nothing_of_a_masked_row_matters():
     say("masked rows of NaN and infinities")
     N, d, V, k = 40, 136, 900, 5
