@@ -36,7 +36,7 @@ class _BlockNorm(torch.autograd.Function):
         d_hidden, d_y, d_gate, d_gamma_y, d_gamma = LL.ll_block_norm_grad(hidden, y, gamma, ctx.eps, g_hidden, g_normed, gate=gate,
                                                                           scale=ctx.scale, gamma_y=gamma_y)
         like = lambda g, p: None if p is None else g.to(p.dtype)
-        return d_hidden, d_y, like(d_gamma, gamma), like(d_gate, gate), like(d_gamma_y, gamma_y), None, None
+        return d_hidden, d_y.reshape(y.shape), like(d_gamma, gamma), like(d_gate, gate), like(d_gamma_y, gamma_y), None, None
 
 
 class _TokenLogp(torch.autograd.Function):

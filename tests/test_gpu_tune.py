@@ -40,6 +40,25 @@ def test_autograd_passes_on_what_the_calls_return():
     assert torch.equal(loss, weight * want) and torch.equal(rows.grad, grad)
 
 
+def test_rows_in_more_than_one_dimension():
+    """As the calls take them: the block's output as a matrix beside hidden states with a batch in front."""
+    say("autograd, batches")
+    B, T, d, V, k = 2, 9, 64, 300, 3
+    g = torch.Generator(device=DEV).manual_seed(8)
+    normal = lambda *s: torch.randn(s, generator=g, device=DEV).to(torch.bfloat16)
+    gamma, W = normal(d), normal(V, d)
+    ids = torch.randint(0, V, (B * T, k), generator=g, device=DEV, dtype=torch.int32)
+    scores = normal(B * T, k).float()
+    h, y = normal(B, T, d).requires_grad_(), normal(B * T, d).requires_grad_()
+    flat = [t.detach().reshape(B * T, d).clone().requires_grad_() for t in (h, y)]
+    for a, b in ((h, y), flat):
+        n = tune.block_norm(a, b, gamma, 1e-5)[1]
+        logp, entropy = tune.token_logp(n, W, ids)
+        (tune.distill(n, W, ids, scores).sum() + logp.sum() + entropy.sum()).backward()
+    assert h.grad.shape == h.shape and y.grad.shape == y.shape
+    assert torch.equal(h.grad.reshape(B * T, d), flat[0].grad) and torch.equal(y.grad, flat[1].grad)
+
+
 def test_a_translator_learns():
     """The inner rows' raw lens does not know the last layer's token; after some steps it does, and the loss has fallen by half."""
     say("translator")
