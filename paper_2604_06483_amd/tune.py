@@ -16,6 +16,7 @@ from __future__ import annotations
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as LL
 
@@ -29,6 +30,7 @@ class _BlockNorm(torch.autograd.Function):
         return LL.ll_block_norm(hidden, y, gamma, eps, gate=gate, scale=scale, gamma_y=gamma_y)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_hidden, g_normed):
         hidden, y, gamma, gate, gamma_y = ctx.saved_tensors
         g_hidden = None if g_hidden is None else g_hidden.contiguous()
@@ -49,6 +51,7 @@ class _TokenLogp(torch.autograd.Function):
         return logp, entropy
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_logp, g_entropy):
         rows, W_U, ids, lse, entropy = ctx.saved_tensors
         g_logp = torch.zeros(ids.shape, device=rows.device) if g_logp is None else g_logp.contiguous()
@@ -65,6 +68,7 @@ class _Distill(torch.autograd.Function):
         return loss if weight is None else weight * loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_loss):
         (grad,) = ctx.saved_tensors
         return (g_loss.reshape(grad.shape[:-1] + (1,)) * grad).to(grad.dtype), None, None, None, None, None

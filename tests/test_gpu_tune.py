@@ -59,6 +59,22 @@ def test_rows_in_more_than_one_dimension():
     assert torch.equal(h.grad.reshape(B * T, d), flat[0].grad) and torch.equal(y.grad, flat[1].grad)
 
 
+def test_a_second_derivative_is_refused():
+    """The gradients are the library's, and it has none of theirs: an error, and no silent zeros."""
+    say("autograd, twice")
+    N, d, V, k = 12, 64, 200, 3
+    g = torch.Generator(device=DEV).manual_seed(9)
+    rows, y = (torch.randn((N, d), generator=g, device=DEV).to(torch.bfloat16).requires_grad_() for _ in range(2))
+    gamma, W = (torch.randn(s, generator=g, device=DEV).to(torch.bfloat16) for s in ((d,), (V, d)))
+    ids = torch.randint(0, V, (N, k), generator=g, device=DEV, dtype=torch.int32)
+    scores = torch.randn((N, k), generator=g, device=DEV)
+    factor = torch.ones((), device=DEV, requires_grad=True)          # so that the gradient depends on something that wants one
+    for value in (tune.block_norm(rows, y, gamma, 1e-5)[1].float().sum(), tune.token_logp(rows, W, ids)[0].sum(), tune.distill(rows, W, ids, scores).sum()):
+        (grad,) = torch.autograd.grad(factor * value, rows, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            grad.float().sum().backward()
+
+
 def test_a_translator_learns():
     """The inner rows' raw lens does not know the last layer's token; after some steps it does, and the loss has fallen by half."""
     say("translator")
