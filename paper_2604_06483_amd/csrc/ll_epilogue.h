@@ -620,7 +620,7 @@ __device__ __forceinline__ void epilogue_store(const GemmArgs& p, const RowState
 template <int KR, bool BIAS = false, bool SHORT = false>
 struct TopKEpilogue {   // a5..a7: softmax statistics, k best logits, target logit (BIAS: Eq. 1's b added to every logit first)
   using State = RowState<KR>;
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false, PAST_CACHES = false;
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = false, PAST_CACHES = false, HALVES_APART = false;
   static constexpr int ROWS = BN, ROW_TILES = 4;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ void init(State& st, const GemmArgs& p, int my_row, int split) {

@@ -937,7 +937,7 @@ __device__ __forceinline__ bool sweep_is_long(const float* sampled, const float*
 template <int KS, bool GENERAL, bool OWN>
 struct AnySweepEpilogue {
   using State = SweepState<KS, GENERAL>;
-  static constexpr bool RELOAD_FRAGMENTS = true, OWN_U = OWN, BACK = false, PAST_CACHES = false;
+  static constexpr bool RELOAD_FRAGMENTS = true, OWN_U = OWN, BACK = false, PAST_CACHES = false, HALVES_APART = false;
   static constexpr int ROWS = OWN_U ? SWEEP_OWN_ROWS : BN, ROW_TILES = 4;
   static __device__ __forceinline__ bool skip(const GemmArgs& p) {
     if (OWN_U) {

@@ -68,6 +68,10 @@ namespace {
 //
 // EPI::PAST_CACHES: W's loads go past the caches, where one row block reads a W that they cannot hold.
 //
+// EPI::HALVES_APART: row blocks that read one W tile side by side ask for its halves in opposite orders, so that either fetches what the other
+// finds in the L2 a moment later, and twice as many of W's lines are on their way (348 x 5120 x 151936 and back 1033 -> 1007 us, 1500 x 2560 x 151936
+// and back 1697 -> 1678, 1500 x 4096 x 128256 1106 -> 1100).
+//
 // EPI::BACK: the product backwards, C [rows, d] = A W with A [rows, V] (the gradient of the logits) and K over the vocabulary.  A is loaded
 // as above.  A stage of W is 64 vocabulary rows by the tile's 256 columns, [64 rows][512 B] in its slot, and K goes down its columns:
 // the fragments are read with ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows, two of them a fragment.  A
@@ -199,6 +203,9 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   const int a_last = p.last_row - rb * ROWS;                          // what rows past the end are read from
   constexpr int IMM_BIAS = 3072;                                      // largest immediate, segment 7
 
+  // (every second row block sends segments 4 to 7 of a W tile before 0 to 3, to the same places)
+  const int turn = EPI::HALVES_APART ? (rb & 1) * 4 : 0;
+
   // Per-lane byte offsets of the 8 segments, fixed for the whole sweep (W: per vocabulary tile,
   // because the last tile clamps its rows to V-1): one load is one instruction.
   unsigned a_off[8], w_off[8];
@@ -224,7 +231,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
       const int w_last = p.V - 1 - tile * DK;
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const int row = 16 * wave + 2 * s + (lane >> 5);
+        const int row = 16 * wave + 2 * (s ^ turn) + (lane >> 5);
         const int chunk = ((lane & 31) ^ (2 * (row & 7))) + tile0 * (BM / 8);
         w_off[s] = (unsigned)(min(row, w_last) * d + min(chunk * 8, d - 8)) * 2u + (7168u - 1024u * s);
       }
@@ -236,7 +243,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
     const int row = 64 * wave + (l >> 3), koff0 = ((l & 7) ^ (l >> 4)) * 8;
 #pragma unroll
     for (int s = 0; s < 8; ++s)
-      w_off[s] = (unsigned)(min(row + 8 * s, w_last) * d + ((s & 1) ? koff0 ^ 32 : koff0)) * 2u + (7168u - 1024u * s);
+      w_off[s] = (unsigned)(min(row + 8 * (s ^ turn), w_last) * d + ((s & 1) ? koff0 ^ 32 : koff0)) * 2u + (7168u - 1024u * s);
     if (TAIL && KT == 1) step_back();
   };
   // TAIL: zeros into the chunks past the row's end of this wavefront's rows of the W tile at LDS offset `tile_off`
@@ -300,6 +307,8 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
 #define LL_DMA_W(S) load_to_lds_16<((S) - 4) * 1024, EPI::PAST_CACHES>(w_base, w_off[S])
 #define LL_DMA_A(S) if constexpr ((S) < A_LOADS) load_to_lds_16<((S) - 4) * 1024>(a_base, a_off[S])
 #define LL_DMA_TILE(DMA) DMA(0); DMA(1); DMA(2); DMA(3); DMA(4); DMA(5); DMA(6); DMA(7)
+  const auto w_base_first = [&]() { set_lds_dma_base(w_lds + 1024 * turn); };
+  const auto w_base_second = [&]() { set_lds_dma_base(w_lds - 1024 * turn); };
 
   // --- MFMA fragment map (v_mfma_f32_16x16x32_bf16): lane reads row (lane % 16) of each 16-row
   // group; of the two K = 32 halves of a stage, half hk is the logical 16-byte chunks
@@ -325,19 +334,23 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   if constexpr (SHORT) EPI::settle(st);
 
   // prologue: W0 A0 W1 A1 and the first half of W2 in flight; stage 0 landed
-  set_lds_dma_base(w_lds);
-  LL_DMA_TILE(LL_DMA_W);
+  w_base_first();
+  LL_DMA_W(0); LL_DMA_W(1); LL_DMA_W(2); LL_DMA_W(3);
+  if (EPI::HALVES_APART) w_base_second();
+  LL_DMA_W(4); LL_DMA_W(5); LL_DMA_W(6); LL_DMA_W(7);
   advance_w();
   set_lds_dma_base(a_lds);
   LL_DMA_TILE(LL_DMA_A);
   advance_a();
-  set_lds_dma_base(w_lds);
-  LL_DMA_TILE(LL_DMA_W);
+  w_base_first();
+  LL_DMA_W(0); LL_DMA_W(1); LL_DMA_W(2); LL_DMA_W(3);
+  if (EPI::HALVES_APART) w_base_second();
+  LL_DMA_W(4); LL_DMA_W(5); LL_DMA_W(6); LL_DMA_W(7);
   advance_w();
   set_lds_dma_base(a_lds);
   LL_DMA_TILE(LL_DMA_A);
   advance_a();
-  set_lds_dma_base(w_lds);
+  w_base_first();
   LL_DMA_W(0); LL_DMA_W(1); LL_DMA_W(2); LL_DMA_W(3);
   __builtin_amdgcn_s_waitcnt(waitcnt_imm(LOADS_PER_TILE + A_LOADS + 4, 15));   // W0 and A0 landed
   if (TAIL && KT == 1) zero_tail(0);
@@ -436,7 +449,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   }
   // (hooks: what goes behind pair P of the slice, besides a fragment read)
 #define LL_HOOK_S0(P)                                \
-  if (P == 1) set_lds_dma_base(w_lds);               \
+  if (P == 1) w_base_second();                       \
   if (P == 7) LL_DMA_W(4);                           \
   if (P == 9) LL_DMA_W(5);                           \
   if (P == 11) LL_DMA_W(6);                          \
@@ -457,7 +470,7 @@ __device__ __forceinline__ void lens_gemm_dma(const GemmArgs& p, unsigned char* 
   if (P == 13) LL_DMA_A(7)
 #define LL_HOOK_S3(P)   /* (the A stream moves on here, behind the barrier, not in the last gap before the wait) */ \
   if (P == 1) advance_a();                           \
-  if (P == 7) set_lds_dma_base(w_lds);               \
+  if (P == 7) w_base_first();                        \
   if (P == 9) LL_DMA_W(0);                           \
   if (P == 11) {                                     \
     LL_DMA_W(1);                                     \

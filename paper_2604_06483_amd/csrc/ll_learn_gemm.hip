@@ -22,7 +22,7 @@ struct LearnEpilogue {
     float ref[RT], s[RT], t[RT];
     RowTerms terms[WHAT == GRAD ? RT : 1];
   };
-  static constexpr bool RELOAD_FRAGMENTS = WHAT == STATS && RT == 4, OWN_U = false, BACK = false, PAST_CACHES = PAST;
+  static constexpr bool RELOAD_FRAGMENTS = WHAT == STATS && RT == 4, OWN_U = false, BACK = false, PAST_CACHES = PAST, HALVES_APART = true;
   static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
   static constexpr float MOST = WHAT == EXPS ? 0x1p60f : 0x1p16f;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
@@ -136,7 +136,7 @@ struct BackEpilogue {
   struct State {
     int split;
   };
-  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = true, PAST_CACHES = PAST;
+  static constexpr bool RELOAD_FRAGMENTS = false, OWN_U = false, BACK = true, PAST_CACHES = PAST, HALVES_APART = true;
   static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ void init(State& st, const GemmArgs&, int, int split) { st.split = split; }
