@@ -76,7 +76,7 @@ namespace {
 // as above.  A stage of W is 64 vocabulary rows by the tile's 256 columns, [64 rows][512 B] in its slot, and K goes down its columns:
 // the fragments are read with ds_read_b64_tr_b16, which hands each of 16 lanes one column of four rows, two of them a fragment.  A
 // lane group's eight K are rows 4 g .. + 3 and 16 + 4 g .. + 3 of a half's 32, and A's columns stand in that order within every 32
-// (place_in_p in ll_learn.hip), so that both halves of a read are whole rows apart.  The 32-byte pieces of a row are XOR-swizzled with the
+// (place_in_p in ll_learn.h), so that both halves of a read are whole rows apart.  The 32-byte pieces of a row are XOR-swizzled with the
 // row's last three bits: the eight rows that half a wavefront reads from, all at one multiple of 512 bytes, then lie in different banks.
 // A workgroup has one tile, of 256 rows by 256 columns, and one slice of the vocabulary.  Rows of W past the last are the last one's
 // again, where A holds zeros; columns past the last chunk are its own again, and are not stored.
