@@ -146,10 +146,18 @@ def _stream(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
-def _rows(t, d):
-    """t as [rows, d]; a matrix of that width as it is (a reshape of it would be the same tensor in another object)."""
+def _rows(t, d, stream=None):
+    """t as [rows, d]; a matrix of that width as it is (a reshape of it would be the same tensor in another object).
+
+    A batch whose strides do not allow that is copied, and the copy has to be the work and the memory of the stream that the call goes to:
+    made on another, the kernel would not wait for it, and its memory could be handed out again while the kernel still reads it."""
     size = t.shape
-    return t if len(size) == 2 and size[1] == d else t.reshape(-1, d)
+    if len(size) == 2 and size[1] == d:
+        return t
+    if stream is None or t.is_contiguous():
+        return t.reshape(-1, d)
+    with torch.cuda.stream(stream):
+        return t.reshape(-1, d)
 
 
 def _scratch(nbytes, device, stream):
@@ -181,7 +189,7 @@ def ll_project(hidden, gamma, W_U, eps, k, target_ids=None, *, workspace=None, s
     plus the three phase times in ms when timed=True (that variant synchronises the stream).
     """
     d = hidden.shape[-1]
-    h2 = _rows(hidden, d)
+    h2 = _rows(hidden, d, stream)
     N = h2.shape[0]
     V = W_U.shape[0]
     _check(h2, torch.bfloat16, "hidden")
@@ -235,7 +243,7 @@ def ll_project_static(hidden, gamma, W_U, eps, k, target_ids=None, *, stream=Non
     call allocates nothing (pass `out` to keep this wrapper from allocating the result tensors).  Calls that may
     overlap on one GPU race on that buffer.  Same results as ll_project."""
     d = hidden.shape[-1]
-    h2 = _rows(hidden, d)
+    h2 = _rows(hidden, d, stream)
     N = h2.shape[0]
     V = W_U.shape[0]
     _check(h2, torch.bfloat16, "hidden")
@@ -280,7 +288,7 @@ def ll_steer_inject(hidden, gamma, eps, v, alpha, *, stream=None, out=None):
     """bf16(RMSNorm(hidden) + alpha v), same shape as hidden (paper Eq. 3, post-norm)."""
     size = hidden.shape
     d = size[-1]
-    h2 = hidden if len(size) == 2 else hidden.reshape(-1, d)
+    h2 = hidden if len(size) == 2 else _rows(hidden, d, stream)
     _check(h2, _BF16, "hidden")
     _check(gamma, _BF16, "gamma", (d,))
     _check(v, _F32, "v", (d,))
@@ -310,7 +318,7 @@ def ll_steer_sweep(hidden, gamma, W_U, eps, v, alphas, target_ids=None, *, k=Non
     with k given (1..LL_SWEEP_KMAX, through ll_steer_sweep_topk) the first two are [A,N,k] lists.
     """
     d = hidden.shape[-1]
-    h2 = _rows(hidden, d)
+    h2 = _rows(hidden, d, stream)
     N = h2.shape[0]
     V = W_U.shape[0]
     A = len(alphas)
@@ -349,7 +357,7 @@ def ll_steer_inject_raw(hidden, v, alpha, layer_scale=1.0, clip_ratio=0.0, *, st
     in-model injection with its two safeguards); same shape as hidden."""
     size = hidden.shape
     d = size[-1]
-    h2 = hidden if len(size) == 2 else hidden.reshape(-1, d)
+    h2 = hidden if len(size) == 2 else _rows(hidden, d, stream)
     _check(h2, _BF16, "hidden")
     _check(v, _F32, "v", (d,))
     o = torch.empty_like(h2) if out is None else _rows(out, d)
@@ -415,7 +423,7 @@ def ll_block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None, 
     Returns (x, gamma x / rms(x)), both bf16 in hidden's shape (`out`: two tensors to hold them).
     """
     d = hidden.shape[-1]
-    h2, y2 = _rows(hidden, d), _rows(y, d)
+    h2, y2 = _rows(hidden, d, stream), _rows(y, d, stream)
     N = h2.shape[0]
     _check(h2, _BF16, "hidden")
     _check(y2, _BF16, "y", (N, d))
@@ -448,8 +456,8 @@ def ll_block_norm_grad(hidden, y, gamma, eps, g_hidden, g_normed, *, gate=None, 
     fp32 [d] (d_gamma_y None without gamma_y).
     """
     size, d = hidden.shape, hidden.shape[-1]
-    h2, y2, gn = _rows(hidden, d), _rows(y, d), _rows(g_normed, d)
-    gh = None if g_hidden is None else _rows(g_hidden, d)
+    h2, y2, gn = _rows(hidden, d, stream), _rows(y, d, stream), _rows(g_normed, d, stream)
+    gh = None if g_hidden is None else _rows(g_hidden, d, stream)
     N = h2.shape[0]
     _check(h2, _BF16, "hidden")
     _check(y2, _BF16, "y", (N, d))
@@ -486,15 +494,15 @@ def ll_distill_workspace_bytes(N: int, d: int, V: int, k: int) -> int:
     return int(lib().ll_distill_workspace_bytes(ll_shape(N, d, V), k))
 
 
-def _lens_rows(rows, W_U, ids, name):
+def _lens_rows(rows, W_U, ids, name, stream):
     """Rows as [N, d], the list as [N, k], and (N, d, V, k)."""
     d = rows.shape[-1]
-    r2 = _rows(rows, d)
+    r2 = _rows(rows, d, stream)
     N, V = r2.shape[0], W_U.shape[0]
     _check(r2, _BF16, "rows")
     _check(W_U, _BF16, "W_U", (V, d))
     k = ids.shape[-1] if ids.dim() > 1 else 1
-    i2 = ids if ids.dim() == 2 else ids.reshape(-1, k)
+    i2 = ids if ids.dim() == 2 else _rows(ids, k, stream)
     _check(i2, torch.int32, name, (N, k))
     return r2, i2, N, d, V, k
 
@@ -504,7 +512,7 @@ def ll_logp(rows, W_U, ids, *, temperature=1.0, workspace=None, stream=None):
 
     Returns (logp [N, k], logsumexp [N], entropy [N]), fp32.
     """
-    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids")
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids", stream)
     dev = rows.device
     logp, lse, ent = _empty((N, k), _F32, dev, stream), _empty((N,), _F32, dev, stream), _empty((N,), _F32, dev, stream)
     ws = _workspace(workspace, lambda: ll_logp_workspace_bytes(N, d, V, k), dev, stream)
@@ -520,8 +528,8 @@ def ll_logp_grad(rows, W_U, ids, lse, entropy, g_logp, g_entropy=None, *, temper
 
     Returns it in bf16 in the rows' shape.
     """
-    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids")
-    g2 = g_logp if g_logp.dim() == 2 else g_logp.reshape(-1, k)
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, ids, "ids", stream)
+    g2 = g_logp if g_logp.dim() == 2 else _rows(g_logp, k, stream)
     _check(g2, _F32, "g_logp", (N, k))
     _check(lse, _F32, "lse", (N,))
     for t, name in ((entropy, "entropy"), (g_entropy, "g_entropy")):
@@ -543,8 +551,8 @@ def ll_distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weigh
 
     Returns (loss [N] fp32, gradient of weight . loss in bf16 in the rows' shape, or None with grad=False).
     """
-    r2, i2, N, d, V, k = _lens_rows(rows, W_U, teacher_ids, "teacher_ids")
-    s2 = teacher_scores if teacher_scores.dim() == 2 else teacher_scores.reshape(-1, k)
+    r2, i2, N, d, V, k = _lens_rows(rows, W_U, teacher_ids, "teacher_ids", stream)
+    s2 = teacher_scores if teacher_scores.dim() == 2 else _rows(teacher_scores, k, stream)
     _check(s2, _F32, "teacher_scores", (N, k))
     if weight is not None:
         _check(weight, _F32, "weight", (N,))

@@ -1,0 +1,90 @@
+"""A batch whose strides do not make it rows is copied, and a call that goes to a stream of its own has its copies made there (no GPU needed)."""
+import contextlib
+
+import pytest
+import torch
+from torch.overrides import TorchFunctionMode
+
+from paper_2604_06483_amd import binding as LL
+
+B, T, d, V, k = 3, 4, 16, 20, 2
+BF16 = torch.bfloat16
+
+
+class Library:
+    """Every call succeeds, every workspace is small."""
+
+    def __getattr__(self, name):
+        return lambda *a: 256 if name.endswith("_bytes") else 0
+
+
+def across(*size, dtype=BF16):
+    """[B, T, ...] in the order of a [T, B, ...]: no rows without a copy."""
+    return torch.zeros((size[1], size[0], *size[2:]), dtype=dtype).transpose(0, 1)
+
+
+def vector(dtype=BF16):
+    return torch.zeros((d,), dtype=dtype)
+
+
+def weights():
+    return torch.zeros((V, d), dtype=BF16)
+
+
+def ids():
+    return across(B, T, k, dtype=torch.int32)
+
+
+def scores():
+    return across(B, T, k, dtype=torch.float32)
+
+
+def row():
+    return torch.zeros((B * T,))
+
+
+CALLS = {   # and how many of the inputs are such batches
+    "ll_project": (1, lambda s: LL.ll_project(across(B, T, d), vector(), weights(), 1e-5, k, stream=s)),
+    "ll_project_static": (1, lambda s: LL.ll_project_static(across(B, T, d), vector(), weights(), 1e-5, k, stream=s)),
+    "ll_steer_inject": (1, lambda s: LL.ll_steer_inject(across(B, T, d), vector(), 1e-5, vector(torch.float32), 1.0, stream=s)),
+    "ll_steer_inject_raw": (1, lambda s: LL.ll_steer_inject_raw(across(B, T, d), vector(torch.float32), 1.0, stream=s)),
+    "ll_steer_sweep": (1, lambda s: LL.ll_steer_sweep(across(B, T, d), vector(), weights(), 1e-5, vector(torch.float32), [1.0], stream=s)),
+    "ll_block_norm": (2, lambda s: LL.ll_block_norm(across(B, T, d), across(B, T, d), vector(), 1e-5, stream=s)),
+    "ll_block_norm_grad": (4, lambda s: LL.ll_block_norm_grad(*[across(B, T, d) for _ in range(2)], vector(), 1e-5,
+                                                              *[across(B, T, d) for _ in range(2)], stream=s)),
+    "ll_logp": (2, lambda s: LL.ll_logp(across(B, T, d), weights(), ids(), stream=s)),
+    "ll_logp_grad": (3, lambda s: LL.ll_logp_grad(across(B, T, d), weights(), ids(), row(), row(), scores(), stream=s)),
+    "ll_distill": (3, lambda s: LL.ll_distill(across(B, T, d), weights(), ids(), scores(), stream=s)),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("given", [True, False])
+def test_copies_are_made_on_the_calls_stream(monkeypatch, name, given):
+    there, mine, copies = [None], object(), []
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, there[0] = there[0], stream
+        yield
+        there[0] = before
+
+    class Copies(TorchFunctionMode):
+        def __torch_function__(self, func, types, args=(), kwargs=None):
+            out = func(*args, **(kwargs or {}))
+            if func is torch.Tensor.reshape and out.data_ptr() != args[0].data_ptr():
+                copies.append(there[0])
+            return out
+
+    plain = lambda size, dtype, device, stream: torch.empty(size, dtype=dtype)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(LL, "_lib", Library())
+    monkeypatch.setattr(LL, "_check", lambda *a, **kw: None)
+    monkeypatch.setattr(LL, "_stream", lambda s: 0)
+    monkeypatch.setattr(LL, "_scratch", lambda n, device, stream: torch.empty(256, dtype=torch.uint8))
+    monkeypatch.setattr(LL, "_empty", plain)
+    monkeypatch.setattr(LL, "_like", lambda t, stream: torch.empty_like(t))
+    count, call = CALLS[name]
+    with Copies():
+        call(mine if given else None)
+    assert copies == [mine if given else None] * count
