@@ -1,4 +1,4 @@
-"""A batch whose strides do not make it rows is copied, and a call that goes to a stream of its own has its copies made there (no GPU needed)."""
+"""What a call on a stream of its own makes, copies of batches that are no rows, results and workspaces, is that stream's (no GPU needed)."""
 import contextlib
 
 import pytest
@@ -88,3 +88,35 @@ def test_copies_are_made_on_the_calls_stream(monkeypatch, name, given):
     with Copies():
         call(mine if given else None)
     assert copies == [mine if given else None] * count
+
+
+MAKES = {n: call for n, (_, call) in CALLS.items()}
+MAKES["ll_steer_vector"] = lambda s: LL.ll_steer_vector(weights(), weights(), stream=s)
+
+
+@pytest.mark.parametrize("name", MAKES)
+def test_results_and_workspaces_are_memory_of_the_calls_stream(monkeypatch, name):
+    """Memory of the current stream's may still be read by what was queued there before it was freed."""
+    there, mine, current, made, kept = [None], object(), object(), [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, there[0] = there[0], stream
+        yield
+        there[0] = before
+
+    class Made(TorchFunctionMode):
+        def __torch_function__(self, func, types, args=(), kwargs=None):
+            if func in (torch.empty, torch.empty_like):
+                made.append(there[0])
+            return func(*args, **(kwargs or {}))
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept.append(s))
+    monkeypatch.setattr(LL, "_lib", Library())
+    monkeypatch.setattr(LL, "_check", lambda *a, **kw: None)
+    monkeypatch.setattr(LL, "_stream", lambda s: 0)
+    with Made():
+        MAKES[name](mine)
+    assert made and all(s is mine for s in made) and kept == [current] * len(made)
