@@ -64,14 +64,15 @@ class _Distill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, W_U, teacher_ids, teacher_scores, temperature, weight):
         loss, grad = LL.ll_distill(rows, W_U, teacher_ids, teacher_scores, temperature=temperature, weight=weight, grad=ctx.needs_input_grad[0])
-        ctx.save_for_backward(grad)
+        ctx.save_for_backward(grad, loss if ctx.needs_input_grad[5] else None)
         return loss if weight is None else weight * loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g_loss):
-        (grad,) = ctx.saved_tensors
-        return (g_loss.reshape(grad.shape[:-1] + (1,)) * grad).to(grad.dtype), None, None, None, None, None
+        grad, loss = ctx.saved_tensors
+        d_rows = None if grad is None else (g_loss.reshape(grad.shape[:-1] + (1,)) * grad).to(grad.dtype)
+        return d_rows, None, None, None, None, None if loss is None else g_loss * loss
 
 
 def block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None):
@@ -85,8 +86,8 @@ def token_logp(rows, W_U, ids, *, temperature=1.0):
 
 
 def distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weight=None):
-    """ll_distill, differentiable in the rows: weight times every row's loss.  The gradient is formed with the loss, in one call; give the
-    weights here (1 / N for a mean), and sum."""
+    """ll_distill, differentiable in the rows and the weight: weight times every row's loss.  The rows' gradient is formed with the loss, in one
+    call; give the weights here (1 / N for a mean), and sum."""
     return _Distill.apply(rows, W_U, teacher_ids, teacher_scores, temperature, weight)
 
 

@@ -1,0 +1,41 @@
+"""What autograd is told of the calls that learn through the lens, with the calls themselves in torch (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2604_06483_amd import tune
+
+N, d, V, k = 6, 8, 12, 3
+
+
+def plain_distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weight=None, grad=True):
+    with torch.enable_grad():
+        a = rows.detach().float().requires_grad_()
+        logp = torch.log_softmax(a @ W_U.detach().float().t() / temperature, 1)
+        log_t = torch.log_softmax(teacher_scores.detach() / temperature, 1)
+        loss = temperature ** 2 * (log_t.exp() * (log_t - logp.gather(1, teacher_ids.long()))).sum(1)
+        out = torch.autograd.grad((loss if weight is None else weight.detach() * loss).sum(), a)[0].to(rows.dtype) if grad else None
+    return loss.detach(), out
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    monkeypatch.setattr(tune.LL, "ll_distill", plain_distill)
+
+
+def inputs():
+    g = torch.Generator().manual_seed(3)
+    rows, W = (torch.randn(s, generator=g).to(torch.bfloat16) for s in ((N, d), (V, d)))
+    return rows, W, torch.randint(0, V, (N, k), generator=g, dtype=torch.int32), torch.randn((N, k), generator=g), torch.rand((N,), generator=g)
+
+
+@pytest.mark.parametrize("trained", [True, False])
+def test_the_weight_of_a_distillation_gets_its_gradient(calls, trained):
+    """It is what the row's loss is without it, whether or not the rows are trained as well."""
+    rows, W, ids, scores, weight = inputs()
+    rows.requires_grad_(trained)
+    weight.requires_grad_()
+    factor = torch.arange(1.0, N + 1)
+    (factor * tune.distill(rows, W, ids, scores, weight=weight)).sum().backward()
+    loss, grad = plain_distill(rows, W, ids, scores, weight=weight)
+    assert torch.equal(weight.grad, factor * loss)
+    assert torch.equal(rows.grad, (factor[:, None] * grad).to(torch.bfloat16)) if trained else rows.grad is None
