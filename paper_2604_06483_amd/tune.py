@@ -75,19 +75,29 @@ class _Distill(torch.autograd.Function):
         return d_rows, None, None, None, None, None if loss is None else g_loss * loss
 
 
+def _no_gradient(**tensors):
+    """What the library has no gradient of is refused where autograd would be asked for one: without it a training step would miss a term."""
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if t.requires_grad:
+                raise ValueError(f"{name} gets no gradient: pass it detached")
+
+
 def block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None):
     """ll_block_norm, differentiable in hidden, y, gamma, gate and gamma_y: (x, gamma x / rms(x))."""
     return _BlockNorm.apply(hidden, y, gamma, gate, gamma_y, eps, scale)
 
 
 def token_logp(rows, W_U, ids, *, temperature=1.0):
-    """ll_logp, differentiable in the rows: (log-probabilities of the listed tokens, entropy)."""
+    """ll_logp, differentiable in the rows: (log-probabilities of the listed tokens, entropy).  W_U gets no gradient: detached, or an error."""
+    _no_gradient(W_U=W_U)
     return _TokenLogp.apply(rows, W_U, ids, temperature)
 
 
 def distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weight=None):
     """ll_distill, differentiable in the rows and the weight: weight times every row's loss.  The rows' gradient is formed with the loss, in one
-    call; give the weights here (1 / N for a mean), and sum."""
+    call; give the weights here (1 / N for a mean), and sum.  W_U and the teacher get no gradient: detached, or an error."""
+    _no_gradient(W_U=W_U, teacher_scores=teacher_scores)
     return _Distill.apply(rows, W_U, teacher_ids, teacher_scores, temperature, weight)
 
 
@@ -125,7 +135,7 @@ class Fit:
 
 def fit(translator, hidden, last_hidden, W_U, *, k=20, temperature=1.0, steps=200, rate=1e-3):
     """Trains a translator on one layer's rows against the last layer's read-out of the same tokens."""
-    N = hidden.shape[0]
+    N, W_U = hidden.shape[0], W_U.detach()      # (the model's own: not trained)
     ids, scores = teacher_of(last_hidden, translator.gamma, W_U, translator.eps, k)
     weight = torch.full((N,), 1.0 / N, device=hidden.device)
     first = lambda: float(token_logp(translator(hidden), W_U, ids[:, :1].contiguous())[0].mean())

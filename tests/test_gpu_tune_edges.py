@@ -30,3 +30,17 @@ def test_the_weight_of_a_distillation_gets_its_gradient(N, trained):
     out.sum().backward()
     assert torch.equal(weight.grad, loss)
     assert torch.equal(rows.grad, grad) if trained else rows.grad is None
+
+
+def test_an_unembedding_that_wants_a_gradient():
+    """A model's own parameter: fit does not train it, and the calls say that they have no gradient of it."""
+    say("W_U that requires a gradient")
+    inner, last, gamma, W = tune.synthetic_layers(64, 128, 500, DEV)
+    W = torch.nn.Parameter(W)
+    result = tune.fit(tune.Translator(128, gamma, 1e-5), inner, last, W, k=4, steps=2)
+    assert len(result.losses) == 2 and W.grad is None
+    ids = torch.zeros((64, 1), dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError, match="W_U"):
+        tune.token_logp(inner, W, ids)
+    with pytest.raises(ValueError, match="W_U"):
+        tune.distill(inner, W, ids, torch.zeros((64, 1), device=DEV))

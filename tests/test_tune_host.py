@@ -39,3 +39,26 @@ def test_the_weight_of_a_distillation_gets_its_gradient(calls, trained):
     loss, grad = plain_distill(rows, W, ids, scores, weight=weight)
     assert torch.equal(weight.grad, factor * loss)
     assert torch.equal(rows.grad, (factor[:, None] * grad).to(torch.bfloat16)) if trained else rows.grad is None
+
+
+def plain_logp(rows, W_U, ids, *, temperature=1.0):
+    logp = torch.log_softmax(rows.detach().float() @ W_U.detach().float().t() / temperature, 1)
+    return logp.gather(1, ids.long()), torch.zeros((N,)), -(logp.exp() * logp).sum(1)
+
+
+@pytest.mark.parametrize("which", ["W_U", "teacher_scores"])
+def test_what_gets_no_gradient_must_not_ask_for_one(calls, monkeypatch, which):
+    """An error, and no training step that misses a term."""
+    monkeypatch.setattr(tune.LL, "ll_logp", plain_logp)
+    rows, W, ids, scores, _ = inputs()
+    rows.requires_grad_()
+    wants = {"W_U": W, "teacher_scores": scores}[which].requires_grad_()
+    uses = [lambda: tune.distill(rows, W, ids, scores)] + ([lambda: tune.token_logp(rows, W, ids)] if which == "W_U" else [])
+    for use in uses:
+        with pytest.raises(ValueError, match=which):
+            use()
+        with torch.no_grad():
+            use()                               # read, not trained
+    wants.requires_grad_(False)
+    for use in uses:
+        use()
