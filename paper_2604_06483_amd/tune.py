@@ -65,7 +65,7 @@ class _Distill(torch.autograd.Function):
     def forward(ctx, rows, W_U, teacher_ids, teacher_scores, temperature, weight):
         loss, grad = LL.ll_distill(rows, W_U, teacher_ids, teacher_scores, temperature=temperature, weight=weight, grad=ctx.needs_input_grad[0])
         ctx.save_for_backward(grad, loss if ctx.needs_input_grad[5] else None)
-        return loss if weight is None else weight * loss
+        return loss if weight is None else (weight * loss).masked_fill(weight == 0, 0.0)   # (a row of weight 0 may hold anything)
 
     @staticmethod
     @once_differentiable

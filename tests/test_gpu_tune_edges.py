@@ -44,3 +44,14 @@ def test_an_unembedding_that_wants_a_gradient():
         tune.token_logp(inner, W, ids)
     with pytest.raises(ValueError, match="W_U"):
         tune.distill(inner, W, ids, torch.zeros((64, 1), device=DEV))
+
+
+def test_a_row_of_weight_zero_adds_nothing_whatever_it_holds():
+    say("distill, a row of NaN with weight 0")
+    rows, W, ids, scores, weight = inputs(20, 128, 700, 4)
+    rows[3, 5], rows[7], weight[3], weight[7] = float("nan"), float("inf"), 0.0, 0.0
+    rows.requires_grad_()
+    out = tune.distill(rows, W, ids, scores, weight=weight)
+    assert torch.isfinite(out).all() and out[3] == 0 and out[7] == 0
+    out.sum().backward()
+    assert torch.isfinite(rows.grad).all() and not rows.grad[[3, 7]].any()

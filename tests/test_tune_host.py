@@ -62,3 +62,13 @@ def test_what_gets_no_gradient_must_not_ask_for_one(calls, monkeypatch, which):
     wants.requires_grad_(False)
     for use in uses:
         use()
+
+
+def test_a_row_of_weight_zero_adds_nothing_whatever_it_holds(monkeypatch):
+    loss, grad = torch.tensor([0.5, float("nan"), float("inf"), 2.0]), torch.zeros((4, d), dtype=torch.bfloat16)
+    monkeypatch.setattr(tune.LL, "ll_distill", lambda *a, **kw: (loss, grad))
+    weight = torch.tensor([0.25, 0.0, -0.0, 0.0], requires_grad=True)
+    out = tune.distill(torch.zeros((4, d), dtype=torch.bfloat16), torch.zeros((V, d), dtype=torch.bfloat16), torch.zeros((4, 1), dtype=torch.int32), torch.zeros((4, 1)), weight=weight)
+    assert torch.equal(out.detach(), torch.tensor([0.125, 0.0, 0.0, 0.0]))
+    out.sum().backward()
+    assert torch.equal(weight.grad.nan_to_num(7.0), loss.nan_to_num(7.0))     # (the weight's own gradient is what the row's loss is)
