@@ -54,7 +54,7 @@ class _TokenLogp(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g_logp, g_entropy):
         rows, W_U, ids, lse, entropy = ctx.saved_tensors
-        g_logp = torch.zeros(ids.shape, device=rows.device) if g_logp is None else g_logp.contiguous()
+        g_logp = torch.zeros(ids.shape, dtype=torch.float32, device=rows.device) if g_logp is None else g_logp.contiguous()
         g_entropy = None if g_entropy is None else g_entropy.contiguous()
         grad = LL.ll_logp_grad(rows, W_U, ids, lse, entropy, g_logp, g_entropy, temperature=ctx.temperature)
         return grad, None, None, None
@@ -107,10 +107,10 @@ class Translator(torch.nn.Module):
 
     def __init__(self, d: int, gamma: torch.Tensor, eps: float, scale: float = 1.0):
         super().__init__()
-        device = gamma.device
-        self.A = torch.nn.Parameter(torch.zeros((d, d), device=device))
-        self.b = torch.nn.Parameter(torch.zeros((d,), device=device))
-        self.gate = torch.nn.Parameter(torch.ones((d,), device=device))
+        like = {"dtype": torch.float32, "device": gamma.device}
+        self.A = torch.nn.Parameter(torch.zeros((d, d), **like))
+        self.b = torch.nn.Parameter(torch.zeros((d,), **like))
+        self.gate = torch.nn.Parameter(torch.ones((d,), **like))
         self.register_buffer("gamma", gamma)
         self.eps, self.scale = eps, scale
 
@@ -137,7 +137,7 @@ def fit(translator, hidden, last_hidden, W_U, *, k=20, temperature=1.0, steps=20
     """Trains a translator on one layer's rows against the last layer's read-out of the same tokens."""
     N, W_U = hidden.shape[0], W_U.detach()      # (the model's own: not trained)
     ids, scores = teacher_of(last_hidden, translator.gamma, W_U, translator.eps, k)
-    weight = torch.full((N,), 1.0 / N, device=hidden.device)
+    weight = torch.full((N,), 1.0 / N, dtype=torch.float32, device=hidden.device)
     first = lambda: float(token_logp(translator(hidden), W_U, ids[:, :1].contiguous())[0].mean())
     with torch.no_grad():
         before = first()

@@ -55,3 +55,15 @@ def test_a_row_of_weight_zero_adds_nothing_whatever_it_holds():
     assert torch.isfinite(out).all() and out[3] == 0 and out[7] == 0
     out.sum().backward()
     assert torch.isfinite(rows.grad).all() and not rows.grad[[3, 7]].any()
+
+
+def test_fit_under_another_default_type():
+    say("fit, torch's default type float64")
+    inner, last, gamma, W = tune.synthetic_layers(64, 128, 500, DEV)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float64)
+    try:
+        wide = tune.fit(tune.Translator(128, gamma, 1e-5), inner, last, W, k=4, steps=2)
+    finally:
+        torch.set_default_dtype(before)
+    assert wide == tune.fit(tune.Translator(128, gamma, 1e-5), inner, last, W, k=4, steps=2)

@@ -72,3 +72,24 @@ def test_a_row_of_weight_zero_adds_nothing_whatever_it_holds(monkeypatch):
     assert torch.equal(out.detach(), torch.tensor([0.125, 0.0, 0.0, 0.0]))
     out.sum().backward()
     assert torch.equal(weight.grad.nan_to_num(7.0), loss.nan_to_num(7.0))     # (the weight's own gradient is what the row's loss is)
+
+
+@pytest.fixture
+def wide_default():
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float64)
+    yield
+    torch.set_default_dtype(before)
+
+
+def test_types_do_not_follow_torchs_default(wide_default, monkeypatch):
+    """The calls take fp32: what autograd and the translator make themselves is fp32 under any default."""
+    seen = []
+    monkeypatch.setattr(tune.LL, "ll_logp", lambda rows, W, ids, **kw: tuple(torch.zeros(s, dtype=torch.float32) for s in ((N, k), (N,), (N,))))
+    monkeypatch.setattr(tune.LL, "ll_logp_grad", lambda rows, W, ids, lse, ent, g, ge, **kw: seen.append(g.dtype) or torch.zeros_like(rows))
+    rows, W, ids, _, _ = inputs()
+    rows.requires_grad_()
+    tune.token_logp(rows, W, ids)[1].sum().backward()
+    assert seen == [torch.float32]
+    t = tune.Translator(d, torch.ones((d,), dtype=torch.bfloat16), 1e-5)
+    assert {p.dtype for p in t.parameters()} == {torch.float32}
