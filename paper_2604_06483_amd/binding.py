@@ -395,12 +395,13 @@ def ll_capture_append(store, slices, t0, *, stream=None):
         raise LLError(rc, "ll_capture_append")
 
 
-def _gate(gate, N, d):
-    """Whether the gate is a row's own: [N, d], against [d] for all rows."""
+def _gate(gate, N, d, stream):
+    """The gate, [d] for all rows or [N, d], and whether it is a row's own."""
     if gate is None:
-        return 0
-    _check(gate, _BF16, "gate", (d,) if gate.dim() == 1 else (N, d))
-    return gate.dim() - 1
+        return None, 0
+    g = _rows(gate, d, stream) if gate.dim() > 2 and gate.shape[-1] == d else gate
+    _check(g, _BF16, "gate", (d,) if g.dim() == 1 else (N, d))
+    return g, g.dim() - 1
 
 
 def _workspace(workspace, need, device, stream):
@@ -414,7 +415,7 @@ def _workspace(workspace, need, device, stream):
 def ll_block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None, stream=None, out=None):
     """The residual and the norms around a block: x = hidden + scale gate u, u = y or gamma_y y / rms(y).
 
-    hidden, y [..., d] bf16, gamma [d] bf16, gate None, [d] or [N, d] bf16, gamma_y None or [d] bf16.
+    hidden, y [..., d] bf16, gamma [d] bf16, gate None, [d] or, a row's own, [..., d] bf16, gamma_y None or [d] bf16.
     Returns (x, gamma x / rms(x)), both bf16 in hidden's shape (`out`: two tensors to hold them).
     """
     d = hidden.shape[-1]
@@ -433,7 +434,8 @@ def ll_block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None, 
             _check(t, _BF16, name)
             if t.numel() != N * d:
                 raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(hidden.shape)}")
-    rc = (_lib or lib()).ll_block_norm(_shape(N, d, 0), h2.data_ptr(), y2.data_ptr(), _ptr(gate), _gate(gate, N, d), float(scale),
+    k2, gate_rows = _gate(gate, N, d, stream)
+    rc = (_lib or lib()).ll_block_norm(_shape(N, d, 0), h2.data_ptr(), y2.data_ptr(), _ptr(k2), gate_rows, float(scale),
                                        _ptr(gamma_y), gamma.data_ptr(), float(eps), x.data_ptr(), n.data_ptr(), _stream(stream))
     if rc != LL_OK:
         raise LLError(rc, "ll_block_norm")
@@ -447,7 +449,7 @@ def ll_block_norm_grad_workspace_bytes(N: int, d: int) -> int:
 def ll_block_norm_grad(hidden, y, gamma, eps, g_hidden, g_normed, *, gate=None, scale=1.0, gamma_y=None, workspace=None, stream=None):
     """Gradient of ll_block_norm: from its inputs, g_hidden (of x; None: zero) and g_normed, bf16 in hidden's shape.
 
-    Returns (d_hidden, d_y, d_gate, d_gamma_y, d_gamma): bf16 in hidden's shape, d_gate as the gate is (fp32 [d] or bf16 [N, d]; None without one),
+    Returns (d_hidden, d_y, d_gate, d_gamma_y, d_gamma): bf16 in hidden's shape, d_gate as the gate is (fp32 [d] or bf16 [..., d]; None without one),
     fp32 [d] (d_gamma_y None without gamma_y).
     """
     size, d = hidden.shape, hidden.shape[-1]
@@ -462,18 +464,20 @@ def ll_block_norm_grad(hidden, y, gamma, eps, g_hidden, g_normed, *, gate=None, 
     _check(gamma, _BF16, "gamma", (d,))
     if gamma_y is not None:
         _check(gamma_y, _BF16, "gamma_y", (d,))
-    gate_rows = _gate(gate, N, d)
+    k2, gate_rows = _gate(gate, N, d, stream)
     dev = hidden.device
     dh, dy = _like(h2, stream), _like(h2, stream)
-    dk = None if gate is None else _like(gate, stream) if gate_rows else _empty((d,), _F32, dev, stream)
+    dk = None if gate is None else _like(k2, stream) if gate_rows else _empty((d,), _F32, dev, stream)
     dgy = None if gamma_y is None else _empty((d,), _F32, dev, stream)
     dg = _empty((d,), _F32, dev, stream)
     ws = _workspace(workspace, lambda: ll_block_norm_grad_workspace_bytes(N, d), dev, stream)
     rc = (_lib or lib()).ll_block_norm_grad(_shape(N, d, 0), ws.data_ptr(), ws.numel() * ws.element_size(), h2.data_ptr(), y2.data_ptr(),
-                                            _ptr(gate), gate_rows, float(scale), _ptr(gamma_y), gamma.data_ptr(), float(eps), _ptr(gh),
+                                            _ptr(k2), gate_rows, float(scale), _ptr(gamma_y), gamma.data_ptr(), float(eps), _ptr(gh),
                                             gn.data_ptr(), dh.data_ptr(), dy.data_ptr(), _ptr(dk), _ptr(dgy), dg.data_ptr(), _stream(stream))
     if rc != LL_OK:
         raise LLError(rc, "ll_block_norm_grad")
+    if gate_rows and dk.shape != gate.shape:
+        dk = dk.reshape(gate.shape)
     return dh if dh.shape == size else dh.reshape(size), dy if dy.shape == size else dy.reshape(size), dk, dgy, dg
 
 

@@ -120,3 +120,22 @@ def test_results_and_workspaces_are_memory_of_the_calls_stream(monkeypatch, name
     with Made():
         MAKES[name](mine)
     assert made and all(s is mine for s in made) and kept == [current] * len(made)
+
+
+@pytest.mark.parametrize("whole", [True, False])
+def test_a_gate_may_have_the_batch_of_its_rows(monkeypatch, whole):
+    def shapes(t, dtype, name, shape=None):
+        if shape is not None and t.shape != shape:
+            raise ValueError(name)
+        assert t.is_contiguous(), name
+
+    monkeypatch.setattr(LL, "_lib", Library())
+    monkeypatch.setattr(LL, "_check", shapes)
+    monkeypatch.setattr(LL, "_stream", lambda s: 0)
+    h = torch.zeros((B, T, d), dtype=BF16)
+    gate = torch.zeros((B, T, d), dtype=BF16) if whole else across(B, T, d)
+    LL.ll_block_norm(h, h, vector(), 1e-5, gate=gate)
+    assert LL.ll_block_norm_grad(h, h, vector(), 1e-5, None, h, gate=gate)[2].shape == (B, T, d)
+    for wrong in (gate[:, :2], gate[..., :8], gate[0], vector()[:8], torch.zeros((), dtype=BF16)):
+        with pytest.raises(ValueError, match="gate"):
+            LL.ll_block_norm(h, h, vector(), 1e-5, gate=wrong)

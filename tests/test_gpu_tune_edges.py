@@ -67,3 +67,18 @@ def test_fit_under_another_default_type():
     finally:
         torch.set_default_dtype(before)
     assert wide == tune.fit(tune.Translator(128, gamma, 1e-5), inner, last, W, k=4, steps=2)
+
+
+def test_a_gate_with_the_batch_of_its_rows():
+    say("block norm, a gate [B, T, d]")
+    B, T, d = 3, 11, 136
+    g = torch.Generator(device=DEV).manual_seed(5)
+    normal = lambda *s: torch.randn(s, generator=g, device=DEV).to(torch.bfloat16)
+    gamma, gx, gn = normal(d), normal(B, T, d), normal(B, T, d)
+    leaves = [normal(B, T, d).requires_grad_() for _ in range(3)]
+    flat = [t.detach().reshape(B * T, d).clone().requires_grad_() for t in leaves]
+    for h, y, gate in (leaves, flat):
+        out = tune.block_norm(h, y, gamma, 1e-5, gate=gate, scale=0.5)
+        torch.autograd.backward(out, [gx.reshape(h.shape), gn.reshape(h.shape)])
+    for a, b in zip(leaves, flat):
+        assert a.grad.shape == a.shape and torch.equal(a.grad.reshape(B * T, d), b.grad)
