@@ -24,6 +24,8 @@ from . import binding as LL
 class _BlockNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, y, gamma, gate, gamma_y, eps, scale):
+        ctx.types = [None if p is None else p.dtype for p in (gamma, gate, gamma_y)]
+        gamma, gate, gamma_y = (p.to(torch.bfloat16) if t == torch.float32 else p for p, t in zip((gamma, gate, gamma_y), ctx.types))
         ctx.save_for_backward(hidden, y, gamma, gate, gamma_y)
         ctx.eps, ctx.scale = eps, scale
         ctx.set_materialize_grads(False)
@@ -37,8 +39,8 @@ class _BlockNorm(torch.autograd.Function):
         g_normed = torch.zeros_like(hidden) if g_normed is None else g_normed.contiguous()
         d_hidden, d_y, d_gate, d_gamma_y, d_gamma = LL.ll_block_norm_grad(hidden, y, gamma, ctx.eps, g_hidden, g_normed, gate=gate,
                                                                           scale=ctx.scale, gamma_y=gamma_y)
-        like = lambda g, p: None if p is None else g.to(p.dtype)
-        return d_hidden, d_y.reshape(y.shape), like(d_gamma, gamma), like(d_gate, gate), like(d_gamma_y, gamma_y), None, None
+        d_gamma, d_gate, d_gamma_y = (None if t is None else g.to(t) for g, t in zip((d_gamma, d_gate, d_gamma_y), ctx.types))
+        return d_hidden, d_y.reshape(y.shape), d_gamma, d_gate, d_gamma_y, None, None
 
 
 class _TokenLogp(torch.autograd.Function):
@@ -84,7 +86,10 @@ def _no_gradient(**tensors):
 
 
 def block_norm(hidden, y, gamma, eps, *, gate=None, scale=1.0, gamma_y=None):
-    """ll_block_norm, differentiable in hidden, y, gamma, gate and gamma_y: (x, gamma x / rms(x))."""
+    """ll_block_norm, differentiable in hidden, y, gamma, gate and gamma_y: (x, gamma x / rms(x)).
+
+    gamma, gate and gamma_y may be fp32: they are rounded to bf16 for the call, and what all rows share gets the call's fp32 sums as they are.
+    The gradient of a parameter in bf16 is rounded to it, as autograd's types demand."""
     return _BlockNorm.apply(hidden, y, gamma, gate, gamma_y, eps, scale)
 
 
@@ -117,7 +122,7 @@ class Translator(torch.nn.Module):
     def forward(self, hidden):
         bf16 = torch.bfloat16
         y = torch.nn.functional.linear(hidden, self.A.to(bf16), self.b.to(bf16))
-        return block_norm(hidden, y, self.gamma, self.eps, gate=self.gate.to(bf16), scale=self.scale)[1]
+        return block_norm(hidden, y, self.gamma, self.eps, gate=self.gate, scale=self.scale)[1]
 
 
 def teacher_of(last_hidden, gamma, W_U, eps, k):

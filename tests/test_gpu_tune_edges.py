@@ -82,3 +82,25 @@ def test_a_gate_with_the_batch_of_its_rows():
         torch.autograd.backward(out, [gx.reshape(h.shape), gn.reshape(h.shape)])
     for a, b in zip(leaves, flat):
         assert a.grad.shape == a.shape and torch.equal(a.grad.reshape(B * T, d), b.grad)
+
+
+def test_a_masters_gradient_is_the_calls_own():
+    say("block norm, parameters in fp32")
+    N, d = 200, 136
+    g = torch.Generator(device=DEV).manual_seed(6)
+    normal = lambda *s: torch.randn(s, generator=g, device=DEV)
+    h, y, gx, gn = (normal(N, d).to(torch.bfloat16) for _ in range(4))
+    gate, gamma, gamma_y = (normal(d).requires_grad_() for _ in range(3))
+    out = tune.block_norm(h, y, gamma, 1e-5, gate=gate, scale=0.5, gamma_y=gamma_y)
+    torch.autograd.backward(out, [gx, gn])
+    rounded = [t.detach().to(torch.bfloat16) for t in (gamma, gate, gamma_y)]
+    _, _, dk, dgy, dg = LL.ll_block_norm_grad(h, y, rounded[0], 1e-5, gx, gn, gate=rounded[1], scale=0.5, gamma_y=rounded[2])
+    for p, want in ((gate, dk), (gamma_y, dgy), (gamma, dg)):
+        assert torch.equal(p.grad, want)
+
+
+def test_other_types_are_refused_still():
+    say("block norm, parameters in fp16")
+    h = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(TypeError, match="gamma"):
+        tune.block_norm(h, h, torch.ones((64,), dtype=torch.float16, device=DEV), 1e-5)

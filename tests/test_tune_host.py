@@ -93,3 +93,33 @@ def test_types_do_not_follow_torchs_default(wide_default, monkeypatch):
     assert seen == [torch.float32]
     t = tune.Translator(d, torch.ones((d,), dtype=torch.bfloat16), 1e-5)
     assert {p.dtype for p in t.parameters()} == {torch.float32}
+
+
+def test_parameters_in_fp32_get_their_sums_unrounded(monkeypatch):
+    """gamma, gamma_y and the gate go into the calls as bf16; a master in fp32 gets the fp32 sums over the rows as the call returns them."""
+    g = torch.Generator().manual_seed(1)
+    sums = [torch.randn((d,), generator=g) for _ in range(3)]
+    given = []
+
+    def forward(hidden, y, gamma, eps, *, gate, scale, gamma_y):
+        given.extend([gamma, gate, gamma_y])
+        return torch.zeros_like(hidden), torch.zeros_like(hidden)
+
+    def backward(hidden, y, gamma, eps, g_hidden, g_normed, *, gate, scale, gamma_y):
+        given.extend([gamma, gate, gamma_y])
+        return torch.zeros_like(hidden), torch.zeros_like(y), sums[0], sums[1], sums[2]
+
+    monkeypatch.setattr(tune.LL, "ll_block_norm", forward)
+    monkeypatch.setattr(tune.LL, "ll_block_norm_grad", backward)
+    h = torch.zeros((N, d), dtype=torch.bfloat16)
+    for dtype in (torch.float32, torch.bfloat16):
+        gate, gamma_y, gamma = (torch.randn((d,), generator=g).to(dtype).requires_grad_() for _ in range(3))
+        del given[:]
+        tune.block_norm(h, h, gamma, 1e-5, gate=gate, gamma_y=gamma_y)[1].sum().backward()
+        for got, p in zip(given, 2 * [gamma, gate, gamma_y]):
+            assert got.dtype == torch.bfloat16 and torch.equal(got, p.detach().to(torch.bfloat16))
+        for p, s in zip((gate, gamma_y, gamma), sums):
+            assert p.grad.dtype == dtype and torch.equal(p.grad, s.to(dtype))
+    translator = tune.Translator(d, torch.ones((d,), dtype=torch.bfloat16), 1e-5)
+    translator(h).sum().backward()
+    assert torch.equal(translator.gate.grad, sums[0])
