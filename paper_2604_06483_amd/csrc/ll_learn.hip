@@ -87,7 +87,8 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
   return first;
 }
 
-// Before the first product: the rows padded, the listed tokens' logits, and the largest in powers of two (of a row without any: 0).
+// Before the first product: the rows padded, the listed tokens' logits, and the largest in powers of two, to the nearest whole one (of a row
+// without any: 0).  What P is relative to is always whole: to change it then changes exponents only, and rounds nothing again.
 __global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref,
                                                                 uint16_t* __restrict__ panel, int64_t lda) {
   __shared__ float z[LIST_MAX];
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p
     if (p.ids[e] >= 0 && p.ids[e] < p.V) most = z[lane] * p.to_log2;
   }
   most = wave_max(most);
-  if (lane == 0) ref[row] = fabsf(most) < 1e30f ? most : 0.f;
+  if (lane == 0) ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
 }
 
 // A row's teacher, by a wavefront, one lane an entry: t = softmax of the scores / temperature over the entries that there are.
@@ -131,15 +132,15 @@ __device__ __forceinline__ float distill_loss(const Teacher& teacher, float logp
 // Teacher, loss, and what the gradient is made of: a row a workgroup, the first wavefront one lane an entry.  With P = 2^(x - base) over the
 // whole row, dz = a (p - t) is a 2^(base - lse2) (P - t 2^(lse2 - base)): the listed tokens' entries are put into P, from their fp32 logits
 // and rounded once, and the rest is the row's factor of the gradient.  A row whose reference has moved in some tile first has its tiles
-// brought to one base, lse2, here.  Of a row without a teacher (or of weight 0, as far as the gradient goes) nothing that the row holds
-// matters.
+// brought to one base here, the whole number next to lse2: by whole powers of two, so that nothing is rounded again.  Of a row without a
+// teacher (or of weight 0, as far as the gradient goes) nothing that the row holds matters.
 __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __restrict__ ids, const float* __restrict__ z, int k, int V,
                                                               float to_log2, const float4* __restrict__ stats, int parts, int stride,
                                                               const float* __restrict__ scores, const float* __restrict__ weight,
                                                               float temperature, float* __restrict__ loss, RowTerms* __restrict__ terms,
                                                               const float* __restrict__ ref, const float* __restrict__ moved, int tiles,
                                                               uint16_t* __restrict__ P, int64_t ldp) {
-  __shared__ float shared_lse2;
+  __shared__ float shared_base;
   __shared__ int shared_moved;
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x & 63;
@@ -163,11 +164,11 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
       bool other = false;
       for (int i = lane; i < parts; i += 64) other |= stats[row * parts + i].x != ref[row];
       other = __builtin_amdgcn_ballot_w64(other) != 0;
-      const float base = other ? r.lse2 : ref[row];
+      const float base = other ? rintf(r.lse2) : ref[row];
       if (lane == 0) {
         terms[row] = {r.lse2, 0.f, 0.f, live ? a * __builtin_amdgcn_exp2f(base - r.lse2) : 0.f};
         shared_moved = live && other;
-        shared_lse2 = r.lse2;
+        shared_base = base;
       }
       t *= __builtin_amdgcn_exp2f(r.lse2 - base);
       l += r.lse2 - base;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void ll_distill_rows_kernel(const int32_t* __r
   if (shared_moved) {
     for (int64_t c = 8 * (int)threadIdx.x; c < ldp; c += 8 * 256) {
       const uint4 q = *reinterpret_cast<const uint4*>(at + c);
-      const float by = __builtin_amdgcn_exp2f(moved[row * tiles + c / BM] - shared_lse2);
+      const float by = __builtin_amdgcn_exp2f(moved[row * tiles + c / BM] - shared_base);
       *reinterpret_cast<uint4*>(at + c) = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
                                                      pack_bf16(bf16_lo(q.z) * by, bf16_hi(q.z) * by), pack_bf16(bf16_lo(q.w) * by, bf16_hi(q.w) * by));
     }

@@ -97,6 +97,7 @@ struct LearnEpilogue {
         // the four lanes of a row together
         m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most)) * c;
         const bool move = with_lane_xor<32>(with_lane_xor<16>(add.x > MOST ? 1u : 0u, any), any) != 0;
+        if (WHAT == EXPS) m = ceilf(m);   // (whole, as it was)
         const float to_ref = move ? fmaxf(m, st.ref[j]) : st.ref[j], before = st.ref[j] - to_ref, keep = __builtin_amdgcn_exp2f(before);
         st.t[j] = keep * fmaf(before, st.s[j], st.t[j]);
         st.s[j] *= keep;
