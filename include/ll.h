@@ -299,7 +299,8 @@ int ll_steer_sweep_topk(const ll_shape* shape, void* workspace, size_t workspace
  *
  * Parameters shared by the rows get the sum over them, added in one order (the same bits every time); N == 0 gives them zeros.
  * d_hidden and d_y may be the buffer of any [N, d] input, but not each other's; no other overlap.
- * workspace: at least ll_block_norm_grad_workspace_bytes(shape) bytes, 256-byte aligned.
+ * workspace: at least ll_block_norm_grad_workspace_bytes(shape) bytes, 256-byte aligned.  A device's first call of a kind may set a kernel
+ * attribute: make it outside stream capture.
  */
 int ll_block_norm(const ll_shape* shape, const void* hidden, const void* y, const void* gate, int gate_rows, float scale,
                   const void* gamma_y, const void* gamma, float eps, void* out_hidden, void* out_normed, void* stream);

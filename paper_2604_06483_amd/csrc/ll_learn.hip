@@ -380,7 +380,7 @@ struct LearnPlan {
 // 203 | 175 | 185 | 198 and 454 | 368 | 374 | 393, 192 rows 256 | 223 | 193 | 201 and 565 | 490 | 414 | 427, 348 rows 453 | 301 | 270 | 301 and
 // 967 | 682 | 586 | 661, 500 rows 567 | 406 | 355 | 313 and 1225 | 888 | 777 | 688; d = 1608, V = 50257, 777 rows 228 | 164 | 143 | 162 and 513 | 350
 // | 328 | 343; d = 8192, V = 128256, 37 rows 427 | 428 | 411 | 456 and 776 | 772 | 759 | 868, 777 rows 2204 | 1513 | 1446 | 1428 and 4545 |
-// 3247 | 2990 | 2900.
+// 3247 | 2990 | 2900.  (The rule takes no account of d: at 8192 it gives away 4 and 2 % of 37 rows' calls and 1 and 3 % of 777's.)
 constexpr double BLOCK_COST[4] = {0.47, 0.6, 0.79, 1.0};
 int row_tiles(int rows) {
   if (rows <= BN) return (rows + 63) / 64;
@@ -404,7 +404,7 @@ struct FewShape {
 // A gradient: up to four rows (two above d = 8192, what the registers hold).  Whole calls, us, so | in two products, ll_distill: d = 256, V =
 // 150 000, 1 row 24 | 56, 4 rows 39 | 56; 1608, 50257: 35 | 76, 49 | 77; 2560, 151936: 136 | 275, 192 | 279; 4096, 128256: 176 | 372, 186 | 374;
 // 8192, 128256: 341 | 760, 363 | 761; 16384, 60000, 1 row 336 | 706.  (Eight rows: 60 | 56, 79 | 79, 360 | 284, 319 | 375 and, in too many registers,
-// 851 | 755.)  Statistics alone: up to eight where a row of W fills the workgroup.  ll_logp, 4 rows and 8: d = 256 23 | 27, 34 | 27; 2560 137 | 145,
+// 851 | 755.  One limit for every d: eight rows gain at 4096 alone.)  Statistics alone: up to eight where a row of W fills the workgroup.  ll_logp, 4 rows and 8: d = 256 23 | 27, 34 | 27; 2560 137 | 145,
 // 185 | 147; 4096 176 | 202, 178 | 205; 8192 342 | 436, 346 | 431.
 FewShape few_shape(const ll_shape* s, Needs needs) {
   const int n8 = s->d >> 3;

@@ -101,7 +101,8 @@ def token_logp(rows, W_U, ids, *, temperature=1.0):
 
 def distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weight=None):
     """ll_distill, differentiable in the rows and the weight: weight times every row's loss.  The rows' gradient is formed with the loss, in one
-    call; give the weights here (1 / N for a mean), and sum.  W_U and the teacher get no gradient: detached, or an error."""
+    call, in bf16: give the weights here (1 / N for a mean), and sum (an incoming gradient other than a power of two rounds it again).  W_U and the
+    teacher get no gradient: detached, or an error."""
     _no_gradient(W_U=W_U, teacher_scores=teacher_scores)
     return _Distill.apply(rows, W_U, teacher_ids, teacher_scores, temperature, weight)
 
