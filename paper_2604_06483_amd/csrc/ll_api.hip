@@ -1,9 +1,7 @@
 // Error reporting of the C ABI, and what the launches of several files need once per device.
 #include "ll_common.h"
 
-#include <mutex>
-#include <utility>
-#include <vector>
+#include <atomic>
 
 namespace ll {
 
@@ -15,18 +13,30 @@ int hip_failed(hipError_t e) {
   return LL_EHIP;
 }
 
-// A kernel that uses more than 64 KB of dynamic LDS has to be told so once per device; remembered
-// here so that the hot path makes no attribute call.
+// A kernel that uses more than 64 KB of dynamic LDS has to be told so once per device; remembered here so that the hot path makes no
+// attribute call.  (Places of fixed number, taken in order and never given back: nothing here allocates, throws or waits.  Two threads may both ask for
+// a kernel that is new, and past the last place every call asks: the attribute is the same each time.)
 int allow_dynamic_lds(const void* kern, size_t lds) {
-  static std::mutex mu;
-  static std::vector<std::pair<int, const void*>> done;
+  constexpr int PLACES = 1024;
+  struct Place {
+    std::atomic<const void*> kern;
+    int dev;
+  };
+  static Place places[PLACES];
+  static std::atomic<int> taken{0};
   int dev = -1;
   LL_HIP_CHECK(hipGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  for (const auto& e : done)
-    if (e.first == dev && e.second == kern) return LL_OK;
+  for (const Place& e : places) {
+    const void* k = e.kern.load(std::memory_order_acquire);   // (dev is written before it)
+    if (k == kern && e.dev == dev) return LL_OK;
+    if (k == nullptr) break;
+  }
   LL_HIP_CHECK(hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-  done.emplace_back(dev, kern);
+  const int at = taken.load(std::memory_order_relaxed) < PLACES ? taken.fetch_add(1, std::memory_order_relaxed) : PLACES;
+  if (at < PLACES) {
+    places[at].dev = dev;
+    places[at].kern.store(kern, std::memory_order_release);
+  }
   return LL_OK;
 }
 
