@@ -12,8 +12,6 @@
 
 #include <atomic>
 #include <climits>
-#include <mutex>
-#include <utility>
 #include <vector>
 
 namespace {
