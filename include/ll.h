@@ -361,6 +361,55 @@ size_t ll_distill_workspace_bytes(const ll_shape* shape, int k);
 int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature, int k,
                const int32_t* teacher_ids, const float* teacher_scores, const float* weight, float* out_loss, void* out_grad, void* stream);
 
+/*
+ * Learning from answers: losses over the model's own tokens, each with its gradient to the rows in one call (about the time of ll_distill: two
+ * products with W_U, where ll_logp, a loss and ll_logp_grad take three).  Row r stands before token ids[r]; with l[r] its log-probability
+ * as in ll_logp,
+ *
+ * ll_policy: a clipped policy loss with a KL term, over sampled tokens:
+ *
+ *   ratio = exp(l - old_logp),   q = ref_logp - l
+ *   out_loss[r] = -min( ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A ) + kl (e^q - q - 1),   A = advantage[r]
+ *
+ *   advantage  fp32 [N];  old_logp  fp32 [N] or NULL: l itself, a ratio of 1 that still has its gradient
+ *   ref_logp   fp32 [N], or NULL (only with kl == 0)
+ *   weight     fp32 [N] or NULL (1): of the row, in the gradient (out_loss is without it); a row of weight 0 gets the gradient 0, whatever it holds
+ *   clip_low   0 to 1;  clip_high  0 or more, infinity: no bound;  kl  finite, not negative
+ *   out_loss, out_logp  fp32 [N];  out_grad  bf16 [N, d] = weight[r] d out_loss[r] / d rows[r, :], or NULL: the losses alone, for about half the
+ *              time; the workspace may then be of ll_logp_workspace_bytes(shape, 1)
+ * A ratio on the border of the clipping counts as inside.
+ *
+ * ll_preference: the loss of pairs of answers of which the first is preferred.  Sequence i is rows offsets[i] to offsets[i + 1] - 1, the pairs are
+ * sequences 2 j (preferred) and 2 j + 1;
+ *
+ *   score[i] = sum of l[r] - ref_logp[r] over the sequence's rows (mean 1: divided by their number),   h = beta (score[2 j] - score[2 j + 1])
+ *   LL_PREFERENCE_LOGISTIC  out_loss[j] = -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h)
+ *   LL_PREFERENCE_HINGE     out_loss[j] = max(0, 1 - h)
+ *   LL_PREFERENCE_SQUARE    out_loss[j] = ((h - 1/2) / beta)^2
+ *
+ *   offsets    int32 [2 n_pairs + 1], device, ascending, within [0, N]; a sequence may be empty (score 0).  Others make losses and gradients
+ *              unspecified, but nothing outside the tensors is read or written
+ *   ref_logp   fp32 [N] or NULL (0);  weight  fp32 [n_pairs] or NULL (1): of the pair, in the gradient; 0: none, whatever the pair holds
+ *   beta       positive, finite;  smoothing  0 to 1/2, 0 but for the logistic form
+ *   out_loss   fp32 [n_pairs];  out_score  fp32 [n_pairs, 2];  out_logp  fp32 [N]
+ *   out_grad   bf16 [N, d] or NULL, as above; rows of no sequence get zeros
+ * With more rows than a pass (2048) the workspace also holds 4 d bytes a row and slice of the vocabulary.  N == 0: the pairs' losses alone.
+ *
+ * In both, a row whose id is outside [0, V) (padding) takes no part: log-probability NaN, loss 0, gradient 0, in no score and no length.  A row
+ * that holds NaN or infinity makes its own results NaN, and its pair's; no other is affected.  Everything else as in ll_logp.
+ */
+#define LL_PREFERENCE_LOGISTIC 0
+#define LL_PREFERENCE_HINGE    1
+#define LL_PREFERENCE_SQUARE   2
+size_t ll_policy_workspace_bytes(const ll_shape* shape);
+int ll_policy(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature,
+              const int32_t* ids, const float* advantage, const float* old_logp, const float* ref_logp, const float* weight, float clip_low,
+              float clip_high, float kl, float* out_loss, float* out_logp, void* out_grad, void* stream);
+size_t ll_preference_workspace_bytes(const ll_shape* shape, int32_t n_pairs);
+int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature,
+                  const int32_t* ids, const int32_t* offsets, int32_t n_pairs, const float* ref_logp, const float* weight, int form, int mean,
+                  float beta, float smoothing, float* out_loss, float* out_score, float* out_logp, void* out_grad, void* stream);
+
 /* Text for an LL_E* code (static storage, never NULL). */
 const char* ll_error_string(int code);
 

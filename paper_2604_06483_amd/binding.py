@@ -17,6 +17,7 @@ LL_OK, LL_EINVAL, LL_EWORKSPACE, LL_EHIP, LL_ESCRATCH = 0, -1, -2, -3, -4
 LL_KMAX = 32
 LL_STATIC_SCRATCH_BYTES = 64 << 20
 LL_LIST_MAX = 64
+LL_PREFERENCE = {"logistic": 0, "hinge": 1, "square": 2}
 LL_FLAG_TOPK_SOFTMAX = 1
 LL_FLAG_REGISTER_STAGED = 2
 
@@ -107,6 +108,14 @@ def lib() -> ctypes.CDLL:
         L.ll_logp_grad.restype = c_int
         L.ll_distill.argtypes = lens + [c_void_p] * 5
         L.ll_distill.restype = c_int
+        L.ll_policy_workspace_bytes.argtypes = [POINTER(ll_shape)]
+        L.ll_policy_workspace_bytes.restype = c_size_t
+        L.ll_policy.argtypes = lens[:6] + [c_void_p] * 5 + [c_float] * 3 + [c_void_p] * 4
+        L.ll_policy.restype = c_int
+        L.ll_preference_workspace_bytes.argtypes = [POINTER(ll_shape), c_int32]
+        L.ll_preference_workspace_bytes.restype = c_size_t
+        L.ll_preference.argtypes = lens[:6] + [c_void_p] * 2 + [c_int32] + [c_void_p] * 2 + [c_int] * 2 + [c_float] * 2 + [c_void_p] * 5
+        L.ll_preference.restype = c_int
         L.ll_error_string.argtypes = [c_int]
         L.ll_error_string.restype = c_char_p
         L.ll_last_hip_error.argtypes = []
@@ -564,3 +573,81 @@ def ll_distill(rows, W_U, teacher_ids, teacher_scores, *, temperature=1.0, weigh
     if rc != LL_OK:
         raise LLError(rc, "ll_distill")
     return loss, out if out is None or out.shape == rows.shape else out.reshape(rows.shape)
+
+
+def ll_policy_workspace_bytes(N: int, d: int, V: int) -> int:
+    return int(lib().ll_policy_workspace_bytes(ll_shape(N, d, V)))
+
+
+def ll_preference_workspace_bytes(N: int, d: int, V: int, pairs: int) -> int:
+    return int(lib().ll_preference_workspace_bytes(ll_shape(N, d, V), pairs))
+
+
+def _each(t, dtype, name, N):
+    """One value a row, in the rows' own leading shape or flat."""
+    if t is None:
+        return None
+    if isinstance(t, _Tensor) and t.dim() != 1 and t.is_contiguous():
+        t = t.reshape(-1)
+    _check(t, dtype, name, (N,))
+    return t
+
+
+def _answer_rows(rows, W_U, ids, stream):
+    d = rows.shape[-1]
+    r2 = _rows(rows, d, stream)
+    N, V = r2.shape[0], W_U.shape[0]
+    _check(r2, _BF16, "rows")
+    _check(W_U, _BF16, "W_U", (V, d))
+    return r2, _each(ids, torch.int32, "ids", N), N, d, V
+
+
+def ll_policy(rows, W_U, ids, advantage, old_logp=None, *, ref_logp=None, weight=None, clip=(0.2, 0.2), kl=0.0, temperature=1.0, grad=True,
+              workspace=None, stream=None):
+    """Clipped policy loss with a KL term over sampled tokens: rows [..., d] bf16 (normalised), W_U [V, d] bf16, ids int32, advantage, old_logp
+    (None: on policy), ref_logp (None: only with kl 0) and weight (None: 1) fp32, one a row; clip: how far the ratio may fall below and rise above 1.
+
+    Returns (loss [N] fp32, the tokens' log-probabilities [N] fp32, gradient of weight . loss in bf16 in the rows' shape, or None with grad=False).
+    """
+    r2, i2, N, d, V = _answer_rows(rows, W_U, ids, stream)
+    A, old, ref, w = (_each(t, _F32, name, N) for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")))
+    dev = rows.device
+    loss, logp = _empty((N,), _F32, dev, stream), _empty((N,), _F32, dev, stream)
+    out = _like(r2, stream) if grad else None
+    ws = _workspace(workspace, lambda: ll_policy_workspace_bytes(N, d, V) if grad else ll_logp_workspace_bytes(N, d, V, 1), dev, stream)
+    rc = (_lib or lib()).ll_policy(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(), float(temperature),
+                                   i2.data_ptr(), _ptr(A), _ptr(old), _ptr(ref), _ptr(w), float(clip[0]), float(clip[1]), float(kl),
+                                   loss.data_ptr(), logp.data_ptr(), _ptr(out), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_policy")
+    return loss, logp, out if out is None or out.shape == rows.shape else out.reshape(rows.shape)
+
+
+def ll_preference(rows, W_U, ids, offsets, *, ref_logp=None, weight=None, beta=0.1, smoothing=0.0, form="logistic", mean=False, temperature=1.0,
+                  grad=True, workspace=None, stream=None):
+    """Preference loss over pairs of answers: rows [..., d] bf16 (normalised), W_U [V, d] bf16, ids int32 and ref_logp fp32 (None: 0), one a row;
+    offsets int32 [2 pairs + 1], on the GPU: where the sequences begin and end, the preferred one of a pair first; weight fp32 [pairs] or None (1).
+    form: "logistic", "hinge" or "square"; mean: scores a token instead of a sequence.
+
+    Returns (loss [pairs] fp32, scores [pairs, 2] fp32, the tokens' log-probabilities [N] fp32, gradient of weight . loss in bf16 in the rows'
+    shape, or None with grad=False).
+    """
+    if form not in LL_PREFERENCE:
+        raise ValueError(f"form: {form!r}, expected one of {sorted(LL_PREFERENCE)}")
+    r2, i2, N, d, V = _answer_rows(rows, W_U, ids, stream)
+    _check(offsets, torch.int32, "offsets")
+    if offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
+        raise ValueError(f"offsets: shape {tuple(offsets.shape)}, expected (2 pairs + 1,)")
+    P = offsets.shape[0] // 2
+    ref, w = _each(ref_logp, _F32, "ref_logp", N), _each(weight, _F32, "weight", P)
+    dev = rows.device
+    loss, score, logp = _empty((P,), _F32, dev, stream), _empty((P, 2), _F32, dev, stream), _empty((N,), _F32, dev, stream)
+    out = _like(r2, stream) if grad else None
+    ws = _workspace(workspace, lambda: ll_preference_workspace_bytes(N, d, V, P) if grad else ll_logp_workspace_bytes(N, d, V, 1), dev, stream)
+    rc = (_lib or lib()).ll_preference(_shape(N, d, V), ws.data_ptr(), ws.numel() * ws.element_size(), r2.data_ptr(), W_U.data_ptr(),
+                                       float(temperature), i2.data_ptr(), offsets.data_ptr(), P, _ptr(ref), _ptr(w), LL_PREFERENCE[form],
+                                       1 if mean else 0, float(beta), float(smoothing), loss.data_ptr(), score.data_ptr(), logp.data_ptr(),
+                                       _ptr(out), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_preference")
+    return loss, score, logp, out if out is None or out.shape == rows.shape else out.reshape(rows.shape)

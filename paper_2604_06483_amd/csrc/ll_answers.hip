@@ -1,0 +1,369 @@
+// Learning from answers through the lens: a clipped policy loss with a KL term over sampled tokens, and a preference loss over pairs of
+// answers, each with its gradient to the (normalised) rows.
+//
+//   l = log softmax(a W^T / T)[id],   dA = c / T (W_id - sum_v p_v W_v),   c = d loss / d l
+//
+// Both products are those of distillation from a list of one token (ll_learn.hip): the first leaves P = 2^(x - base) behind it, the second
+// multiplies P, with the row's own token put into it, by W_U.  What is new is c.  Nothing of it is needed before the second product's sums
+// are rounded, where it is a factor of the row, so that the logits are formed once: with the log-probabilities and their gradient as two
+// calls there is a third product (1500 rows, d = 4096, V = 128256: see the figures at the entry points).
+//
+// A policy's c is the row's own.  A preference's is known when every row of its pair has been through W_U.  Up to one pass of rows the
+// pairs are joined between the two products; beyond, every pass's sums stay in fp32 (4 d bytes a row and slice of the vocabulary, beside
+// 4 d V flops) and are joined, scaled and rounded once behind the last pass: no product is formed again, however long the answers are.
+#include "ll_learn_host.h"
+
+namespace {
+
+struct PolicyArgs {
+  const float* advantage;
+  const float* old_logp;    // or nullptr: the log-probability itself
+  const float* ref_logp;    // or nullptr: no KL term
+  const float* weight;      // or nullptr: 1
+  float* loss;
+  float low, high, kl;
+};
+
+struct AnswerArgs {
+  const int32_t* ids;
+  const float* z;             // the tokens' logits
+  const float4* stats;
+  int parts, stride;          // parts of a row, and rows between them (1: a row's are side by side)
+  int V;
+  float to_log2, inv_t;
+  float* logp;
+  RowTerms* terms;            // or nullptr: no gradient
+  // the products' P; nullptr with few rows, whose sums are relative to lse2
+  uint16_t* P;
+  int64_t ldp;
+  const float* ref;
+  const float* moved;
+  int tiles;
+  PolicyArgs policy;
+};
+
+// Loss of a sampled token and what it gains by the token's log-probability.  A ratio on the border of the clipping counts as inside.
+struct PolicyTerm {
+  float loss, c;
+};
+__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t row, float logp) {
+  const float A = p.advantage[row];
+  const float ratio = p.old_logp != nullptr ? expf(logp - p.old_logp[row]) : 1.f;
+  const float most = 1.f + p.high, least = 1.f - p.low;
+  const bool clipped = A > 0.f ? ratio > most : ratio < least;
+  PolicyTerm r;
+  r.loss = A == 0.f ? 0.f : -A * (clipped ? (A > 0.f ? most : least) : ratio);   // (an advantage of 0 has no loss, whatever the ratio)
+  r.c = A == 0.f || clipped ? 0.f : -A * ratio;
+  if (p.ref_logp != nullptr) {
+    const float q = p.ref_logp[row] - logp, e = expm1f(q);     // e^q - 1 keeps its digits where the two policies are near
+    r.loss = fmaf(p.kl, e - q, r.loss);
+    r.c = fmaf(-p.kl, e, r.c);
+  }
+  r.c *= p.weight != nullptr ? p.weight[row] : 1.f;
+  if (p.weight != nullptr && p.weight[row] == 0.f) r.c = 0.f;  // (whatever the row holds)
+  return r;
+}
+
+// A row a workgroup: its log-probability and what its gradient is made of.  terms.a is the gradient's factor without c, terms.factor with it
+// (a preference's comes later: ll_preference_pairs_kernel).  P as in ll_distill_rows_kernel, with one entry of share 1.
+template <bool POLICY>
+__global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p) {
+  __shared__ float shared_base;
+  __shared__ int shared_moved;
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  int id = -1;
+  bool live = false;
+  float put = 0.f;
+  if (threadIdx.x < 64) {
+    const RowStats r = join_stats(p.stride == 1 ? p.stats + row * p.parts : p.stats + row, p.parts, lane, p.stride);
+    id = p.ids[row];
+    const bool valid = id >= 0 && id < p.V;
+    const float l = fmaf(p.z[row], p.to_log2, -r.lse2);
+    bool other = false;
+    if (p.P != nullptr)
+      for (int i = lane; i < p.parts; i += 64) other |= p.stats[row * p.parts + i].x != p.ref[row];
+    other = __builtin_amdgcn_ballot_w64(other) != 0;
+    const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : p.ref[row];
+    PolicyTerm t = {0.f, 0.f};
+    if (POLICY && valid) t = policy_term(p.policy, row, l * LN2);
+    live = valid && (!POLICY || t.c != 0.f);
+    if (lane == 0) {
+      p.logp[row] = valid ? l * LN2 : NAN;
+      if (POLICY) p.policy.loss[row] = t.loss;
+      if (p.terms != nullptr) {
+        const float unit = -p.inv_t * (p.P == nullptr ? 1.f : __builtin_amdgcn_exp2f(base - r.lse2));
+        p.terms[row] = {r.lse2, unit, 0.f, POLICY && live ? unit * t.c : 0.f};
+      }
+      shared_moved = live && other;
+      shared_base = base;
+    }
+    put = __builtin_amdgcn_exp2f(l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
+  }
+  if (p.P == nullptr) return;
+  __syncthreads();
+  uint16_t* const at = p.P + row * p.ldp;
+  if (shared_moved) {
+    tiles_to_base(at, p.ldp, p.moved + row * p.tiles, shared_base);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0 && live) at[place_in_p(id)] = (uint16_t)pack_bf16(put, 0.f);
+}
+
+struct PairArgs {
+  const int32_t* ids;
+  const int32_t* offsets;   // [2 pairs + 1]
+  const float* logp;
+  const float* ref_logp;    // or nullptr: 0
+  const float* weight;      // or nullptr: 1
+  int64_t N;
+  int V, form, mean;
+  float beta, smoothing;
+  float* loss;
+  float* score;             // [pairs, 2]
+  RowTerms* terms;          // or nullptr: no gradient
+};
+
+__device__ __forceinline__ double group_total(double x, double* red) {
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  const double sum = (red[0] + red[1]) + (red[2] + red[3]);
+  __syncthreads();
+  return sum;
+}
+
+// A pair a workgroup: the two answers' scores, summed in 64 bits (a long answer's log-ratios cancel) in one order, the loss, and every
+// row's c.  Offsets that are out of order or out of range are brought into it: no row outside [0, N) is touched.
+__global__ __launch_bounds__(256) void ll_preference_pairs_kernel(const PairArgs p) {
+  __shared__ double red[4];
+  const int64_t pair = blockIdx.x;
+  int64_t begin[2], end[2];
+  double score[2], length[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const int64_t b = p.offsets[2 * pair + side], e = p.offsets[2 * pair + side + 1];
+    begin[side] = b < 0 ? 0 : b > p.N ? p.N : b;
+    end[side] = e < begin[side] ? begin[side] : e > p.N ? p.N : e;
+    double sum = 0., count = 0.;
+    for (int64_t r = begin[side] + (int)threadIdx.x; r < end[side]; r += 256) {
+      if (p.ids[r] < 0 || p.ids[r] >= p.V) continue;
+      sum += (double)p.logp[r] - (p.ref_logp != nullptr ? (double)p.ref_logp[r] : 0.);
+      count += 1.;
+    }
+    sum = group_total(sum, red);
+    count = group_total(count, red);
+    length[side] = p.mean && count > 1. ? count : 1.;
+    score[side] = sum / length[side];
+  }
+  const float h = (float)((double)p.beta * (score[0] - score[1]));
+  float loss, slope;
+  if (p.form == LL_PREFERENCE_LOGISTIC) {
+    const float e = expf(-fabsf(h)), soft = log1pf(e);
+    const float to = 1.f / (1.f + e), from = e / (1.f + e);        // sigmoids of |h| and of -|h|
+    const float up = h > 0.f ? to : from, down = h > 0.f ? from : to;
+    loss = (1.f - p.smoothing) * (soft + fmaxf(-h, 0.f)) + p.smoothing * (soft + fmaxf(h, 0.f));
+    slope = p.smoothing * up - (1.f - p.smoothing) * down;
+    if (h != h) loss = slope = h;
+  } else if (p.form == LL_PREFERENCE_HINGE) {
+    loss = h < 1.f ? 1.f - h : h - h;
+    slope = h < 1.f ? -1.f : h - h;
+    if (h > 1.f) loss = slope = 0.f;
+  } else {
+    const float off = (float)((score[0] - score[1]) - 0.5 / (double)p.beta);
+    loss = off * off;
+    slope = 2.f * off / p.beta;
+  }
+  if (threadIdx.x == 0) {
+    p.loss[pair] = loss;
+    p.score[2 * pair] = (float)score[0];
+    p.score[2 * pair + 1] = (float)score[1];
+  }
+  if (p.terms == nullptr) return;
+  const float w = p.weight != nullptr ? p.weight[pair] : 1.f;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const float c = w == 0.f ? 0.f : w * slope * p.beta / (side == 0 ? (float)length[side] : -(float)length[side]);
+    for (int64_t r = begin[side] + (int)threadIdx.x; r < end[side]; r += 256)
+      if (p.ids[r] >= 0 && p.ids[r] < p.V) p.terms[r].factor = c != 0.f ? p.terms[r].a * c : 0.f;
+  }
+}
+
+// Few rows: the parts' sums joined, and the row's token.
+__global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinArgs p, const RowTerms* __restrict__ terms) {
+  __shared__ float scale[FEW_LEARN_STREAMS];
+  __shared__ float share[1];
+  __shared__ int id_of[1];
+  const int row = blockIdx.y;
+  const RowTerms t = terms[row];
+  for (int i = threadIdx.x; i < p.parts; i += 256) {
+    const float4 q = p.f.stats[(int64_t)i * p.stride + row];
+    scale[i] = q.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(q.x - t.lse2);
+  }
+  if (threadIdx.x == 0) {
+    const int id = p.f.list.ids[row];
+    share[0] = -1.f;
+    id_of[0] = id < p.f.list.V ? id : -1;
+  }
+  __syncthreads();
+  few_join_columns(p, row, t.factor, scale, share, id_of);
+}
+
+// ---------------------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------------------
+// What distillation from one token has, every row's terms, and where pairs take more rows than a pass the passes' sums.
+struct AnswerPlan {
+  LearnPlan l;
+  bool keep;
+  int64_t passes;
+  size_t pass_sums, terms, sums, total;
+};
+
+AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
+  AnswerPlan a = {};
+  a.l = plan_for(s, 1, needs);
+  a.passes = (s->N + a.l.pass_rows - 1) / a.l.pass_rows;
+  a.keep = pairs && needs == BACKWARD && a.passes > 1;
+  a.total = a.l.total;
+  if (needs == FORWARD) return a;
+  a.terms = a.total;
+  a.total = align_up(a.total + (size_t)(s->N > 0 ? s->N : 1) * sizeof(RowTerms), 256);
+  if (a.keep) {
+    a.sums = a.total;
+    a.pass_sums = align_up((size_t)a.l.back_splits * a.l.pass_rows * s->d * sizeof(float), 256);
+    a.total += a.pass_sums * (size_t)a.passes;
+  }
+  return a;
+}
+
+// The first product of a pass and its rows' terms; POLICY: and losses.
+template <bool POLICY>
+int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids, float temperature, float* logp, RowTerms* terms,
+                const PolicyArgs& policy, FewJoinArgs& join) {
+  const LearnPlan& l = a.l;
+  AnswerArgs r = {};
+  r.ids = ids;
+  r.z = at<float>(ws, l.z);
+  r.stats = at<float4>(ws, l.stats);
+  r.V = p.shape->V;
+  r.to_log2 = p.to_log2;
+  r.inv_t = 1.f / temperature;
+  r.logp = logp;
+  r.terms = terms;
+  r.policy = policy;
+  if (l.few) {
+    LL_TRY(terms != nullptr ? p.few<EXPS>(ids, join.f) : p.few<STATS>(ids, join.f));
+    r.parts = l.few_parts;
+    r.stride = l.few_rows;
+  } else {
+    hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
+                       p.panel(), l.lda);
+    LL_HIP_CHECK(hipGetLastError());
+    LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());
+    r.parts = l.splits;
+    r.stride = 1;
+    if (terms != nullptr) {
+      r.P = at<uint16_t>(ws, l.P);
+      r.ldp = l.ldp;
+      r.ref = at<float>(ws, l.ref);
+      r.moved = at<float>(ws, l.moved);
+      r.tiles = l.tiles;
+    }
+  }
+  hipLaunchKernelGGL(ll_answers_rows_kernel<POLICY>, dim3(p.n), dim3(r.P != nullptr ? 256 : 64), 0, p.stream, r);
+  LL_HIP_CHECK(hipGetLastError());
+  return LL_OK;
+}
+
+int answer_few_join(const Pass& p, const AnswerPlan& a, FewJoinArgs& j, const RowTerms* terms, void* out) {
+  j.parts = a.l.few_parts;
+  j.stride = a.l.few_rows;
+  j.out = (uint16_t*)out;
+  hipLaunchKernelGGL(ll_answers_few_join_kernel, dim3((p.shape->d + 63) / 64, p.n), dim3(256), 0, p.stream, j, terms);
+  LL_HIP_CHECK(hipGetLastError());
+  return LL_OK;
+}
+
+bool finite(float x) { return x - x == 0.f; }
+
+}  // namespace
+
+extern "C" {
+
+size_t ll_policy_workspace_bytes(const ll_shape* shape) { return valid(shape, 1) ? answer_plan(shape, false, BACKWARD).total : 0; }
+
+int ll_policy(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature,
+              const int32_t* ids, const float* advantage, const float* old_logp, const float* ref_logp, const float* weight, float clip_low,
+              float clip_high, float kl, float* out_loss, float* out_logp, void* out_grad, void* stream) {
+  if (!valid(shape, 1)) return LL_EINVAL;
+  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !(kl >= 0.f) || !finite(kl) || (kl != 0.f && ref_logp == nullptr))
+    return LL_EINVAL;
+  if (shape->N == 0) return LL_OK;
+  if (advantage == nullptr || out_loss == nullptr || out_logp == nullptr) return LL_EINVAL;
+  if (misaligned(advantage, 4) || misaligned(old_logp, 4) || misaligned(ref_logp, 4) || misaligned(weight, 4) || misaligned(out_loss, 4) ||
+      misaligned(out_logp, 4) || misaligned(out_grad, 16))
+    return LL_EINVAL;
+  const bool grad = out_grad != nullptr;
+  const AnswerPlan a = answer_plan(shape, false, grad ? BACKWARD : FORWARD);
+  LL_TRY(check(shape, workspace, workspace_bytes, a.total, rows, W_U, temperature, ids));
+  return for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream, [&](const Pass& p, int64_t r0) -> int {
+    const auto from = [&](const float* x) { return x != nullptr ? x + r0 : nullptr; };
+    const PolicyArgs policy = {advantage + r0, from(old_logp), kl != 0.f ? from(ref_logp) : nullptr, from(weight), out_loss + r0, clip_low, clip_high, kl};
+    RowTerms* const terms = grad ? at<RowTerms>(workspace, a.terms) + r0 : nullptr;
+    FewJoinArgs j = {};
+    LL_TRY(answer_rows<true>(p, a, workspace, ids + r0, temperature, out_logp + r0, terms, policy, j));
+    if (!grad) return LL_OK;
+    if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
+    return p.back((uint16_t*)out_grad + r0 * shape->d, terms, at<float>(workspace, a.l.part));
+  });
+}
+
+size_t ll_preference_workspace_bytes(const ll_shape* shape, int32_t n_pairs) {
+  return valid(shape, 1) && n_pairs >= 0 ? answer_plan(shape, true, BACKWARD).total : 0;
+}
+
+int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes, const void* rows, const void* W_U, float temperature,
+                  const int32_t* ids, const int32_t* offsets, int32_t n_pairs, const float* ref_logp, const float* weight, int form, int mean,
+                  float beta, float smoothing, float* out_loss, float* out_score, float* out_logp, void* out_grad, void* stream) {
+  if (!valid(shape, 1) || n_pairs < 0) return LL_EINVAL;
+  if (form != LL_PREFERENCE_LOGISTIC && form != LL_PREFERENCE_HINGE && form != LL_PREFERENCE_SQUARE) return LL_EINVAL;
+  if ((mean != 0 && mean != 1) || !(beta > 0.f) || !finite(beta) || !(smoothing >= 0.f && smoothing <= 0.5f)) return LL_EINVAL;
+  if (form != LL_PREFERENCE_LOGISTIC && smoothing != 0.f) return LL_EINVAL;
+  if (n_pairs > 0 && (offsets == nullptr || out_loss == nullptr || out_score == nullptr)) return LL_EINVAL;
+  if (misaligned(offsets, 4) || misaligned(ref_logp, 4) || misaligned(weight, 4) || misaligned(out_loss, 4) || misaligned(out_score, 4) ||
+      misaligned(out_logp, 4) || misaligned(out_grad, 16))
+    return LL_EINVAL;
+  const bool grad = out_grad != nullptr;
+  const AnswerPlan a = answer_plan(shape, true, grad ? BACKWARD : FORWARD);
+  if (shape->N > 0) {
+    if (out_logp == nullptr) return LL_EINVAL;
+    LL_TRY(check(shape, workspace, workspace_bytes, a.total, rows, W_U, temperature, ids));
+  }
+  RowTerms* const terms = grad && shape->N > 0 ? at<RowTerms>(workspace, a.terms) : nullptr;
+  const auto pairs = [&]() -> int {
+    if (n_pairs == 0) return LL_OK;
+    const PairArgs q = {ids, offsets, out_logp, ref_logp, weight, shape->N, shape->V, form, mean, beta, smoothing, out_loss, out_score, terms};
+    hipLaunchKernelGGL(ll_preference_pairs_kernel, dim3((unsigned)n_pairs), dim3(256), 0, (hipStream_t)stream, q);
+    LL_HIP_CHECK(hipGetLastError());
+    return LL_OK;
+  };
+  const auto sums_of = [&](int64_t r0) { return at<float>(workspace, a.sums + (size_t)(r0 / a.l.pass_rows) * a.pass_sums); };
+  const bool between = grad && shape->N > 0 && !a.keep;      // one pass: the pairs come between the products
+  LL_TRY(for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream, [&](const Pass& p, int64_t r0) -> int {
+    FewJoinArgs j = {};
+    LL_TRY(answer_rows<false>(p, a, workspace, ids + r0, temperature, out_logp + r0, grad ? terms + r0 : nullptr, PolicyArgs{}, j));
+    if (!grad) return LL_OK;
+    if (a.keep) return p.back(nullptr, terms + r0, sums_of(r0));
+    LL_TRY(pairs());
+    if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
+    return p.back((uint16_t*)out_grad, terms, at<float>(workspace, a.l.part));
+  }));
+  if (between) return LL_OK;
+  LL_TRY(pairs());
+  if (!a.keep) return LL_OK;
+  return for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream,
+                    [&](const Pass& p, int64_t r0) -> int { return p.join((uint16_t*)out_grad + r0 * shape->d, terms + r0, sums_of(r0)); });
+}
+
+}  // extern "C"

@@ -1,0 +1,299 @@
+"""ll_policy and ll_preference against the fp64 oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.answers_oracle as O
+from oracle.learn_oracle import _log_softmax
+from paper_2604_06483_amd import binding as LL
+from tests.conftest import say
+from tests.test_gpu_learn import f64, inputs, logit_error
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+# few rows of every width that they are dealt by; less than a tile, ragged, one pass and several, the gradient in one slice
+SIZES = [(1, 8, 1), (1, 64, 5), (2, 72, 257), (3, 328, 1000), (4, 1024, 900), (2, 2048, 700), (4, 4096, 600), (4, 8192, 1000), (2, 16384, 500),
+         (3, 16384, 300), (5, 2504, 5001), (64, 256, 4096), (257, 128, 3001), (300, 1608, 2050), (33, 2560, 20000), (17, 200, 70000),
+         (600, 520, 60), (2048, 1024, 300), (2100, 64, 777), (4500, 72, 300)]
+
+
+def case(N, d, V, seed=0):
+    a, W, ids, g = inputs(N, d, V, 1, seed=seed)
+    ids = ids[:, 0].clone()
+    if N > 4:
+        ids[torch.randint(0, N, (N // 5,), generator=g)] = torch.randint(0, V, (N // 5,), generator=g).to(torch.int32)   # unlikely tokens
+        ids[1], ids[2] = -1, V                                         # rows that hold none
+    return a, W, ids, g
+
+
+def grad_close(got, dz, W, slack, what):
+    """P is rounded to bf16 at most twice, by up to 2^-8 of itself, independently: 4 2^-8 over the root of the squares is six to seven of
+    its standard deviations.  The result once.  slack: what is left by errors of l, of the sums and of c."""
+    ref, got = dz @ W, f64(got)
+    bound = 2.0 ** -8 * np.abs(ref) + 8 * 2.0 ** -9 * np.sqrt((dz * dz) @ (W * W)) + slack + 1e-37
+    bad = ~(np.abs(got - ref) <= bound)
+    assert not bad.any(), (what, int(bad.sum()), float(np.nanmax(np.abs(got - ref) / bound)))
+
+
+def unit_gradient(r, w, ids, temperature):
+    """(p + the token's 1) |W| / T of every row: what an error of c is multiplied by."""
+    lp, _ = _log_softmax(r, w, temperature)
+    ok = (ids >= 0) & (ids < w.shape[0])
+    p, at = np.exp(lp), np.where(ok, ids, 0)[:, None]
+    np.put_along_axis(p, at, np.take_along_axis(p, at, 1) + 1, 1)
+    return p @ np.abs(w) / temperature
+
+
+def check_policy(a, W, ids, A, old, ref, weight, low, high, kl, temperature):
+    r, w, n = f64(a), f64(W), ids.numpy()
+    ez = logit_error(r, w, temperature)
+    to = lambda x: None if x is None else x.to(DEV)
+    args = (a.to(DEV), W.to(DEV), ids.to(DEV), A.to(DEV), to(old))
+    kw = dict(ref_logp=to(ref), weight=to(weight), clip=(low, high), kl=kl, temperature=temperature)
+    loss, logp, grad = LL.ll_policy(*args, **kw)
+    alone, alone_logp, none = LL.ll_policy(*args, **kw, grad=False)
+    assert none is None
+    rl, rlogp, dz, _ = O.policy(r, w, n, f64(A), f64(old), f64(ref), f64(weight), low, high, kl, temperature)
+    ratio = np.ones_like(rlogp) if old is None else np.exp(np.nan_to_num(rlogp) - f64(old))
+    q = np.zeros_like(ratio) if ref is None else f64(ref) - np.nan_to_num(rlogp)
+    # l is off by 2 ez; exp, its product and the sum by some units of 2^-24 of what they are made of
+    size = np.abs(f64(A)) * ratio + kl * (np.exp(q) + np.abs(q) + 1)
+    bound = size * (2.02 * ez + 8 * 2.0 ** -24)
+    for got_loss, got_logp in ((loss, logp), (alone, alone_logp)):
+        assert np.all(np.abs(f64(got_loss) - rl) <= bound), float(np.max(np.abs(f64(got_loss) - rl) / bound))
+        assert np.array_equal(np.isnan(f64(got_logp)), np.isnan(rlogp))
+        np.testing.assert_allclose(f64(got_logp), rlogp, rtol=0, atol=2 * ez)
+    each = np.abs(f64(weight)) if weight is not None else 1.0
+    ok = (n >= 0) & (n < w.shape[0])
+    off = (np.where(ok, each * size, 0.0) * (6 * ez + 12 * 2.0 ** -24))[:, None]
+    grad_close(grad, dz, w, off * unit_gradient(r, w, n, temperature), "policy grad")
+    return loss, logp, grad
+
+
+def policy_inputs(a, W, ids, g, temperature):
+    """The sampling policy's and the reference's log-probabilities beside the row's own; no ratio within 1e-3 of a border."""
+    N = len(ids)
+    l = torch.from_numpy(np.nan_to_num(O.policy(f64(a), f64(W), ids.numpy(), np.ones(N), temperature=temperature)[1]))
+    ratio = torch.exp(0.3 * torch.randn((N,), generator=g).double())
+    for border in (0.8, 1.2, 0.9, 1.4):
+        ratio = torch.where((ratio - border).abs() < 1e-3, border + 2e-3, ratio)
+    old = (l - torch.log(ratio)).float()
+    ref = (l + 0.4 * torch.randn((N,), generator=g)).float()
+    return torch.randn((N,), generator=g), old, ref, torch.rand((N,), generator=g)
+
+
+@pytest.mark.parametrize("N,d,V", SIZES)
+@pytest.mark.parametrize("temperature", [1.0, 0.7])
+def test_policy_against_the_oracle(N, d, V, temperature):
+    say(f"policy N={N} d={d} V={V} T={temperature}")
+    a, W, ids, g = case(N, d, V)
+    A, old, ref, weight = policy_inputs(a, W, ids, g, temperature)
+    A[0] = 0.0
+    if N > 4:
+        weight[3] = 0.0
+    if temperature == 1.0:
+        check_policy(a, W, ids, A, old, None, None, 0.2, 0.2, 0.0, temperature)
+    else:
+        _, _, grad = check_policy(a, W, ids, A, old, ref, weight, 0.1, 0.4, 0.3, temperature)
+        if N > 4:
+            assert not grad[[1, 2, 3]].any()
+
+
+def test_policy_on_its_own_samples_and_without_an_upper_bound():
+    for N, d, V in ((3, 512, 2000), (130, 328, 1000)):
+        say(f"policy on its own samples N={N}")
+        a, W, ids, g = case(N, d, V, seed=1)
+        A, old, ref, weight = policy_inputs(a, W, ids, g, 1.0)
+        loss, _, _ = check_policy(a, W, ids, A, None, ref, weight, 0.2, 0.2, 0.05, 1.0)
+        check_policy(a, W, ids, A, old, None, weight, 1.0, math.inf, 0.0, 1.0)
+        loss, _, _ = LL.ll_policy(a.to(DEV), W.to(DEV), ids.to(DEV), A.to(DEV))
+        ok = (ids >= 0) & (ids < V)
+        assert np.array_equal(f64(loss), f64(torch.where(ok, -A, torch.zeros(()))))
+
+
+def pair_offsets(N, P, g, full=False):
+    cuts = torch.randint(0, N + 1, (2 * P - 1,), generator=g).sort().values
+    last = torch.tensor([N if full else N - N // 8])
+    return torch.cat([torch.zeros(1, dtype=torch.long), torch.minimum(cuts, last), last]).to(torch.int32)
+
+
+def check_preference(a, W, ids, offsets, ref, weight, beta, smoothing, form, mean, temperature):
+    r, w, n, o = f64(a), f64(W), ids.numpy(), offsets.numpy()
+    ez = logit_error(r, w, temperature)
+    to = lambda x: None if x is None else x.to(DEV)
+    args = (a.to(DEV), W.to(DEV), ids.to(DEV), offsets.to(DEV))
+    kw = dict(ref_logp=to(ref), weight=to(weight), beta=beta, smoothing=smoothing, form=form, mean=mean, temperature=temperature)
+    loss, score, logp, grad = LL.ll_preference(*args, **kw)
+    alone = LL.ll_preference(*args, **kw, grad=False)
+    assert alone[3] is None
+    rl, rs, rlogp, dz, size = O.preference(r, w, n, o, f64(ref), f64(weight), beta, smoothing, form, mean, temperature)
+    P = len(rl)
+    ok = (n >= 0) & (n < w.shape[0])
+    count = np.array([max(1, ok[o[i]:o[i + 1]].sum()) for i in range(2 * P)]).reshape(P, 2)
+    length = count if mean else np.ones((P, 2))
+    off_s = count / length * 2 * ez + 2.0 ** -24 * np.abs(rs)             # every l of an answer off by 2 ez, the same way
+    off_d = off_s.sum(1) + 2.0 ** -24 * np.abs(rs[:, 0] - rs[:, 1])
+    h = beta * (rs[:, 0] - rs[:, 1])
+    slope = np.array([O.pair_loss(form, x, beta, smoothing)[1] for x in h])
+    curve = {"logistic": 0.25, "hinge": 0.0, "square": 2 / beta ** 2}[form]
+    off_h = beta * off_d + 2.0 ** -22 * np.abs(h)
+    off_l = np.abs(slope) * off_h + curve * off_h ** 2 + 8 * 2.0 ** -24 * (np.abs(rl) + 1)
+    for got in ((loss, score, logp), alone[:3]):
+        assert np.all(np.abs(f64(got[1]) - rs) <= off_s), float(np.max(np.abs(f64(got[1]) - rs) / off_s))
+        assert np.all(np.abs(f64(got[0]) - rl) <= off_l), float(np.max(np.abs(f64(got[0]) - rl) / off_l))
+        np.testing.assert_allclose(f64(got[2]), rlogp, rtol=0, atol=2 * ez)
+    # c is weight slope beta / length
+    off_c = np.zeros(len(n))
+    each = np.ones(P) if weight is None else np.abs(f64(weight))
+    for i in range(2 * P):
+        off_c[o[i]:o[i + 1]] = each[i // 2] * beta * (curve * off_h[i // 2] + (8 * 2.0 ** -24 + 4 * ez) * np.abs(slope[i // 2])) / length[i // 2, i % 2]
+    grad_close(grad, dz, w, np.where(ok, off_c, 0.0)[:, None] * unit_gradient(r, w, n, temperature), "preference grad")
+    return loss, score, logp, grad
+
+
+@pytest.mark.parametrize("N,d,V", SIZES)
+@pytest.mark.parametrize("form", ["logistic", "hinge", "square"])
+def test_preference_against_the_oracle(N, d, V, form):
+    P = max(1, min(9, N // 2))
+    say(f"preference N={N} d={d} V={V} pairs={P} {form}")
+    a, W, ids, g = case(N, d, V)
+    mean, temperature = form != "logistic", 0.7 if form == "hinge" else 1.0
+    offsets = pair_offsets(N, P, g, full=N < 8)
+    l = torch.from_numpy(np.nan_to_num(O.policy(f64(a), f64(W), ids.numpy(), np.ones(N), temperature=temperature)[1]))
+    ref = None if form == "hinge" else (l + 0.5 * torch.randn((N,), generator=g)).float()
+    weight = None if form == "logistic" else torch.rand((P,), generator=g)
+    if weight is not None and P > 2:
+        weight[1] = 0.0
+    _, _, _, grad = check_preference(a, W, ids, offsets, ref, weight, 0.1 if form != "hinge" else 0.4, 0.1 if form == "logistic" else 0.0, form, mean,
+                                     temperature)
+    assert not grad[int(offsets[-1]):].any()
+    if weight is not None and P > 2:
+        assert not grad[int(offsets[2]):int(offsets[4])].any()
+
+
+def test_one_long_pair_over_several_passes():
+    """The two answers of one pair lie in three passes."""
+    N, d, V = 5000, 64, 500
+    say(f"preference, one pair of {N} rows")
+    a, W, ids, g = case(N, d, V, seed=2)
+    check_preference(a, W, ids, torch.tensor([0, 2600, N], dtype=torch.int32), None, None, 0.02, 0.0, "logistic", True, 1.0)
+
+
+def test_rows_far_from_the_token():
+    """A token 2^-150 as likely as the most likely one: the exponentials' reference moves, and the loss is as large as it is."""
+    N, d, V = 40, 64, 2000
+    say("policy and preference of impossible tokens")
+    g = torch.Generator().manual_seed(3)
+    W = torch.randn((V, d), generator=g).to(torch.bfloat16)
+    a = (2.0 * W[torch.randint(0, V, (N,), generator=g)].float()).to(torch.bfloat16)
+    z = a.double() @ W.double().T
+    ids = z.argmin(1).to(torch.int32)
+    assert float((z.max(1).values - z.min(1).values).min()) > 104
+    A = torch.randn((N,), generator=g)
+    for rows in (N, 3):
+        check_policy(a[:rows], W, ids[:rows], A[:rows], None, None, None, 0.2, 0.2, 0.0, 1.0)
+        check_preference(a[:rows], W, ids[:rows], torch.tensor([0, 1, rows], dtype=torch.int32), None, None, 0.01, 0.0, "logistic", False, 1.0)
+
+
+@pytest.mark.parametrize("N,d,V", [(4, 512, 900), (70, 328, 1000), (2100, 64, 777)])
+def test_rows_that_hold_nan_stay_alone(N, d, V):
+    say(f"NaN rows N={N}")
+    a, W, ids, g = case(N, d, V, seed=4)
+    ids = ids.clamp(0, V - 1)
+    A, old, _, weight = policy_inputs(a, W, ids, g, 1.0)
+    bad = N - 1
+    b = a.clone()
+    b[bad, 3] = float("nan")
+    dev = lambda *t: [x.to(DEV) for x in t]
+    clean, dirty = LL.ll_policy(*dev(a, W, ids, A, old)), LL.ll_policy(*dev(b, W, ids, A, old))
+    for x, y in zip(clean, dirty):
+        assert torch.equal(x[:bad], y[:bad]) and torch.isnan(y[bad:]).all()
+    weight[bad] = 0.0
+    got = LL.ll_policy(*dev(b, W, ids, A, old), weight=weight.to(DEV))
+    assert not got[2][bad].any()
+    offsets = torch.tensor([0, N // 4, N // 2, N // 2 + 1, N], dtype=torch.int32)
+    clean, dirty = LL.ll_preference(*dev(a, W, ids, offsets)), LL.ll_preference(*dev(b, W, ids, offsets))
+    assert torch.equal(clean[0][:1], dirty[0][:1]) and torch.equal(clean[3][:N // 2], dirty[3][:N // 2])
+    assert torch.isnan(dirty[0][1]) and torch.isnan(dirty[3][N // 2:]).all()
+    got = LL.ll_preference(*dev(b, W, ids, offsets), weight=torch.tensor([1.0, 0.0], device=DEV))
+    assert torch.equal(got[3][:N // 2], clean[3][:N // 2]) and not got[3][N // 2:].any()
+
+
+def test_offsets_out_of_range_touch_nothing_outside():
+    """Every access is within the tensors whatever the offsets say; pairs whose own are right have their results."""
+    N, d, V = 50, 64, 300
+    say("preference, offsets out of range")
+    a, W, ids, g = case(N, d, V, seed=5)
+    dev = lambda *t: [x.to(DEV) for x in t]
+    good = LL.ll_preference(*dev(a, W, ids, torch.tensor([0, 10, 20], dtype=torch.int32)))
+    odd = torch.tensor([0, 10, 20, 2 ** 31 - 1, -5, 30, -2 ** 31], dtype=torch.int32)
+    got = LL.ll_preference(*dev(a, W, ids, odd))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][:1], good[0]) and torch.equal(got[1][:1], good[1])
+
+
+def test_no_rows_and_no_pairs():
+    say("preference without rows, without pairs")
+    d, V = 64, 300
+    W = torch.zeros((V, d), dtype=torch.bfloat16, device=DEV)
+    none = torch.zeros((0, d), dtype=torch.bfloat16, device=DEV)
+    ids = torch.zeros((0,), dtype=torch.int32, device=DEV)
+    loss, score, logp, grad = LL.ll_preference(none, W, ids, torch.zeros((5,), dtype=torch.int32, device=DEV))
+    assert np.allclose(loss.cpu(), math.log(2), rtol=2 ** -22, atol=0) and not score.any() and logp.numel() == grad.numel() == 0
+    rows = torch.ones((6, d), dtype=torch.bfloat16, device=DEV)
+    loss, score, logp, grad = LL.ll_preference(rows, W, torch.zeros((6,), dtype=torch.int32, device=DEV), torch.zeros((1,), dtype=torch.int32, device=DEV))
+    assert loss.numel() == 0 and not grad.any() and np.allclose(logp.cpu(), -math.log(V), rtol=2 ** -21, atol=0)
+    assert [t.numel() for t in LL.ll_policy(none, W, ids, torch.zeros((0,), device=DEV))] == [0, 0, 0]
+
+
+@pytest.mark.parametrize("N,d,V", [(2, 512, 3000), (100, 200, 3000), (2100, 64, 500)])
+def test_captured_and_replayed(N, d, V):
+    """One workspace, three replays with the program's own work between them, new inputs in the captured buffers: eager bits each time."""
+    say(f"answers in a graph N={N}")
+    a, W, ids, g = case(N, d, V, seed=6)
+    A, old, ref, weight = (x.to(DEV) for x in policy_inputs(a, W, ids, g, 1.0))
+    a, W, ids = a.to(DEV), W.to(DEV), ids.to(DEV)
+    offsets = torch.tensor([0, N // 2, N], dtype=torch.int32, device=DEV)
+    ws = torch.empty((max(LL.ll_policy_workspace_bytes(N, d, V), LL.ll_preference_workspace_bytes(N, d, V, 1)),), dtype=torch.uint8, device=DEV)
+    s = torch.cuda.Stream()
+
+    def both(stream=None):
+        return (LL.ll_policy(a, W, ids, A, old, ref_logp=ref, weight=weight, kl=0.1, workspace=ws, stream=stream)
+                + LL.ll_preference(a, W, ids, offsets, ref_logp=ref, workspace=ws, stream=stream))
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        held = both(s)
+    for turn in range(3):
+        a.copy_(torch.flip(a, (0,)))
+        want = [t.clone() for t in both()]
+        torch.cuda.synchronize()
+        ws.fill_(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(held, want):
+            assert torch.equal(x.nan_to_num(7.0), y.nan_to_num(7.0)), turn
+
+
+def test_on_another_stream_and_in_a_batch():
+    N, d, V = 24, 256, 1000
+    say("answers on another stream, rows as a batch")
+    a, W, ids, g = case(N, d, V, seed=7)
+    A = torch.randn((N,), generator=g)
+    a, W, ids, A = (x.to(DEV) for x in (a, W, ids, A))
+    want = LL.ll_policy(a, W, ids, A)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = LL.ll_policy(a.view(4, 6, d), W, ids.view(4, 6), A.view(4, 6), stream=s)
+    s.synchronize()
+    assert got[2].shape == (4, 6, d)
+    for x, y in zip(got, want):
+        assert torch.equal(x.reshape(y.shape).nan_to_num(7.0), y.nan_to_num(7.0))
+    turned = a.view(4, 6, d).transpose(0, 1)
+    got = LL.ll_policy(turned, W, ids.view(4, 6).T.contiguous(), A.view(4, 6).T.contiguous())
+    assert torch.equal(got[2].transpose(0, 1).reshape(N, d), want[2])
