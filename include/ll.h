@@ -410,6 +410,60 @@ int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes
                   const int32_t* ids, const int32_t* offsets, int32_t n_pairs, const float* ref_logp, const float* weight, int form, int mean,
                   float beta, float smoothing, float* out_loss, float* out_score, float* out_logp, void* out_grad, void* stream);
 
+/*
+ * A training step over many tensors at once.  The list is in HOST memory, read during the call; its tensors are on the device, contiguous,
+ * 16-byte aligned (scales: 4), of at most LL_TENSOR_MAX elements, any number from 0, none overlapping another.
+ *
+ * ll_grad_norm: out_norm[0] = sqrt of the sum of g^2 over all gradients of the list (of the entries grad, n and flags alone are used).  Sums are in 64 bits, in one
+ * order.  workspace: at least ll_grad_norm_workspace_bytes(n_tensors) bytes, 256-byte aligned.  An empty list has the norm 0.
+ *
+ * ll_adamw: per element, with t the step, counted from 1,
+ *
+ *   g' = g min(1, max_norm / norm)                    (norm given: e.g. out_norm of ll_grad_norm; NULL: g)
+ *   m' = beta1 m + (1 - beta1) g',   v' = beta2 v + (1 - beta2) g'^2
+ *   p' = p (1 - rate decay) - rate / (1 - beta1^t) m' / ( sqrt(v') / sqrt(1 - beta2^t) + eps )
+ *
+ * in place of param, m and v, in fp32; copy (if given, for fp32 parameters) gets p' in bf16.  A norm that is infinite or NaN: the whole step is left
+ * out.  Without one, such a gradient makes NaN of its own element.
+ *
+ *   param  fp32, or bf16 (LL_TENSOR_PARAM_BF16): rounded stochastically
+ *   grad   fp32, or bf16 (LL_TENSOR_GRAD_BF16)
+ *   m, v   fp32, m_scale and v_scale NULL; or (LL_TENSOR_STATE_8BIT) m in e4m3 and v in e5m2, one byte an element, with fp32 m_scale and v_scale, one for
+ *          LL_STATE_BLOCK elements (the last may be fewer): the value is code times scale.  Scales are the smallest powers of two that fit the
+ *          block; codes are rounded stochastically, but a positive v never to 0.  All zeros, or the states of an earlier call, to begin with
+ *   seed   of the stochastic rounding, with the step, the tensor's place in the list and the element's in the tensor: the same call gives the same bits
+ *   step   of this call, from 1; or, with a clock, nothing
+ *   clock  int64 [4] on the device, or NULL: clock[0] steps have been done, the call makes it one more (not where a step is left out) and takes t from it, so that a
+ *          captured call counts its replays; the other three are the call's own.  One call at a time
+ *   device_rate  fp32 [1] on the device, or NULL: in place of options->rate, with a clock only
+ * rate and decay finite, not negative; betas in [0, 1); eps positive; max_norm positive (infinity: no clipping).
+ */
+#define LL_STATE_BLOCK       256
+#define LL_TENSOR_MAX        ((int64_t)1 << 33)
+#define LL_TENSOR_PARAM_BF16 1u
+#define LL_TENSOR_GRAD_BF16  2u
+#define LL_TENSOR_STATE_8BIT 4u
+typedef struct ll_tensor {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  int64_t n;        /* elements */
+  uint32_t flags;   /* LL_TENSOR_* */
+} ll_tensor;
+typedef struct ll_adamw_options {
+  double rate, beta1, beta2, eps, decay, max_norm;
+  int64_t step;
+  uint32_t seed;
+} ll_adamw_options;
+size_t ll_grad_norm_workspace_bytes(int32_t n_tensors);
+int ll_grad_norm(const ll_tensor* tensors, int32_t n_tensors, void* workspace, size_t workspace_bytes, float* out_norm, void* stream);
+int ll_adamw(const ll_tensor* tensors, int32_t n_tensors, const ll_adamw_options* options, const float* norm, int64_t* clock,
+             const float* device_rate, void* stream);
+
 /* Text for an LL_E* code (static storage, never NULL). */
 const char* ll_error_string(int code);
 

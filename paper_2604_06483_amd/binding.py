@@ -17,6 +17,8 @@ LL_OK, LL_EINVAL, LL_EWORKSPACE, LL_EHIP, LL_ESCRATCH = 0, -1, -2, -3, -4
 LL_KMAX = 32
 LL_STATIC_SCRATCH_BYTES = 64 << 20
 LL_LIST_MAX = 64
+LL_STATE_BLOCK = 256
+LL_TENSOR_PARAM_BF16, LL_TENSOR_GRAD_BF16, LL_TENSOR_STATE_8BIT = 1, 2, 4
 LL_PREFERENCE = {"logistic": 0, "hinge": 1, "square": 2}
 LL_FLAG_TOPK_SOFTMAX = 1
 LL_FLAG_REGISTER_STAGED = 2
@@ -40,6 +42,14 @@ class LLError(RuntimeError):
 
 class ll_capture_shape(Structure):
     _fields_ = [("L", c_int32), ("C", c_int32), ("T", c_int64), ("d", c_int32)]
+
+
+class ll_tensor(Structure):
+    _fields_ = [(n, c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", c_int64), ("flags", ctypes.c_uint32)]
+
+
+class ll_adamw_options(Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("rate", "beta1", "beta2", "eps", "decay", "max_norm")] + [("step", c_int64), ("seed", ctypes.c_uint32)]
 
 
 _PROJECT_ARGS = [POINTER(ll_shape), c_void_p, c_size_t, c_void_p, c_void_p, c_void_p, c_float, c_int,
@@ -116,6 +126,12 @@ def lib() -> ctypes.CDLL:
         L.ll_preference_workspace_bytes.restype = c_size_t
         L.ll_preference.argtypes = lens[:6] + [c_void_p] * 2 + [c_int32] + [c_void_p] * 2 + [c_int] * 2 + [c_float] * 2 + [c_void_p] * 5
         L.ll_preference.restype = c_int
+        L.ll_grad_norm_workspace_bytes.argtypes = [c_int32]
+        L.ll_grad_norm_workspace_bytes.restype = c_size_t
+        L.ll_grad_norm.argtypes = [POINTER(ll_tensor), c_int32, c_void_p, c_size_t, c_void_p, c_void_p]
+        L.ll_grad_norm.restype = c_int
+        L.ll_adamw.argtypes = [POINTER(ll_tensor), c_int32, POINTER(ll_adamw_options)] + [c_void_p] * 4
+        L.ll_adamw.restype = c_int
         L.ll_error_string.argtypes = [c_int]
         L.ll_error_string.restype = c_char_p
         L.ll_last_hip_error.argtypes = []
@@ -651,3 +667,116 @@ def ll_preference(rows, W_U, ids, offsets, *, ref_logp=None, weight=None, beta=0
     if rc != LL_OK:
         raise LLError(rc, "ll_preference")
     return loss, score, logp, out if out is None or out.shape == rows.shape else out.reshape(rows.shape)
+
+
+class TensorList:
+    """The tensors that a step is about, as ll_grad_norm and ll_adamw take them, checked and marshalled once: `grads` alone for the norm; for a
+    step also `params`, `m` and `v` (fp32; or m in float8_e4m3fn and v in float8_e5m2 with fp32 `m_scale` and `v_scale`, one for LL_STATE_BLOCK
+    elements) and, where fp32 parameters have one, a bf16 copy each (`copies`; None: none).  The tensors are kept, and worked on in place.
+    """
+
+    def __init__(self, grads, params=None, m=None, v=None, m_scale=None, v_scale=None, copies=None):
+        kinds = {"params": params, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies}
+        self.grads = list(grads)
+        count = len(self.grads)
+        for name, of in kinds.items():
+            of = [None] * count if of is None else list(of)
+            if len(of) != count:
+                raise ValueError(f"{name}: {len(of)} tensors, expected {count}")
+            setattr(self, name, of)
+        self.whole = params is not None
+        if self.whole and (m is None or v is None):
+            raise ValueError("a step needs m and v")
+        self.device = self.grads[0].device if count else torch.device("cuda")
+        self.array = (ll_tensor * max(count, 1))()
+        written = set()
+        for i, g in enumerate(self.grads):
+            t = self.array[i]
+            t.n, t.grad = g.numel(), g.data_ptr()
+            t.flags = self._grad_flag(g, f"grads[{i}]")
+            if not self.whole:
+                continue
+            p = self.params[i]
+            _check(p, p.dtype if p.dtype in (_F32, _BF16) else _F32, f"params[{i}]", g.shape)
+            eight = self.m[i].dtype == torch.float8_e4m3fn
+            _check(self.m[i], torch.float8_e4m3fn if eight else _F32, f"m[{i}]", g.shape)
+            _check(self.v[i], torch.float8_e5m2 if eight else _F32, f"v[{i}]", g.shape)
+            blocks = (t.n + LL_STATE_BLOCK - 1) // LL_STATE_BLOCK
+            for name, of in (("m_scale", self.m_scale), ("v_scale", self.v_scale)):
+                if eight:
+                    _check(of[i], _F32, f"{name}[{i}]", (blocks,))
+                elif of[i] is not None:
+                    raise ValueError(f"{name}[{i}]: states in fp32 have none")
+            if self.copies[i] is not None:
+                if p.dtype != _F32:
+                    raise ValueError(f"copies[{i}]: only fp32 parameters have one")
+                _check(self.copies[i], _BF16, f"copies[{i}]", g.shape)
+            t.param, t.m, t.v, t.m_scale, t.v_scale, t.copy = (_ptr(x) for x in (p, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i], self.copies[i]))
+            t.flags |= (LL_TENSOR_PARAM_BF16 if p.dtype == _BF16 else 0) | (LL_TENSOR_STATE_8BIT if eight else 0)
+            for x in (t.param, t.m, t.v, t.copy):
+                if t.n and x in written:
+                    raise ValueError(f"tensor {i}: the same memory is in the list twice")
+                written.add(x) if x else None
+
+    @staticmethod
+    def _grad_flag(g, name):
+        if isinstance(g, _Tensor) and g.dtype == _BF16:
+            _check(g, _BF16, name)
+            return LL_TENSOR_GRAD_BF16
+        _check(g, _F32, name)
+        return 0
+
+    def set_grads(self, grads):
+        """Other gradients of the same shapes (a backward pass that made new tensors)."""
+        grads = list(grads)
+        if len(grads) != len(self.grads):
+            raise ValueError(f"grads: {len(grads)} tensors, expected {len(self.grads)}")
+        for i, (g, old) in enumerate(zip(grads, self.grads)):
+            if g is old:
+                continue
+            flag = self._grad_flag(g, f"grads[{i}]")
+            if g.shape != old.shape:
+                raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, expected {tuple(old.shape)}")
+            self.array[i].grad = g.data_ptr()
+            self.array[i].flags = (self.array[i].flags & ~LL_TENSOR_GRAD_BF16) | flag
+        self.grads = grads
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def ll_grad_norm_workspace_bytes(tensors) -> int:
+    return int(lib().ll_grad_norm_workspace_bytes(len(tensors)))
+
+
+def ll_grad_norm(tensors, *, workspace=None, stream=None, out=None):
+    """Norm of all gradients of a TensorList (or of a sequence of fp32 and bf16 tensors): [1] fp32, on the GPU."""
+    if not isinstance(tensors, TensorList):
+        tensors = TensorList(tensors)
+    ws = _workspace(workspace, lambda: ll_grad_norm_workspace_bytes(tensors), tensors.device, stream)
+    if out is None:
+        out = _empty((1,), _F32, tensors.device, stream)
+    else:
+        _check(out, _F32, "out", (1,))
+    rc = (_lib or lib()).ll_grad_norm(tensors.array, len(tensors), ws.data_ptr(), ws.numel() * ws.element_size(), out.data_ptr(), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_grad_norm")
+    return out
+
+
+def ll_adamw(tensors, step=None, *, rate=1e-3, betas=(0.9, 0.999), eps=1e-8, decay=0.0, norm=None, max_norm=float("inf"), seed=0, clock=None,
+             device_rate=None, stream=None):
+    """One AdamW step over a TensorList, in place.  step: of this call, from 1; or clock: int64 [4] on the GPU, zeros to begin with, which counts
+    the steps (a captured call's replays).  norm [1] fp32 (of ll_grad_norm): clipped to max_norm, and no step where it is not finite.  seed: of the
+    stochastic rounding of 8-bit states and bf16 parameters.  device_rate [1] fp32: in place of rate, with a clock."""
+    if not isinstance(tensors, TensorList) or not tensors.whole:
+        raise TypeError("tensors: need a TensorList with params, m and v")
+    if (step is None) == (clock is None):
+        raise ValueError("need a step or a clock")
+    for t, dtype, name, size in ((norm, _F32, "norm", (1,)), (clock, torch.int64, "clock", (4,)), (device_rate, _F32, "device_rate", (1,))):
+        if t is not None:
+            _check(t, dtype, name, size)
+    options = ll_adamw_options(rate, betas[0], betas[1], eps, decay, max_norm, 0 if step is None else step, seed & 0xFFFFFFFF)
+    rc = (_lib or lib()).ll_adamw(tensors.array, len(tensors), options, _ptr(norm), _ptr(clock), _ptr(device_rate), _stream(stream))
+    if rc != LL_OK:
+        raise LLError(rc, "ll_adamw")
