@@ -3,9 +3,11 @@
 //
 //   l = log softmax(a W^T / T)[id],   dA = c / T (W_id - sum_v p_v W_v),   c = d loss / d l
 //
-// Both products are those of distillation from a list of one token (ll_learn.hip): the first leaves P = 2^(x - base) behind it, the second
-// multiplies P, with the row's own token put into it, by W_U.  What is new is c.  Nothing of it is needed before the second product's sums
-// are rounded, where it is a factor of the row, so that the logits are formed once: with the log-probabilities and their gradient as two
+// Both products are those of distillation (ll_learn.hip): the first leaves P = 2^(x - base) behind it in bf16, the second multiplies P by W_U.
+// The row's own token is left out of P and its whole part, p - 1, which outweighs all others', joins the sums in fp32: rounded into P it would
+// be most of the gradient's error (rms, of the gradient: 0.0026 with it in P, 0.0017 without, which is the result's own rounding).
+// What is new is c.  Nothing of it is needed before the second product's sums are rounded, where it is a factor of the row, so that the logits
+// are formed once: with the log-probabilities and their gradient as two
 // calls there is a third product (1500 rows, d = 4096, V = 128256: see the figures at the entry points).
 //
 // A policy's c is the row's own.  A preference's is known when every row of its pair has been through W_U.  Up to one pass of rows the
@@ -65,7 +67,8 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t r
 }
 
 // A row a workgroup: its log-probability and what its gradient is made of.  terms.a is the gradient's factor without c, terms.factor with it
-// (a preference's comes later: ll_preference_pairs_kernel).  P as in ll_distill_rows_kernel, with one entry of share 1.
+// (a preference's comes later: ll_preference_pairs_kernel), terms.b the own token's part, (p - 1) 2^(lse2 - base), whose place in P is 0.  Tiles
+// of P are brought to one base as in ll_distill_rows_kernel.
 template <bool POLICY>
 __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p) {
   __shared__ float shared_base;
@@ -74,7 +77,6 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
   const int lane = threadIdx.x & 63;
   int id = -1;
   bool live = false;
-  float put = 0.f;
   if (threadIdx.x < 64) {
     const RowStats r = join_stats(p.stride == 1 ? p.stats + row * p.parts : p.stats + row, p.parts, lane, p.stride);
     id = p.ids[row];
@@ -93,12 +95,12 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
       if (POLICY) p.policy.loss[row] = t.loss;
       if (p.terms != nullptr) {
         const float unit = -p.inv_t * (p.P == nullptr ? 1.f : __builtin_amdgcn_exp2f(base - r.lse2));
-        p.terms[row] = {r.lse2, unit, 0.f, POLICY && live ? unit * t.c : 0.f};
+        const float own = __builtin_amdgcn_exp2f(l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
+        p.terms[row] = {r.lse2, unit, own, POLICY && live ? unit * t.c : 0.f};
       }
       shared_moved = live && other;
       shared_base = base;
     }
-    put = __builtin_amdgcn_exp2f(l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
   }
   if (p.P == nullptr) return;
   __syncthreads();
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
     tiles_to_base(at, p.ldp, p.moved + row * p.tiles, shared_base);
     __syncthreads();
   }
-  if (threadIdx.x == 0 && live) at[place_in_p(id)] = (uint16_t)pack_bf16(put, 0.f);
+  if (threadIdx.x == 0 && live) at[place_in_p(id)] = 0;
 }
 
 struct PairArgs {
@@ -189,6 +191,31 @@ __global__ __launch_bounds__(256) void ll_preference_pairs_kernel(const PairArgs
   }
 }
 
+// The slices' sums joined, in order, and the own token's part; a row that takes no part gets zeros whatever W holds.
+__global__ __launch_bounds__(256) void ll_answers_join_kernel(const float* __restrict__ part, int splits, int rows, int d, const int32_t* __restrict__ ids,
+                                                              const uint16_t* __restrict__ W, const RowTerms* __restrict__ terms,
+                                                              uint16_t* __restrict__ out) {
+  const int64_t row = blockIdx.y;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (c >= d) return;
+  const RowTerms t = terms[row];
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (t.factor != 0.f) {                       // (so the row has a token)
+    const uint2 w = *reinterpret_cast<const uint2*>(W + (int64_t)ids[row] * d + c);
+#pragma unroll 8
+    for (int q = 0; q < splits; ++q) {
+      const float4 x = *reinterpret_cast<const float4*>(part + ((int64_t)q * rows + row) * d + c);
+      s.x += x.x;
+      s.y += x.y;
+      s.z += x.z;
+      s.w += x.w;
+    }
+    s = make_float4(t.factor * fmaf(t.b, bf16_lo(w.x), s.x), t.factor * fmaf(t.b, bf16_hi(w.x), s.y), t.factor * fmaf(t.b, bf16_lo(w.y), s.z),
+                    t.factor * fmaf(t.b, bf16_hi(w.y), s.w));
+  }
+  *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+}
+
 // Few rows: the parts' sums joined, and the row's token.
 __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinArgs p, const RowTerms* __restrict__ terms) {
   __shared__ float scale[FEW_LEARN_STREAMS];
@@ -212,28 +239,23 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
 // ---------------------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------------------
-// What distillation from one token has, every row's terms, and where pairs take more rows than a pass the passes' sums.
+// What distillation from one token has, every row's terms, and where pairs take more rows than a pass every pass's sums.
 struct AnswerPlan {
   LearnPlan l;
-  bool keep;
-  int64_t passes;
-  size_t pass_sums, terms, sums, total;
+  bool keep;                // the sums of all passes are joined behind the last
+  size_t terms, total;
 };
 
 AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
   AnswerPlan a = {};
-  a.l = plan_for(s, 1, needs);
-  a.passes = (s->N + a.l.pass_rows - 1) / a.l.pass_rows;
-  a.keep = pairs && needs == BACKWARD && a.passes > 1;
+  a.l = plan_for(s, 1, needs, 1);
+  const int64_t passes = (s->N + a.l.pass_rows - 1) / a.l.pass_rows;
+  a.keep = pairs && needs == BACKWARD && passes > 1;
+  if (a.keep) a.l = plan_for(s, 1, needs, passes);
   a.total = a.l.total;
   if (needs == FORWARD) return a;
   a.terms = a.total;
   a.total = align_up(a.total + (size_t)(s->N > 0 ? s->N : 1) * sizeof(RowTerms), 256);
-  if (a.keep) {
-    a.sums = a.total;
-    a.pass_sums = align_up((size_t)a.l.back_splits * a.l.pass_rows * s->d * sizeof(float), 256);
-    a.total += a.pass_sums * (size_t)a.passes;
-  }
   return a;
 }
 
@@ -285,6 +307,14 @@ int answer_few_join(const Pass& p, const AnswerPlan& a, FewJoinArgs& j, const Ro
   return LL_OK;
 }
 
+// The gradient of a pass from its sums.
+int answer_join(const Pass& p, const AnswerPlan& a, const float* sums, const int32_t* ids, const RowTerms* terms, uint16_t* out) {
+  hipLaunchKernelGGL(ll_answers_join_kernel, dim3((p.shape->d + 1023) / 1024, p.n), dim3(256), 0, p.stream, sums, a.l.back_splits, p.n, p.shape->d, ids,
+                     p.W, terms, out);
+  LL_HIP_CHECK(hipGetLastError());
+  return LL_OK;
+}
+
 bool finite(float x) { return x - x == 0.f; }
 
 }  // namespace
@@ -315,7 +345,9 @@ int ll_policy(const ll_shape* shape, void* workspace, size_t workspace_bytes, co
     LL_TRY(answer_rows<true>(p, a, workspace, ids + r0, temperature, out_logp + r0, terms, policy, j));
     if (!grad) return LL_OK;
     if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
-    return p.back((uint16_t*)out_grad + r0 * shape->d, terms, at<float>(workspace, a.l.part));
+    float* const sums = at<float>(workspace, a.l.part);
+    LL_TRY(p.back(nullptr, sums));
+    return answer_join(p, a, sums, ids + r0, terms, (uint16_t*)out_grad + r0 * shape->d);
   });
 }
 
@@ -348,22 +380,22 @@ int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   };
-  const auto sums_of = [&](int64_t r0) { return at<float>(workspace, a.sums + (size_t)(r0 / a.l.pass_rows) * a.pass_sums); };
+  const auto sums_of = [&](int64_t r0) { return at<float>(workspace, a.l.part) + (a.keep ? r0 * a.l.back_splits * shape->d : 0); };
   const bool between = grad && shape->N > 0 && !a.keep;      // one pass: the pairs come between the products
   LL_TRY(for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream, [&](const Pass& p, int64_t r0) -> int {
     FewJoinArgs j = {};
     LL_TRY(answer_rows<false>(p, a, workspace, ids + r0, temperature, out_logp + r0, grad ? terms + r0 : nullptr, PolicyArgs{}, j));
     if (!grad) return LL_OK;
-    if (a.keep) return p.back(nullptr, terms + r0, sums_of(r0));
-    LL_TRY(pairs());
+    if (!a.keep) LL_TRY(pairs());
     if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
-    return p.back((uint16_t*)out_grad, terms, at<float>(workspace, a.l.part));
+    LL_TRY(p.back(nullptr, sums_of(r0)));
+    return a.keep ? LL_OK : answer_join(p, a, sums_of(r0), ids, terms, (uint16_t*)out_grad);
   }));
   if (between) return LL_OK;
   LL_TRY(pairs());
   if (!a.keep) return LL_OK;
   return for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream,
-                    [&](const Pass& p, int64_t r0) -> int { return p.join((uint16_t*)out_grad + r0 * shape->d, terms + r0, sums_of(r0)); });
+                    [&](const Pass& p, int64_t r0) -> int { return answer_join(p, a, sums_of(r0), ids + r0, terms + r0, (uint16_t*)out_grad + r0 * shape->d); });
 }
 
 }  // extern "C"

@@ -230,7 +230,8 @@ int slices(int64_t tiles, int stages, int rows, int d, double stage_us) {
   return best;
 }
 
-LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
+// sums_of: the passes whose sums of the product backwards are kept, or 0: as many as the call itself needs.
+LearnPlan plan_for(const ll_shape* s, int k, Needs needs, int64_t sums_of = 0) {
   LearnPlan l = {};
   const int64_t N = s->N > 0 ? s->N : 1;
   const int64_t passes = (N + PASS_ROWS - 1) / PASS_ROWS, each = (N + passes - 1) / passes;
@@ -272,7 +273,7 @@ LearnPlan plan_for(const ll_shape* s, int k, Needs needs) {
     l.terms = take(rows * sizeof(RowTerms));
     l.moved = take(rows * l.tiles * sizeof(float));
     l.P = take(rows * l.ldp * 2);
-    l.part = take(l.back_splits > 1 ? rows * l.back_splits * s->d * sizeof(float) : 0);
+    l.part = take((l.back_splits > 1 || sums_of > 0 ? rows * l.back_splits * s->d * sizeof(float) : 0) * (size_t)(sums_of > 1 ? sums_of : 1));
     l.list = take(rows * k * sizeof(float2));
   }
   l.total = off;
@@ -372,8 +373,8 @@ struct Pass {
     return LL_OK;
   }
 
-  // P to the gradient of the rows; or, without `out`, its product alone, a slice of the vocabulary after the other, to `part`.
-  int back(uint16_t* out, const RowTerms* terms, float* part) const {
+  // P to the gradient of the rows; or, without `out`, its product alone to `part`, a slice of the vocabulary after the other.
+  int back(uint16_t* out, float* part) const {
     LearnBackArgs p = {};
     p.A = at<uint16_t>(ws, l.P);
     p.W = W;
@@ -387,18 +388,20 @@ struct Pass {
     p.row_blocks = (n + l.block_rows - 1) / l.block_rows;
     p.col_blocks = l.col_blocks;
     p.out = p.splits == 1 ? out : nullptr;
-    p.terms = terms;
+    p.terms = at<RowTerms>(ws, l.terms);
     const size_t lds = LEARN_LDS;
     const LearnBackKernel kernel = learn_back_kernel(past_caches(), l.row_tiles);
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); rc != LL_OK) return rc;
     const unsigned groups = (unsigned)((p.row_blocks * p.col_blocks * p.splits + NUM_XCD - 1) / NUM_XCD * NUM_XCD);
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(NTHREADS), lds, stream, p);
     LL_HIP_CHECK(hipGetLastError());
-    return out != nullptr && p.out == nullptr ? join(out, terms, part) : LL_OK;
+    return LL_OK;
   }
-  int back(uint16_t* out) const { return back(out, at<RowTerms>(ws, l.terms), at<float>(ws, l.part)); }
-  int join(uint16_t* out, const RowTerms* terms, const float* part) const {
-    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 1023) / 1024, n), dim3(256), 0, stream, part, l.back_splits, n, shape->d, terms, out);
+  int back(uint16_t* out) const {
+    float* const part = at<float>(ws, l.part);
+    if (const int rc = back(out, part); rc != LL_OK || l.back_splits == 1) return rc;
+    hipLaunchKernelGGL(ll_learn_join_kernel, dim3((shape->d + 1023) / 1024, n), dim3(256), 0, stream, part, l.back_splits, n, shape->d,
+                       at<RowTerms>(ws, l.terms), out);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   }
