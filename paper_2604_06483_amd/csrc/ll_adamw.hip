@@ -22,11 +22,19 @@ using namespace ll;
 
 constexpr int BLOCK = LL_STATE_BLOCK;          // of 8-bit states: four elements for each lane of a wavefront
 constexpr int THREADS = 256;
-constexpr int UNIT = THREADS * 4;              // elements of a workgroup at a time: four blocks
+#ifndef LL_BLOCKS
+#define LL_BLOCKS 1
+#endif
+constexpr int BLOCKS = LL_BLOCKS;                      // of a wavefront
+constexpr int UNIT_BLOCKS = THREADS / 64 * BLOCKS, UNIT = UNIT_BLOCKS * BLOCK;   // of a workgroup
 constexpr int STEP_TENSORS = 48;               // of one launch: their list is the kernel's argument (4 KB at most)
 constexpr int NORM_TENSORS = 160;
-constexpr int NORM_GROUPS = 1024;              // workgroups of a launch, and their partial sums
-constexpr int NORM_UNIT = 8192;
+constexpr int NORM_GROUPS = 2048;              // workgroups of a launch, and their partial sums
+constexpr int NORM_UNIT = 1024;                // elements, by a wavefront; four of them in flight
+#ifndef LL_ALONE
+#define LL_ALONE 128
+#endif
+constexpr int NORM_ALONE = LL_ALONE;           // units that one workgroup takes by itself
 
 // ---- numbers ------------------------------------------------------------------------------------
 // A permutation of 32-bit words: PCG's RXS-M-XS output function over its own multiplier and increment (M. O'Neill, 2014), used as a hash
@@ -52,21 +60,30 @@ __host__ __device__ __forceinline__ StepTerms step_terms(double rate, double bet
   return s;
 }
 
-// The smallest power of two, at least 2^-126, that brings `most` to at most 1.75 2^TOP.
+// The smallest power of two, at least 2^-126, that brings `most` to at most 1.75 2^TOP, as fp32's own exponent.  (It grows with `most`: the largest
+// of several numbers' is the largest number's.)
 template <int TOP>
-__device__ __forceinline__ int scale_exponent(float most) {
-  const uint32_t bits = __float_as_uint(most);
-  const int e = (int)(bits >> 23) - 127 - TOP + ((bits & 0x7FFFFF) > 0x600000 ? 1 : 0);
-  return e < -126 ? -126 : e;
+__device__ __forceinline__ uint32_t scale_exponent(float most) {
+  const int e = (int)((__float_as_uint(most) + 0x1FFFFF) >> 23) - TOP;   // (one more above 1.75)
+  return e < 1 ? 1 : e;
 }
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+__device__ __forceinline__ float power_of_two(uint32_t e) { return __uint_as_float(e << 23); }
 
-// x >= 0 as the code of an 8-bit float with MANTISSA bits, rounded up with the probability of its distance from the code below; r: 16 random bits.
-template <int MANTISSA, int BIAS>
-__device__ __forceinline__ uint32_t stochastic(float x, uint32_t r) {
-  constexpr int STEP = 23 - MANTISSA;
-  if (x >= __builtin_ldexpf(1.f, 1 - BIAS)) return ((__float_as_uint(x) + (r << (STEP - 16))) >> STEP) - ((127 - BIAS) << MANTISSA);
-  return (uint32_t)floorf(fmaf(x, __builtin_ldexpf(1.f, BIAS - 1 + MANTISSA), (float)r * (1.f / 65536.f)));   // (both products exact)
+// The hardware's own stochastic rounding is the one that the states are defined by: it adds the upper 20 (e4m3; 21, e5m2) bits of a word to
+// those that a number loses, a subnormal code's as well.  Sixteen of them are random here.
+template <int AT>
+__device__ __forceinline__ uint32_t put_e4m3(uint32_t codes, float x, uint32_t word) {
+  return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, (int)(word & 0xFFFF0000u), (int)codes, AT);
+}
+template <int AT>
+__device__ __forceinline__ uint32_t put_e5m2(uint32_t codes, float x, uint32_t word) {
+  return (uint32_t)__builtin_amdgcn_cvt_sr_bf8_f32(x, (int)(word << 16), (int)codes, AT);
+}
+
+// The larger of each half of two words.
+__device__ __forceinline__ uint32_t most_of_halves(uint32_t a, uint32_t b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
 // m' and v' of an element.  No product is contracted into a sum: what the 8-bit codes are made of is then the same number wherever the
@@ -92,7 +109,7 @@ struct StepTensor {
 
 struct StepArgs {
   StepTensor tensors[STEP_TENSORS];
-  uint32_t first[STEP_TENSORS + 1];     // units before each tensor
+  uint32_t first[64];                   // units before each tensor; more than any unit behind the last
   int count;
   StepTerms terms;
   const StepTerms* clock_terms;         // or nullptr: `terms`
@@ -111,6 +128,7 @@ __device__ __forceinline__ void load4(const void* from, int64_t at, int there, f
       x[0] = bf16_lo(q.x), x[1] = bf16_hi(q.x), x[2] = bf16_lo(q.y), x[3] = bf16_hi(q.y);
       return;
     }
+#pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = i < there ? __uint_as_float((uint32_t)p[i] << 16) : 0.f;
   } else {
     const float* p = static_cast<const float*>(from) + at;
@@ -119,6 +137,7 @@ __device__ __forceinline__ void load4(const void* from, int64_t at, int there, f
       x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
       return;
     }
+#pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = i < there ? p[i] : 0.f;
   }
 }
@@ -128,7 +147,9 @@ __device__ __forceinline__ void store4(float* to, int64_t at, int there, const f
     *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
     return;
   }
-  for (int i = 0; i < there; ++i) to[i] = x[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < there) to[i] = x[i];
 }
 __device__ __forceinline__ void store4(uint16_t* to, int64_t at, int there, uint2 q) {
   to += at;
@@ -136,7 +157,9 @@ __device__ __forceinline__ void store4(uint16_t* to, int64_t at, int there, uint
     *reinterpret_cast<uint2*>(to) = q;
     return;
   }
-  for (int i = 0; i < there; ++i) to[i] = (uint16_t)((i < 2 ? q.x : q.y) >> (16 * (i & 1)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < there) to[i] = (uint16_t)((i < 2 ? q.x : q.y) >> (16 * (i & 1)));
 }
 __device__ __forceinline__ void store4(uint8_t* to, int64_t at, int there, uint32_t q) {
   to += at;
@@ -144,107 +167,152 @@ __device__ __forceinline__ void store4(uint8_t* to, int64_t at, int there, uint3
     *reinterpret_cast<uint32_t*>(to) = q;
     return;
   }
-  for (int i = 0; i < there; ++i) to[i] = (uint8_t)(q >> (8 * i));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < there) to[i] = (uint8_t)(q >> (8 * i));
 }
 __device__ __forceinline__ uint32_t load_codes(const uint8_t* from, int64_t at, int there) {
   from += at;
   if (there == 4) return *reinterpret_cast<const uint32_t*>(from);
   uint32_t q = 0;
-  for (int i = 0; i < there; ++i) q |= (uint32_t)from[i] << (8 * i);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q |= i < there ? (uint32_t)from[i] << (8 * i) : 0u;
   return q;
 }
 
+// Four elements of a lane, a block of a wavefront; in 8 bits the states' codes, a byte an element.
+template <bool PARAM_BF16, bool GRAD_BF16, bool STATE_8>
+struct StepFour {
+  float g[4], w[4], m[4], v[4];
+  uint32_t mq, vq;
+  float m_by, v_by;
+
+  __device__ __forceinline__ void load(const StepTensor& t, int64_t at, int64_t block, int there) {
+    load4<PARAM_BF16>(t.param, at, there, w);
+    load4<GRAD_BF16>(t.grad, at, there, g);
+    if constexpr (STATE_8) {
+      mq = load_codes(static_cast<const uint8_t*>(t.m), at, there);
+      vq = load_codes(static_cast<const uint8_t*>(t.v), at, there);
+      m_by = t.m_scale[block];
+      v_by = t.v_scale[block];
+    } else {
+      load4<false>(t.m, at, there, m);
+      load4<false>(t.v, at, there, v);
+    }
+  }
+
+  __device__ __forceinline__ void step(const StepArgs& p, const StepTerms& terms, const StepTensor& t, float clip, int64_t at, int64_t block, int there) {
+    if constexpr (STATE_8) {
+      const auto m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, true);
+      const auto v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, true);
+      m[0] = m0[0] * m_by, m[1] = m0[1] * m_by, m[2] = m1[0] * m_by, m[3] = m1[1] * m_by;
+      v[0] = v0[0] * v_by, v[1] = v0[1] * v_by, v[2] = v1[0] * v_by, v[3] = v1[1] * v_by;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) moments(g[i] * clip, m[i], v[i], p.beta1, p.less1, p.beta2, p.less2);
+    // The quotient's last bits are far below the parameter's: the hardware's own root and reciprocal, each within one.  They take subnormal numbers
+    // for 0, which is nothing beside an eps that is large beside their roots.
+    if (p.eps >= 1e-10f) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = fmaf(-terms.rate * m[i], __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), terms.root, p.eps)), w[i] * terms.keep);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = fmaf(-terms.rate * m[i], 1.f / fmaf(sqrtf(v[i]), terms.root, p.eps), w[i] * terms.keep);
+    }
+    uint32_t words[4];
+    if (STATE_8 || PARAM_BF16) {
+      uint32_t key = scramble(terms.key + t.ordinal);
+      if ((at >> 32) != 0) key ^= scramble((uint32_t)(at >> 32));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) words[i] = scramble((uint32_t)(at + i) ^ key);
+    }
+    if constexpr (STATE_8) {
+      // (the largest of numbers passes NaN by; an infinite one, which says nothing of the others, is looked for apart)
+      float most_m = fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3]))), most_v = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+      if (__builtin_amdgcn_ballot_w64(!(fmaxf(most_m, most_v) < INFINITY)) != 0) {
+        asm volatile("; not worth doing ahead");
+        most_m = most_v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          most_m = fmaxf(most_m, fabsf(m[i]) < INFINITY ? fabsf(m[i]) : 0.f);
+          most_v = fmaxf(most_v, v[i] < INFINITY ? v[i] : 0.f);
+        }
+      }
+      const uint32_t e = wave_combine(scale_exponent<8>(most_m) | scale_exponent<15>(most_v) << 16, most_of_halves);
+      const uint32_t em = e & 0xFFFF, ev = e >> 16;
+      const float to_m = power_of_two(254 - em), to_v = power_of_two(254 - ev);
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = v[i] > 0.f ? fmaxf(v[i] * to_v, 0x1p-16f) : v[i];      // (at least the smallest code: rounded to it at least)
+      uint32_t a = 0, b = 0;
+      a = put_e4m3<0>(a, m[0] * to_m, words[0]);
+      a = put_e4m3<1>(a, m[1] * to_m, words[1]);
+      a = put_e4m3<2>(a, m[2] * to_m, words[2]);
+      a = put_e4m3<3>(a, m[3] * to_m, words[3]);
+      b = put_e5m2<0>(b, y[0], words[0]);
+      b = put_e5m2<1>(b, y[1], words[1]);
+      b = put_e5m2<2>(b, y[2], words[2]);
+      b = put_e5m2<3>(b, y[3], words[3]);
+      store4(static_cast<uint8_t*>(t.m), at, there, a);
+      store4(static_cast<uint8_t*>(t.v), at, there, b);
+      if ((threadIdx.x & 63) == 0) {
+        t.m_scale[block] = power_of_two(em);
+        t.v_scale[block] = power_of_two(ev);
+      }
+    } else {
+      store4(static_cast<float*>(t.m), at, there, m);
+      store4(static_cast<float*>(t.v), at, there, v);
+    }
+    if constexpr (PARAM_BF16) {
+      // A step is a thousandth of the parameter, a last bit of bf16 a 256th: stochastically here too.
+      uint32_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t bits = __float_as_uint(w[i]);
+        h[i] = fabsf(w[i]) < INFINITY ? (bits + (scramble(words[i]) & 0xFFFF)) >> 16 : pack_bf16(w[i], 0.f) & 0xFFFF;
+      }
+      store4(static_cast<uint16_t*>(t.param), at, there, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
+    } else {
+      store4(static_cast<float*>(t.param), at, there, w);
+      if (t.copy != nullptr) store4(t.copy, at, there, make_uint2(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])));
+    }
+  }
+};
+
 template <bool PARAM_BF16, bool GRAD_BF16, bool STATE_8>
 __global__ __launch_bounds__(THREADS) void ll_adamw_kernel(const StepArgs p) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t unit = blockIdx.x;
+  const int which = __popcll(__builtin_amdgcn_ballot_w64(unit >= p.first[lane])) - 1;
+  const StepTensor& t = p.tensors[which];
+  const int64_t n = t.n;
+  const int64_t block0 = (int64_t)(unit - p.first[which]) * UNIT_BLOCKS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * BLOCKS;
+  const bool whole = (block0 + BLOCKS) * BLOCK <= n;
+  StepFour<PARAM_BF16, GRAD_BF16, STATE_8> four[BLOCKS];
+  if (whole) {
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) four[k].load(t, (block0 + k) * BLOCK + 4 * lane, block0 + k, 4);
+  }
   float clip = 1.f;
   if (p.norm != nullptr) {
     const float norm = *p.norm;
     if (!(norm < INFINITY)) return;                       // gradients that overflowed, or NaN: no step
-    clip = norm > p.max_norm ? p.max_norm / norm : 1.f;
+    if (norm > p.max_norm) clip = p.max_norm / norm;
   }
-  const StepTerms terms = p.clock_terms != nullptr ? *p.clock_terms : p.terms;
-  int lo = 0, hi = p.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (blockIdx.x >= p.first[mid]) lo = mid;
-    else hi = mid - 1;
-  }
-  const StepTensor& t = p.tensors[lo];
-  const int64_t n = t.n, at = (int64_t)(blockIdx.x - p.first[lo]) * UNIT + 4 * (int)threadIdx.x;
-  const int64_t block = (int64_t)__builtin_amdgcn_readfirstlane((int)(at / BLOCK));
-  if (block * BLOCK >= n) return;                         // (a whole wavefront)
-  const int there = n - at >= 4 ? 4 : n > at ? (int)(n - at) : 0;
-  float g[4], w[4], m[4], v[4];
-  load4<PARAM_BF16>(t.param, at, there, w);
-  load4<GRAD_BF16>(t.grad, at, there, g);
-  if constexpr (STATE_8) {
-    const float m_by = t.m_scale[block], v_by = t.v_scale[block];
-    const uint32_t mq = load_codes(static_cast<const uint8_t*>(t.m), at, there), vq = load_codes(static_cast<const uint8_t*>(t.v), at, there);
-    const auto m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, true);
-    const auto v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, true);
-    m[0] = m0[0] * m_by, m[1] = m0[1] * m_by, m[2] = m1[0] * m_by, m[3] = m1[1] * m_by;
-    v[0] = v0[0] * v_by, v[1] = v0[1] * v_by, v[2] = v1[0] * v_by, v[3] = v1[1] * v_by;
-  } else {
-    load4<false>(t.m, at, there, m);
-    load4<false>(t.v, at, there, v);
-  }
+  StepTerms terms = p.terms;
+  if (p.clock_terms != nullptr) terms = *p.clock_terms;
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    moments(g[i] * clip, m[i], v[i], p.beta1, p.less1, p.beta2, p.less2);
-    // (the quotient's last bits are far below the parameter's: the hardware's own root and reciprocal, each within one)
-    const float by = __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), terms.root, p.eps));
-    w[i] = fmaf(-terms.rate * m[i], by, w[i] * terms.keep);
+    for (int k = 0; k < BLOCKS; ++k) four[k].step(p, terms, t, clip, (block0 + k) * BLOCK + 4 * lane, block0 + k, 4);
+    return;
   }
-  uint32_t words[4];
-  if (STATE_8 || PARAM_BF16) {
-    uint32_t key = scramble(terms.key + t.ordinal);
-    if ((at >> 32) != 0) key ^= scramble((uint32_t)(at >> 32));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) words[i] = scramble((uint32_t)(at + i) ^ key);
-  }
-  if constexpr (STATE_8) {
-    float most_m = 0.f, most_v = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      most_m = fmaxf(most_m, i < there && fabsf(m[i]) < INFINITY ? fabsf(m[i]) : 0.f);
-      most_v = fmaxf(most_v, i < there && v[i] < INFINITY ? v[i] : 0.f);
-    }
-    const int em = scale_exponent<8>(wave_max(most_m)), ev = scale_exponent<15>(wave_max(most_v));
-    const float to_m = power_of_two(-em), to_v = power_of_two(-ev);
-    uint32_t mq = 0, vq = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = m[i] * to_m, y = v[i] * to_v;
-      uint32_t a = min(stochastic<3, 7>(fabsf(x), words[i] >> 16), 0x7Eu), b = min(stochastic<2, 15>(y, words[i] & 0xFFFF), 0x7Bu);
-      if (!(fabsf(x) < INFINITY)) a = 0x7F;               // NaN, of its own element alone
-      if (!(y < INFINITY)) b = 0x7F;
-      b = max(b, y > 0.f ? 1u : 0u);
-      a |= __float_as_uint(x) >> 31 << 7;
-      mq |= a << (8 * i);
-      vq |= b << (8 * i);
-    }
-    store4(static_cast<uint8_t*>(t.m), at, there, mq);
-    store4(static_cast<uint8_t*>(t.v), at, there, vq);
-    if ((threadIdx.x & 63) == 0) {
-      t.m_scale[block] = power_of_two(em);
-      t.v_scale[block] = power_of_two(ev);
-    }
-  } else {
-    store4(static_cast<float*>(t.m), at, there, m);
-    store4(static_cast<float*>(t.v), at, there, v);
-  }
-  if constexpr (PARAM_BF16) {
-    // A step is a thousandth of the parameter, a last bit of bf16 a 256th: stochastically here too.
-    uint32_t h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t bits = __float_as_uint(w[i]);
-      h[i] = fabsf(w[i]) < INFINITY ? (bits + (scramble(words[i]) & 0xFFFF)) >> 16 : pack_bf16(w[i], 0.f) & 0xFFFF;
-    }
-    store4(static_cast<uint16_t*>(t.param), at, there, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
-  } else {
-    store4(static_cast<float*>(t.param), at, there, w);
-    if (t.copy != nullptr) store4(t.copy, at, there, make_uint2(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])));
+#pragma unroll 1
+  for (int64_t block = block0; block < block0 + BLOCKS && block * BLOCK < n; ++block) {   // (a whole wavefront)
+    const int64_t at = block * BLOCK + 4 * lane;
+    const int there = n - at >= 4 ? 4 : n > at ? (int)(n - at) : 0;
+    four[0].load(t, at, block, there);
+    four[0].step(p, terms, t, clip, at, block, there);
   }
 }
 
@@ -264,53 +332,108 @@ struct NormTensor {
 };
 struct NormArgs {
   NormTensor tensors[NORM_TENSORS];      // n below 0: -n values of bf16
-  uint32_t first[NORM_TENSORS + 1];      // units before each tensor
-  int count;
+  uint32_t first[192];                   // units before each tensor; more than any unit behind the last
+  uint32_t units;
   double* partial;                       // [workgroups]
+  float* norm;                           // or nullptr: of the one workgroup that there is
 };
-static_assert(sizeof(NormArgs) <= 4096, "a kernel's arguments");
+static_assert(sizeof(NormArgs) <= 4096 && NORM_TENSORS < 192, "a kernel's arguments");
 
 // The sum over the workgroup, in one order; thread 0 has it.
-__device__ __forceinline__ double sum_of_group(double x, double* red) {
+template <int T>
+__device__ __forceinline__ double sum_of_group(double x) {
+  __shared__ double red[T / 64];
   for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  double sum = 0.;
+#pragma unroll
+  for (int i = 0; i < T / 64; ++i) sum += red[i];
+  return sum;
 }
 
-// Sums of squares in 64 bits: the norm is then exact to its last bit whatever the order, and so is what a step is clipped by.
-__global__ __launch_bounds__(THREADS) void ll_grad_norm_kernel(const NormArgs p) {
-  __shared__ double red[THREADS / 64];
-  double sum = 0.;
-  for (uint32_t unit = blockIdx.x; unit < p.first[p.count]; unit += gridDim.x) {
-    int lo = 0, hi = p.count - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (unit >= p.first[mid]) lo = mid;
-      else hi = mid - 1;
-    }
-    const NormTensor t = p.tensors[lo];
-    const bool bf16 = t.n < 0;
-    const int64_t n = bf16 ? -t.n : t.n, from = (int64_t)(unit - p.first[lo]) * NORM_UNIT;
-    const int64_t end = from + NORM_UNIT < n ? from + NORM_UNIT : n;
-    for (int64_t at = from + 4 * (int)threadIdx.x; at < end; at += 4 * THREADS) {
-      float g[4];
-      const int there = end - at >= 4 ? 4 : (int)(end - at);
-      if (bf16) load4<true>(t.grad, at, there, g);
-      else load4<false>(t.grad, at, there, g);
+__device__ __forceinline__ void add_square(double& sum, float x) { sum = fma((double)x, (double)x, sum); }
+__device__ __forceinline__ void add_squares(double (&sum)[4], const float4 q) {
+  add_square(sum[0], q.x);
+  add_square(sum[1], q.y);
+  add_square(sum[2], q.z);
+  add_square(sum[3], q.w);
+}
+__device__ __forceinline__ void add_squares(double (&sum)[4], const uint4 q) {
+  add_squares(sum, make_float4(bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)));
+  add_squares(sum, make_float4(bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w)));
+}
+
+// Sums of squares in 64 bits: the norm is then exact to its last bit whatever the order, and so is what a step is clipped by.  A wavefront
+// takes four units, 8 or 16 KB in flight, one after the other where they are not all whole and of one tensor.
+template <int T>
+__global__ __launch_bounds__(T) void ll_grad_norm_kernel(const NormArgs p) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t wave = blockIdx.x * (T / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = gridDim.x * (T / 64);
+  double sum[4] = {0., 0., 0., 0.};
+  uint32_t begin = 1, end = 0;
+  const void* grad = nullptr;
+  int64_t n = 0;
+  bool bf16 = false;
+  const auto locate = [&](uint32_t unit) {
+    if (unit >= begin && unit < end) return;
+    int which = -1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum = fma((double)g[i], (double)g[i], sum);
+    for (int i = 0; i < 3; ++i) which += __popcll(__builtin_amdgcn_ballot_w64(unit >= p.first[64 * i + lane]));
+    begin = p.first[which];
+    end = p.first[which + 1];
+    grad = p.tensors[which].grad;
+    n = p.tensors[which].n;
+    bf16 = n < 0;
+    n = bf16 ? -n : n;
+  };
+  for (uint32_t unit = 4 * wave; unit < p.units; unit += 4 * waves) {
+    locate(unit);
+    const int64_t at = (int64_t)(unit - begin) * NORM_UNIT;
+    if (at + 4 * NORM_UNIT <= n) {
+      if (bf16) {
+        const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(grad) + at) + lane;
+        uint4 q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = from[64 * i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add_squares(sum, q[i]);
+      } else {
+        const float4* from = reinterpret_cast<const float4*>(static_cast<const float*>(grad) + at) + lane;
+        float4 q[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[i] = from[64 * i];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) add_squares(sum, q[i]);
+      }
+      continue;
+    }
+#pragma unroll 1
+    for (uint32_t u = unit; u < unit + 4 && u < p.units; ++u) {
+      locate(u);
+      const int64_t from = (int64_t)(u - begin) * NORM_UNIT + 4 * lane;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t e = from + 256 * i;
+        const int there = n - e >= 4 ? 4 : n > e ? (int)(n - e) : 0;
+        float g[4];
+        if (bf16) load4<true>(grad, e, there, g);
+        else load4<false>(grad, e, there, g);
+        add_squares(sum, make_float4(g[0], g[1], g[2], g[3]));
+      }
     }
   }
-  sum = sum_of_group(sum, red);
-  if (threadIdx.x == 0) p.partial[blockIdx.x] = sum;
+  const double all = sum_of_group<T>((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (threadIdx.x != 0) return;
+  if (p.norm != nullptr) *p.norm = (float)sqrt(all);
+  else p.partial[blockIdx.x] = all;
 }
 
 __global__ __launch_bounds__(THREADS) void ll_grad_norm_join_kernel(const double* __restrict__ partial, int parts, float* __restrict__ norm) {
-  __shared__ double red[THREADS / 64];
   double sum = 0.;
+#pragma unroll 8
   for (int i = threadIdx.x; i < parts; i += THREADS) sum += partial[i];
-  sum = sum_of_group(sum, red);
+  sum = sum_of_group<THREADS>(sum);
   if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
@@ -345,7 +468,8 @@ static_assert(LL_TENSOR_PARAM_BF16 == 1 && LL_TENSOR_GRAD_BF16 == 2 && LL_TENSOR
 
 // Units of one launch of a step: a grid has fewer than 2^32 threads.
 constexpr int64_t MOST_UNITS = ((int64_t)1 << 24) - 1;
-static_assert(MOST_ELEMENTS / UNIT <= MOST_UNITS && MOST_ELEMENTS / NORM_UNIT * NORM_TENSORS < (int64_t)1 << 31, "a tensor fits one, and units 32 bits");
+static_assert(MOST_ELEMENTS / UNIT <= MOST_UNITS, "a tensor fits one");
+static_assert(MOST_ELEMENTS / NORM_UNIT * NORM_TENSORS < (int64_t)1 << 31, "units, and a stride of the grid beyond them, in 32 bits");
 
 }  // namespace
 
@@ -363,20 +487,31 @@ int ll_grad_norm(const ll_tensor* tensors, int32_t n_tensors, void* workspace, s
   double* const partial = static_cast<double*>(workspace);
   int parts = 0;
   for (int32_t i = 0; i < n_tensors;) {
-    NormArgs a = {};
+    NormArgs a;
+    for (uint32_t& first : a.first) first = UINT32_MAX;
+    int count = 0;
     int64_t units = 0;
-    for (; i < n_tensors && a.count < NORM_TENSORS; ++i) {
+    const bool first_launch = i == 0;
+    for (; i < n_tensors && count < NORM_TENSORS; ++i) {
       const ll_tensor& t = tensors[i];
       if (t.n == 0) continue;
-      a.tensors[a.count] = {t.grad, (t.flags & LL_TENSOR_GRAD_BF16) != 0 ? -t.n : t.n};
-      a.first[a.count++] = (uint32_t)units;
+      a.tensors[count] = {t.grad, (t.flags & LL_TENSOR_GRAD_BF16) != 0 ? -t.n : t.n};
+      a.first[count++] = (uint32_t)units;
       units += (t.n + NORM_UNIT - 1) / NORM_UNIT;
-      a.first[a.count] = (uint32_t)units;
     }
-    if (a.count == 0) continue;
-    const int groups = (int)(units < NORM_GROUPS ? units : NORM_GROUPS);
+    if (count == 0) continue;
+    a.units = (uint32_t)units;
     a.partial = partial + parts;
-    hipLaunchKernelGGL(ll_grad_norm_kernel, dim3(groups), dim3(THREADS), 0, (hipStream_t)stream, a);
+    a.norm = nullptr;
+    if (first_launch && i == n_tensors && units <= NORM_ALONE) {
+      a.norm = out_norm;
+      hipLaunchKernelGGL(ll_grad_norm_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)stream, a);
+      LL_HIP_CHECK(hipGetLastError());
+      return LL_OK;
+    }
+    const int64_t wanted = (units + 15) / 16;             // four units for each of a workgroup's four wavefronts
+    const int groups = (int)(wanted < NORM_GROUPS ? wanted : NORM_GROUPS);
+    hipLaunchKernelGGL(ll_grad_norm_kernel<THREADS>, dim3(groups), dim3(THREADS), 0, (hipStream_t)stream, a);
     LL_HIP_CHECK(hipGetLastError());
     parts += groups;
   }
@@ -421,6 +556,7 @@ int ll_adamw(const ll_tensor* tensors, int32_t n_tensors, const ll_adamw_options
   for (uint32_t flags = 0; flags <= ALL_FLAGS; ++flags) {   // a launch for every kind of tensor that there is, and as many tensors as its arguments hold
     for (int32_t i = 0; i < n_tensors;) {
       a.count = 0;
+      for (uint32_t& first : a.first) first = UINT32_MAX;
       int64_t units = 0;
       for (; i < n_tensors && a.count < STEP_TENSORS; ++i) {
         const ll_tensor& t = tensors[i];
@@ -430,7 +566,6 @@ int ll_adamw(const ll_tensor* tensors, int32_t n_tensors, const ll_adamw_options
         a.tensors[a.count] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, static_cast<uint16_t*>(t.copy), t.n, (uint32_t)i};
         a.first[a.count++] = (uint32_t)units;
         units += more;
-        a.first[a.count] = (uint32_t)units;
       }
       if (a.count == 0) continue;
       hipLaunchKernelGGL(step_kernel(flags), dim3((unsigned)units), dim3(THREADS), 0, (hipStream_t)stream, a);
