@@ -22,28 +22,22 @@ using namespace ll;
 
 constexpr int BLOCK = LL_STATE_BLOCK;          // of 8-bit states: four elements for each lane of a wavefront
 constexpr int THREADS = 256;
-#ifndef LL_BLOCKS
-#define LL_BLOCKS 1
-#endif
-constexpr int BLOCKS = LL_BLOCKS;                      // of a wavefront
-constexpr int UNIT_BLOCKS = THREADS / 64 * BLOCKS, UNIT = UNIT_BLOCKS * BLOCK;   // of a workgroup
+constexpr int UNIT_BLOCKS = THREADS / 64, UNIT = UNIT_BLOCKS * BLOCK;   // of a workgroup, a block a wavefront (two or four: 3 to 7 % slower)
 constexpr int STEP_TENSORS = 48;               // of one launch: their list is the kernel's argument (4 KB at most)
 constexpr int NORM_TENSORS = 160;
 constexpr int NORM_GROUPS = 2048;              // workgroups of a launch, and their partial sums
 constexpr int NORM_UNIT = 1024;                // elements, by a wavefront; four of them in flight
-#ifndef LL_ALONE
-#define LL_ALONE 128
-#endif
-constexpr int NORM_ALONE = LL_ALONE;           // units that one workgroup takes by itself
+constexpr int NORM_ALONE = 128;                // units that one workgroup takes by itself
 
 // ---- numbers ------------------------------------------------------------------------------------
 // A permutation of 32-bit words: PCG's RXS-M-XS output function over its own multiplier and increment (M. O'Neill, 2014), used as a hash
 // of a counter.
-__host__ __device__ __forceinline__ uint32_t scramble(uint32_t x) {
-  const uint32_t s = x * 747796405u + 2891336453u;
+constexpr uint32_t SCRAMBLE = 747796405u, SCRAMBLE_MORE = 2891336453u;
+__host__ __device__ __forceinline__ uint32_t scramble_state(uint32_t s) {
   const uint32_t w = ((s >> ((s >> 28) + 4)) ^ s) * 277803737u;
   return (w >> 22) ^ w;
 }
+__host__ __device__ __forceinline__ uint32_t scramble(uint32_t x) { return scramble_state(x * SCRAMBLE + SCRAMBLE_MORE); }
 
 // What all tensors of a step share.
 struct StepTerms {
@@ -118,13 +112,35 @@ struct StepArgs {
 };
 static_assert(sizeof(StepArgs) <= 4096, "a kernel's arguments");
 
-// Four elements, those that there are.
+// Past the caches: a step's tensors are read once and written once, and what is read between two steps is far more than the caches hold.  Both
+// ways or not at all (us, loads and stores through the caches | loads past them | stores | both: eight d = 2560 layers in fp32 292 | 294 | 291 |
+// 267; twelve of d = 4096, 8 bits 576 | 580 | 559 | 515; lists that the caches would hold see no difference).
+template <int BYTES>
+struct Word {
+  typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4)));
+};
+template <>
+struct Word<4> {
+  typedef uint32_t type;
+};
+template <class V>
+__device__ __forceinline__ V load_past(const void* from) {
+  typedef typename Word<sizeof(V)>::type T;
+  return __builtin_bit_cast(V, __builtin_nontemporal_load(static_cast<const T*>(from)));
+}
+template <class V>
+__device__ __forceinline__ void store_past(void* to, V x) {
+  typedef typename Word<sizeof(V)>::type T;
+  __builtin_nontemporal_store(__builtin_bit_cast(T, x), static_cast<T*>(to));
+}
+
+// A lane's four elements of those from `from` on, as many as there are.
 template <bool BF16>
-__device__ __forceinline__ void load4(const void* from, int64_t at, int there, float (&x)[4]) {
+__device__ __forceinline__ void load4(const void* from, uint32_t at, int there, float (&x)[4]) {
   if constexpr (BF16) {
     const uint16_t* p = static_cast<const uint16_t*>(from) + at;
     if (there == 4) {
-      const uint2 q = *reinterpret_cast<const uint2*>(p);
+      const uint2 q = load_past<uint2>(p);
       x[0] = bf16_lo(q.x), x[1] = bf16_hi(q.x), x[2] = bf16_lo(q.y), x[3] = bf16_hi(q.y);
       return;
     }
@@ -133,7 +149,7 @@ __device__ __forceinline__ void load4(const void* from, int64_t at, int there, f
   } else {
     const float* p = static_cast<const float*>(from) + at;
     if (there == 4) {
-      const float4 q = *reinterpret_cast<const float4*>(p);
+      const float4 q = load_past<float4>(p);
       x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
       return;
     }
@@ -141,39 +157,35 @@ __device__ __forceinline__ void load4(const void* from, int64_t at, int there, f
     for (int i = 0; i < 4; ++i) x[i] = i < there ? p[i] : 0.f;
   }
 }
-__device__ __forceinline__ void store4(float* to, int64_t at, int there, const float (&x)[4]) {
-  to += at;
+__device__ __forceinline__ void store4(float* to, int there, const float (&x)[4]) {
   if (there == 4) {
-    *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    store_past(to, make_float4(x[0], x[1], x[2], x[3]));
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i < there) to[i] = x[i];
 }
-__device__ __forceinline__ void store4(uint16_t* to, int64_t at, int there, uint2 q) {
-  to += at;
+__device__ __forceinline__ void store4(uint16_t* to, int there, uint2 q) {
   if (there == 4) {
-    *reinterpret_cast<uint2*>(to) = q;
+    store_past(to, q);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i < there) to[i] = (uint16_t)((i < 2 ? q.x : q.y) >> (16 * (i & 1)));
 }
-__device__ __forceinline__ void store4(uint8_t* to, int64_t at, int there, uint32_t q) {
-  to += at;
+__device__ __forceinline__ void store4(uint8_t* to, int there, uint32_t q) {
   if (there == 4) {
-    *reinterpret_cast<uint32_t*>(to) = q;
+    store_past(to, q);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i < there) to[i] = (uint8_t)(q >> (8 * i));
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* from, int64_t at, int there) {
-  from += at;
-  if (there == 4) return *reinterpret_cast<const uint32_t*>(from);
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* from, int there) {
+  if (there == 4) return load_past<uint32_t>(from);
   uint32_t q = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) q |= i < there ? (uint32_t)from[i] << (8 * i) : 0u;
@@ -187,21 +199,25 @@ struct StepFour {
   uint32_t mq, vq;
   float m_by, v_by;
 
-  __device__ __forceinline__ void load(const StepTensor& t, int64_t at, int64_t block, int there) {
-    load4<PARAM_BF16>(t.param, at, there, w);
-    load4<GRAD_BF16>(t.grad, at, there, g);
+  // block, and all that is made of it, is the wavefront's: the lane adds a constant to its addresses
+  static constexpr int PARAM = PARAM_BF16 ? 2 : 4, GRAD = GRAD_BF16 ? 2 : 4, STATE = STATE_8 ? 1 : 4;
+  static __device__ __forceinline__ char* of_block(const void* p, int64_t block, int bytes) { return (char*)p + block * (BLOCK * bytes); }
+
+  __device__ __forceinline__ void load(const StepTensor& t, int64_t block, uint32_t at, int there) {
+    load4<PARAM_BF16>(of_block(t.param, block, PARAM), at, there, w);
+    load4<GRAD_BF16>(of_block(t.grad, block, GRAD), at, there, g);
     if constexpr (STATE_8) {
-      mq = load_codes(static_cast<const uint8_t*>(t.m), at, there);
-      vq = load_codes(static_cast<const uint8_t*>(t.v), at, there);
+      mq = load_codes((const uint8_t*)of_block(t.m, block, STATE) + at, there);
+      vq = load_codes((const uint8_t*)of_block(t.v, block, STATE) + at, there);
       m_by = t.m_scale[block];
       v_by = t.v_scale[block];
     } else {
-      load4<false>(t.m, at, there, m);
-      load4<false>(t.v, at, there, v);
+      load4<false>(of_block(t.m, block, STATE), at, there, m);
+      load4<false>(of_block(t.v, block, STATE), at, there, v);
     }
   }
 
-  __device__ __forceinline__ void step(const StepArgs& p, const StepTerms& terms, const StepTensor& t, float clip, int64_t at, int64_t block, int there) {
+  __device__ __forceinline__ void step(const StepArgs& p, const StepTerms& terms, const StepTensor& t, float clip, int64_t block, uint32_t at, int there) {
     if constexpr (STATE_8) {
       const auto m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mq, true);
       const auto v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vq, true);
@@ -223,9 +239,12 @@ struct StepFour {
     uint32_t words[4];
     if (STATE_8 || PARAM_BF16) {
       uint32_t key = scramble(terms.key + t.ordinal);
-      if ((at >> 32) != 0) key ^= scramble((uint32_t)(at >> 32));
+      if ((block >> 24) != 0) key ^= scramble((uint32_t)(block >> 24));
+      // words[i] = scramble(element ^ key), the four elements' products formed from one
+      uint32_t product = (((uint32_t)block * BLOCK + at) ^ (key & ~3u)) * SCRAMBLE;
+      asm("" : "+v"(product));                              // (the compiler would have four products again)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) words[i] = scramble((uint32_t)(at + i) ^ key);
+      for (int i = 0; i < 4; ++i) words[i] = scramble_state(product + (((key & 3) ^ i) * SCRAMBLE + SCRAMBLE_MORE));
     }
     if constexpr (STATE_8) {
       // (the largest of numbers passes NaN by; an infinite one, which says nothing of the others, is looked for apart)
@@ -254,15 +273,15 @@ struct StepFour {
       b = put_e5m2<1>(b, y[1], words[1]);
       b = put_e5m2<2>(b, y[2], words[2]);
       b = put_e5m2<3>(b, y[3], words[3]);
-      store4(static_cast<uint8_t*>(t.m), at, there, a);
-      store4(static_cast<uint8_t*>(t.v), at, there, b);
+      store4((uint8_t*)of_block(t.m, block, STATE) + at, there, a);
+      store4((uint8_t*)of_block(t.v, block, STATE) + at, there, b);
       if ((threadIdx.x & 63) == 0) {
         t.m_scale[block] = power_of_two(em);
         t.v_scale[block] = power_of_two(ev);
       }
     } else {
-      store4(static_cast<float*>(t.m), at, there, m);
-      store4(static_cast<float*>(t.v), at, there, v);
+      store4((float*)of_block(t.m, block, STATE) + at, there, m);
+      store4((float*)of_block(t.v, block, STATE) + at, there, v);
     }
     if constexpr (PARAM_BF16) {
       // A step is a thousandth of the parameter, a last bit of bf16 a 256th: stochastically here too.
@@ -272,10 +291,10 @@ struct StepFour {
         const uint32_t bits = __float_as_uint(w[i]);
         h[i] = fabsf(w[i]) < INFINITY ? (bits + (scramble(words[i]) & 0xFFFF)) >> 16 : pack_bf16(w[i], 0.f) & 0xFFFF;
       }
-      store4(static_cast<uint16_t*>(t.param), at, there, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
+      store4((uint16_t*)of_block(t.param, block, PARAM) + at, there, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
     } else {
-      store4(static_cast<float*>(t.param), at, there, w);
-      if (t.copy != nullptr) store4(t.copy, at, there, make_uint2(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])));
+      store4((float*)of_block(t.param, block, PARAM) + at, there, w);
+      if (t.copy != nullptr) store4((uint16_t*)of_block(t.copy, block, 2) + at, there, make_uint2(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])));
     }
   }
 };
@@ -287,13 +306,13 @@ __global__ __launch_bounds__(THREADS) void ll_adamw_kernel(const StepArgs p) {
   const int which = __popcll(__builtin_amdgcn_ballot_w64(unit >= p.first[lane])) - 1;
   const StepTensor& t = p.tensors[which];
   const int64_t n = t.n;
-  const int64_t block0 = (int64_t)(unit - p.first[which]) * UNIT_BLOCKS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * BLOCKS;
-  const bool whole = (block0 + BLOCKS) * BLOCK <= n;
-  StepFour<PARAM_BF16, GRAD_BF16, STATE_8> four[BLOCKS];
-  if (whole) {
-#pragma unroll
-    for (int k = 0; k < BLOCKS; ++k) four[k].load(t, (block0 + k) * BLOCK + 4 * lane, block0 + k, 4);
-  }
+  const int64_t block = (int64_t)(unit - p.first[which]) * UNIT_BLOCKS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t left = n - block * BLOCK;
+  if (left <= 0) return;
+  StepFour<PARAM_BF16, GRAD_BF16, STATE_8> four;
+  const int there = left >= BLOCK ? 4 : max(0, min(4, (int)left - 4 * lane));
+  if (left >= BLOCK) four.load(t, block, 4 * lane, 4);
+  else four.load(t, block, 4 * lane, there);
   float clip = 1.f;
   if (p.norm != nullptr) {
     const float norm = *p.norm;
@@ -302,18 +321,8 @@ __global__ __launch_bounds__(THREADS) void ll_adamw_kernel(const StepArgs p) {
   }
   StepTerms terms = p.terms;
   if (p.clock_terms != nullptr) terms = *p.clock_terms;
-  if (whole) {
-#pragma unroll
-    for (int k = 0; k < BLOCKS; ++k) four[k].step(p, terms, t, clip, (block0 + k) * BLOCK + 4 * lane, block0 + k, 4);
-    return;
-  }
-#pragma unroll 1
-  for (int64_t block = block0; block < block0 + BLOCKS && block * BLOCK < n; ++block) {   // (a whole wavefront)
-    const int64_t at = block * BLOCK + 4 * lane;
-    const int there = n - at >= 4 ? 4 : n > at ? (int)(n - at) : 0;
-    four[0].load(t, at, block, there);
-    four[0].step(p, terms, t, clip, at, block, there);
-  }
+  if (left >= BLOCK) four.step(p, terms, t, clip, block, 4 * lane, 4);
+  else four.step(p, terms, t, clip, block, 4 * lane, there);
 }
 
 // A step that the GPU counts: clock[0] steps have been done; clock[1] and [2] take this one's terms.
@@ -417,8 +426,8 @@ __global__ __launch_bounds__(T) void ll_grad_norm_kernel(const NormArgs p) {
         const int64_t e = from + 256 * i;
         const int there = n - e >= 4 ? 4 : n > e ? (int)(n - e) : 0;
         float g[4];
-        if (bf16) load4<true>(grad, e, there, g);
-        else load4<false>(grad, e, there, g);
+        if (bf16) load4<true>(static_cast<const uint16_t*>(grad) + e, 0, there, g);
+        else load4<false>(static_cast<const float*>(grad) + e, 0, there, g);
         add_squares(sum, make_float4(g[0], g[1], g[2], g[3]));
       }
     }
