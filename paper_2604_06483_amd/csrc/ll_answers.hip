@@ -118,13 +118,55 @@ struct PairArgs {
   const float* logp;
   const float* ref_logp;    // or nullptr: 0
   const float* weight;      // or nullptr: 1
-  int64_t N;
+  int64_t N, pairs;
   int V, form, mean;
   float beta, smoothing;
   float* loss;
   float* score;             // [pairs, 2]
   RowTerms* terms;          // or nullptr: no gradient
 };
+
+// Rows of a sequence: [begin, end), brought into [0, N) whatever the offsets say.
+struct Sequence {
+  int64_t begin, end;
+};
+__device__ __forceinline__ Sequence sequence_of(const PairArgs& p, int64_t i) {
+  const int64_t b = p.offsets[i], e = p.offsets[i + 1];
+  Sequence s;
+  s.begin = b < 0 ? 0 : b > p.N ? p.N : b;
+  s.end = e < s.begin ? s.begin : e > p.N ? p.N : e;
+  return s;
+}
+
+// A pair's loss and d loss / d h from its scores.
+struct PairTerm {
+  float loss, slope;
+};
+__device__ __forceinline__ PairTerm pair_term(const PairArgs& p, const double (&score)[2]) {
+  const float h = (float)((double)p.beta * (score[0] - score[1]));
+  PairTerm t;
+  if (p.form == LL_PREFERENCE_LOGISTIC) {
+    const float e = expf(-fabsf(h)), soft = log1pf(e);
+    const float to = 1.f / (1.f + e), from = e / (1.f + e);        // sigmoids of |h| and of -|h|
+    const float up = h > 0.f ? to : from, down = h > 0.f ? from : to;
+    t.loss = (1.f - p.smoothing) * (soft + fmaxf(-h, 0.f)) + p.smoothing * (soft + fmaxf(h, 0.f));
+    t.slope = p.smoothing * up - (1.f - p.smoothing) * down;
+    if (h != h) t.loss = t.slope = h;
+  } else if (p.form == LL_PREFERENCE_HINGE) {
+    t.loss = h < 1.f ? 1.f - h : h > 1.f ? 0.f : h - h;            // (h - h: 0, or NaN of NaN)
+    t.slope = h < 1.f ? -1.f : h > 1.f ? 0.f : h - h;
+  } else {
+    const float off = (float)((score[0] - score[1]) - 0.5 / (double)p.beta);
+    t.loss = off * off;
+    t.slope = 2.f * off / p.beta;
+  }
+  return t;
+}
+// What the loss gains by the log-probability of a row of the pair's first (side 0) or second sequence.
+__device__ __forceinline__ float pair_c(const PairArgs& p, int64_t pair, float slope, double length, int side) {
+  const float w = p.weight != nullptr ? p.weight[pair] : 1.f;
+  return w == 0.f ? 0.f : w * slope * p.beta / (side == 0 ? (float)length : -(float)length);
+}
 
 __device__ __forceinline__ double group_total(double x, double* red) {
   for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
@@ -140,15 +182,13 @@ __device__ __forceinline__ double group_total(double x, double* red) {
 __global__ __launch_bounds__(256) void ll_preference_pairs_kernel(const PairArgs p) {
   __shared__ double red[4];
   const int64_t pair = blockIdx.x;
-  int64_t begin[2], end[2];
+  Sequence rows[2];
   double score[2], length[2];
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
-    const int64_t b = p.offsets[2 * pair + side], e = p.offsets[2 * pair + side + 1];
-    begin[side] = b < 0 ? 0 : b > p.N ? p.N : b;
-    end[side] = e < begin[side] ? begin[side] : e > p.N ? p.N : e;
+    rows[side] = sequence_of(p, 2 * pair + side);
     double sum = 0., count = 0.;
-    for (int64_t r = begin[side] + (int)threadIdx.x; r < end[side]; r += 256) {
+    for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256) {
       if (p.ids[r] < 0 || p.ids[r] >= p.V) continue;
       sum += (double)p.logp[r] - (p.ref_logp != nullptr ? (double)p.ref_logp[r] : 0.);
       count += 1.;
@@ -158,35 +198,17 @@ __global__ __launch_bounds__(256) void ll_preference_pairs_kernel(const PairArgs
     length[side] = p.mean && count > 1. ? count : 1.;
     score[side] = sum / length[side];
   }
-  const float h = (float)((double)p.beta * (score[0] - score[1]));
-  float loss, slope;
-  if (p.form == LL_PREFERENCE_LOGISTIC) {
-    const float e = expf(-fabsf(h)), soft = log1pf(e);
-    const float to = 1.f / (1.f + e), from = e / (1.f + e);        // sigmoids of |h| and of -|h|
-    const float up = h > 0.f ? to : from, down = h > 0.f ? from : to;
-    loss = (1.f - p.smoothing) * (soft + fmaxf(-h, 0.f)) + p.smoothing * (soft + fmaxf(h, 0.f));
-    slope = p.smoothing * up - (1.f - p.smoothing) * down;
-    if (h != h) loss = slope = h;
-  } else if (p.form == LL_PREFERENCE_HINGE) {
-    loss = h < 1.f ? 1.f - h : h - h;
-    slope = h < 1.f ? -1.f : h - h;
-    if (h > 1.f) loss = slope = 0.f;
-  } else {
-    const float off = (float)((score[0] - score[1]) - 0.5 / (double)p.beta);
-    loss = off * off;
-    slope = 2.f * off / p.beta;
-  }
+  const PairTerm t = pair_term(p, score);
   if (threadIdx.x == 0) {
-    p.loss[pair] = loss;
+    p.loss[pair] = t.loss;
     p.score[2 * pair] = (float)score[0];
     p.score[2 * pair + 1] = (float)score[1];
   }
   if (p.terms == nullptr) return;
-  const float w = p.weight != nullptr ? p.weight[pair] : 1.f;
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
-    const float c = w == 0.f ? 0.f : w * slope * p.beta / (side == 0 ? (float)length[side] : -(float)length[side]);
-    for (int64_t r = begin[side] + (int)threadIdx.x; r < end[side]; r += 256)
+    const float c = pair_c(p, pair, t.slope, length[side], side);
+    for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256)
       if (p.ids[r] >= 0 && p.ids[r] < p.V) p.terms[r].factor = c != 0.f ? p.terms[r].a * c : 0.f;
   }
 }
@@ -216,24 +238,78 @@ __global__ __launch_bounds__(256) void ll_answers_join_kernel(const float* __res
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
-// Few rows: the parts' sums joined, and the row's token.
-__global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinArgs p, const RowTerms* __restrict__ terms) {
+// Few rows: block (64 columns, row) forms the row's terms itself (a preference's from all rows', which are no more than its wavefronts), in
+// place of a launch or two of some 5 us each, then joins the parts' sums and the row's token.
+constexpr int FEW_MOST = 4;
+template <bool POLICY>
+__global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinArgs p, const AnswerArgs r, const PairArgs q) {
+  static_assert(FEW_MOST * 64 == 256, "a wavefront a row");
   __shared__ float scale[FEW_LEARN_STREAMS];
   __shared__ float share[1];
   __shared__ int id_of[1];
-  const int row = blockIdx.y;
-  const RowTerms t = terms[row];
-  for (int i = threadIdx.x; i < p.parts; i += 256) {
-    const float4 q = p.f.stats[(int64_t)i * p.stride + row];
-    scale[i] = q.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(q.x - t.lse2);
-  }
-  if (threadIdx.x == 0) {
-    const int id = p.f.list.ids[row];
-    share[0] = -1.f;
-    id_of[0] = id < p.f.list.V ? id : -1;
+  __shared__ float logp[FEW_MOST];
+  __shared__ float shared_ref, shared_c;
+  const int row = blockIdx.y, rows = gridDim.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int of_wave = POLICY ? row : wave;
+  if (POLICY ? wave == 0 : wave < rows) {
+    const RowStats stats = join_stats(r.stats + of_wave, r.parts, lane, r.stride);
+    const int id = r.ids[of_wave];
+    if (lane == 0) {
+      logp[POLICY ? 0 : wave] = id >= 0 && id < r.V ? fmaf(r.z[of_wave], r.to_log2, -stats.lse2) * LN2 : NAN;
+      if (of_wave == row) {
+        shared_ref = stats.lse2;
+        shared_c = 0.f;
+        share[0] = -1.f;
+        id_of[0] = id < r.V ? id : -1;
+      }
+    }
   }
   __syncthreads();
-  few_join_columns(p, row, t.factor, scale, share, id_of);
+  const bool valid = id_of[0] >= 0, writes = blockIdx.x == 0;
+  if (POLICY) {
+    if (threadIdx.x == 0) {
+      PolicyTerm t = {0.f, 0.f};
+      if (valid) t = policy_term(r.policy, row, logp[0]);
+      shared_c = t.c;
+      if (writes) {
+        r.logp[row] = logp[0];
+        r.policy.loss[row] = t.loss;
+      }
+    }
+  } else {
+    if (threadIdx.x == 0 && writes) r.logp[row] = logp[row];
+    for (int64_t pair = threadIdx.x; pair < q.pairs; pair += 256) {
+      Sequence of[2];
+      double score[2], length[2];
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        of[side] = sequence_of(q, 2 * pair + side);
+        double sum = 0., count = 0.;
+        for (int64_t i = of[side].begin; i < of[side].end; ++i) {
+          if (q.ids[i] < 0 || q.ids[i] >= q.V) continue;
+          sum += (double)logp[i] - (q.ref_logp != nullptr ? (double)q.ref_logp[i] : 0.);
+          count += 1.;
+        }
+        length[side] = q.mean && count > 1. ? count : 1.;
+        score[side] = sum / length[side];
+      }
+      const PairTerm t = pair_term(q, score);
+      if (writes && row == 0) {
+        q.loss[pair] = t.loss;
+        q.score[2 * pair] = (float)score[0];
+        q.score[2 * pair + 1] = (float)score[1];
+      }
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+        if (valid && row >= of[side].begin && row < of[side].end) shared_c = pair_c(q, pair, t.slope, length[side], side);
+    }
+  }
+  for (int i = threadIdx.x; i < p.parts; i += 256) {
+    const float4 part = p.f.stats[(int64_t)i * p.stride + row];
+    scale[i] = part.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(part.x - shared_ref);
+  }
+  __syncthreads();
+  few_join_columns(p, row, shared_c != 0.f ? -r.inv_t * shared_c : 0.f, scale, share, id_of);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -259,10 +335,10 @@ AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
   return a;
 }
 
-// The first product of a pass and its rows' terms; POLICY: and losses.
+// The first product of a pass and its rows' terms; POLICY: and losses.  Of few rows with a gradient, all there is.
 template <bool POLICY>
 int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids, float temperature, float* logp, RowTerms* terms,
-                const PolicyArgs& policy, FewJoinArgs& join) {
+                const PolicyArgs& policy, const PairArgs& pairs, void* out) {
   const LearnPlan& l = a.l;
   AnswerArgs r = {};
   r.ids = ids;
@@ -275,9 +351,16 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
   r.terms = terms;
   r.policy = policy;
   if (l.few) {
-    LL_TRY(terms != nullptr ? p.few<EXPS>(ids, join.f) : p.few<STATS>(ids, join.f));
-    r.parts = l.few_parts;
-    r.stride = l.few_rows;
+    FewJoinArgs j = {};
+    LL_TRY(terms != nullptr ? p.few<EXPS>(ids, j.f) : p.few<STATS>(ids, j.f));
+    j.parts = r.parts = l.few_parts;
+    j.stride = r.stride = l.few_rows;
+    j.out = (uint16_t*)out;
+    if (terms != nullptr) {
+      hipLaunchKernelGGL(ll_answers_few_join_kernel<POLICY>, dim3((p.shape->d + 63) / 64, p.n), dim3(256), 0, p.stream, j, r, pairs);
+      LL_HIP_CHECK(hipGetLastError());
+      return LL_OK;
+    }
   } else {
     hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
                        p.panel(), l.lda);
@@ -294,15 +377,6 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
     }
   }
   hipLaunchKernelGGL(ll_answers_rows_kernel<POLICY>, dim3(p.n), dim3(r.P != nullptr ? 256 : 64), 0, p.stream, r);
-  LL_HIP_CHECK(hipGetLastError());
-  return LL_OK;
-}
-
-int answer_few_join(const Pass& p, const AnswerPlan& a, FewJoinArgs& j, const RowTerms* terms, void* out) {
-  j.parts = a.l.few_parts;
-  j.stride = a.l.few_rows;
-  j.out = (uint16_t*)out;
-  hipLaunchKernelGGL(ll_answers_few_join_kernel, dim3((p.shape->d + 63) / 64, p.n), dim3(256), 0, p.stream, j, terms);
   LL_HIP_CHECK(hipGetLastError());
   return LL_OK;
 }
@@ -341,10 +415,8 @@ int ll_policy(const ll_shape* shape, void* workspace, size_t workspace_bytes, co
     const auto from = [&](const float* x) { return x != nullptr ? x + r0 : nullptr; };
     const PolicyArgs policy = {advantage + r0, from(old_logp), kl != 0.f ? from(ref_logp) : nullptr, from(weight), out_loss + r0, clip_low, clip_high, kl};
     RowTerms* const terms = grad ? at<RowTerms>(workspace, a.terms) + r0 : nullptr;
-    FewJoinArgs j = {};
-    LL_TRY(answer_rows<true>(p, a, workspace, ids + r0, temperature, out_logp + r0, terms, policy, j));
-    if (!grad) return LL_OK;
-    if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
+    LL_TRY(answer_rows<true>(p, a, workspace, ids + r0, temperature, out_logp + r0, terms, policy, PairArgs{}, out_grad));
+    if (!grad || a.l.few) return LL_OK;
     float* const sums = at<float>(workspace, a.l.part);
     LL_TRY(p.back(nullptr, sums));
     return answer_join(p, a, sums, ids + r0, terms, (uint16_t*)out_grad + r0 * shape->d);
@@ -373,9 +445,9 @@ int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes
     LL_TRY(check(shape, workspace, workspace_bytes, a.total, rows, W_U, temperature, ids));
   }
   RowTerms* const terms = grad && shape->N > 0 ? at<RowTerms>(workspace, a.terms) : nullptr;
+  const PairArgs q = {ids, offsets, out_logp, ref_logp, weight, shape->N, n_pairs, shape->V, form, mean, beta, smoothing, out_loss, out_score, terms};
   const auto pairs = [&]() -> int {
     if (n_pairs == 0) return LL_OK;
-    const PairArgs q = {ids, offsets, out_logp, ref_logp, weight, shape->N, shape->V, form, mean, beta, smoothing, out_loss, out_score, terms};
     hipLaunchKernelGGL(ll_preference_pairs_kernel, dim3((unsigned)n_pairs), dim3(256), 0, (hipStream_t)stream, q);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
@@ -383,11 +455,9 @@ int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes
   const auto sums_of = [&](int64_t r0) { return at<float>(workspace, a.l.part) + (a.keep ? r0 * a.l.back_splits * shape->d : 0); };
   const bool between = grad && shape->N > 0 && !a.keep;      // one pass: the pairs come between the products
   LL_TRY(for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream, [&](const Pass& p, int64_t r0) -> int {
-    FewJoinArgs j = {};
-    LL_TRY(answer_rows<false>(p, a, workspace, ids + r0, temperature, out_logp + r0, grad ? terms + r0 : nullptr, PolicyArgs{}, j));
-    if (!grad) return LL_OK;
+    LL_TRY(answer_rows<false>(p, a, workspace, ids + r0, temperature, out_logp + r0, grad ? terms + r0 : nullptr, PolicyArgs{}, q, out_grad));
+    if (!grad || a.l.few) return LL_OK;
     if (!a.keep) LL_TRY(pairs());
-    if (a.l.few) return answer_few_join(p, a, j, terms, out_grad);
     LL_TRY(p.back(nullptr, sums_of(r0)));
     return a.keep ? LL_OK : answer_join(p, a, sums_of(r0), ids, terms, (uint16_t*)out_grad);
   }));

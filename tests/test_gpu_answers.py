@@ -8,7 +8,7 @@ import torch
 import oracle.answers_oracle as O
 from oracle.learn_oracle import _log_softmax
 from paper_2604_06483_amd import binding as LL
-from tests.conftest import say
+from tests.conftest import kernels_of, say
 from tests.test_gpu_learn import f64, inputs, logit_error
 
 pytestmark = pytest.mark.gpu
@@ -172,6 +172,29 @@ def test_preference_against_the_oracle(N, d, V, form):
     assert not grad[int(offsets[-1]):].any()
     if weight is not None and P > 2:
         assert not grad[int(offsets[2]):int(offsets[4])].any()
+
+
+@pytest.mark.parametrize("N", [3, 4, 40])
+def test_more_pairs_than_threads(N):
+    """600 pairs, of which most are empty, and two that are not."""
+    d, V, P = 64, 300, 600
+    say(f"preference, {P} pairs over {N} rows")
+    a, W, ids, g = case(N, d, V, seed=8)
+    offsets = torch.zeros((2 * P + 1,), dtype=torch.int32)
+    offsets[5:] = 1                                               # sequence 4, the preferred one of pair 2: row 0
+    offsets[2 * 500 + 2:] = N - 1                                 # pair 500: rows 1 to N - 2 not preferred; the last row in none
+    _, score, _, grad = check_preference(a, W, ids, offsets, None, torch.rand((P,), generator=g), 0.3, 0.0, "logistic", False, 1.0)
+    assert int((score != 0).sum()) == 2 and not grad[N - 1].any()
+
+
+@pytest.mark.parametrize("N,d,V", [(2, 2560, 3000), (4, 1024, 900)])
+def test_few_rows_take_two_launches(N, d, V):
+    say(f"answers in two launches N={N}")
+    a, W, ids, g = case(N, d, V, seed=9)
+    dev = [x.to(DEV) for x in (a, W, ids)]
+    A, offsets = torch.ones((N,), device=DEV), torch.tensor([0, 1, N], dtype=torch.int32, device=DEV)
+    LL.ll_policy(*dev, A), LL.ll_preference(*dev, offsets)
+    assert [len(kernels_of(lambda: f(*dev, x))) for f, x in ((LL.ll_policy, A), (LL.ll_preference, offsets))] == [2, 2]
 
 
 def test_one_long_pair_over_several_passes():
