@@ -599,12 +599,12 @@ def ll_preference_workspace_bytes(N: int, d: int, V: int, pairs: int) -> int:
     return int(lib().ll_preference_workspace_bytes(ll_shape(N, d, V), pairs))
 
 
-def _each(t, dtype, name, N):
+def _each(t, dtype, name, N, stream):
     """One value a row, in the rows' own leading shape or flat."""
     if t is None:
         return None
-    if isinstance(t, _Tensor) and t.dim() != 1 and t.is_contiguous():
-        t = t.reshape(-1)
+    if isinstance(t, _Tensor) and t.dim() != 1:
+        t = _rows(t, 1, stream).reshape(-1)
     _check(t, dtype, name, (N,))
     return t
 
@@ -615,7 +615,7 @@ def _answer_rows(rows, W_U, ids, stream):
     N, V = r2.shape[0], W_U.shape[0]
     _check(r2, _BF16, "rows")
     _check(W_U, _BF16, "W_U", (V, d))
-    return r2, _each(ids, torch.int32, "ids", N), N, d, V
+    return r2, _each(ids, torch.int32, "ids", N, stream), N, d, V
 
 
 def ll_policy(rows, W_U, ids, advantage, old_logp=None, *, ref_logp=None, weight=None, clip=(0.2, 0.2), kl=0.0, temperature=1.0, grad=True,
@@ -626,7 +626,7 @@ def ll_policy(rows, W_U, ids, advantage, old_logp=None, *, ref_logp=None, weight
     Returns (loss [N] fp32, the tokens' log-probabilities [N] fp32, gradient of weight . loss in bf16 in the rows' shape, or None with grad=False).
     """
     r2, i2, N, d, V = _answer_rows(rows, W_U, ids, stream)
-    A, old, ref, w = (_each(t, _F32, name, N) for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")))
+    A, old, ref, w = (_each(t, _F32, name, N, stream) for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")))
     dev = rows.device
     loss, logp = _empty((N,), _F32, dev, stream), _empty((N,), _F32, dev, stream)
     out = _like(r2, stream) if grad else None
@@ -655,7 +655,7 @@ def ll_preference(rows, W_U, ids, offsets, *, ref_logp=None, weight=None, beta=0
     if offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
         raise ValueError(f"offsets: shape {tuple(offsets.shape)}, expected (2 pairs + 1,)")
     P = offsets.shape[0] // 2
-    ref, w = _each(ref_logp, _F32, "ref_logp", N), _each(weight, _F32, "weight", P)
+    ref, w = _each(ref_logp, _F32, "ref_logp", N, stream), _each(weight, _F32, "weight", P, stream)
     dev = rows.device
     loss, score, logp = _empty((P,), _F32, dev, stream), _empty((P, 2), _F32, dev, stream), _empty((N,), _F32, dev, stream)
     out = _like(r2, stream) if grad else None
