@@ -128,9 +128,10 @@ def lib() -> ctypes.CDLL:
         L.ll_preference.restype = c_int
         L.ll_grad_norm_workspace_bytes.argtypes = [c_int32]
         L.ll_grad_norm_workspace_bytes.restype = c_size_t
-        L.ll_grad_norm.argtypes = [POINTER(ll_tensor), c_int32, c_void_p, c_size_t, c_void_p, c_void_p]
+        L.ll_grad_norm.argtypes = [c_void_p, c_int32,       # (addresses: a pointer made of a structure is a microsecond)
+                                    c_void_p, c_size_t, c_void_p, c_void_p]
         L.ll_grad_norm.restype = c_int
-        L.ll_adamw.argtypes = [POINTER(ll_tensor), c_int32, POINTER(ll_adamw_options)] + [c_void_p] * 4
+        L.ll_adamw.argtypes = [c_void_p, c_int32] + [c_void_p] * 5
         L.ll_adamw.restype = c_int
         L.ll_error_string.argtypes = [c_int]
         L.ll_error_string.restype = c_char_p
@@ -688,7 +689,8 @@ class TensorList:
         if self.whole and (m is None or v is None):
             raise ValueError("a step needs m and v")
         self.device = self.grads[0].device if count else torch.device("cuda")
-        self.array = (ll_tensor * max(count, 1))()
+        self.array, self.options = (ll_tensor * max(count, 1))(), ll_adamw_options()
+        self.address, self.options_address = ctypes.addressof(self.array), ctypes.addressof(self.options)
         written = set()
         for i, g in enumerate(self.grads):
             t = self.array[i]
@@ -758,7 +760,7 @@ def ll_grad_norm(tensors, *, workspace=None, stream=None, out=None):
         out = _empty((1,), _F32, tensors.device, stream)
     else:
         _check(out, _F32, "out", (1,))
-    rc = (_lib or lib()).ll_grad_norm(tensors.array, len(tensors), ws.data_ptr(), ws.numel() * ws.element_size(), out.data_ptr(), _stream(stream))
+    rc = (_lib or lib()).ll_grad_norm(tensors.address, len(tensors.grads), ws.data_ptr(), ws.numel() * ws.element_size(), out.data_ptr(), _stream(stream))
     if rc != LL_OK:
         raise LLError(rc, "ll_grad_norm")
     return out
@@ -773,10 +775,15 @@ def ll_adamw(tensors, step=None, *, rate=1e-3, betas=(0.9, 0.999), eps=1e-8, dec
         raise TypeError("tensors: need a TensorList with params, m and v")
     if (step is None) == (clock is None):
         raise ValueError("need a step or a clock")
-    for t, dtype, name, size in ((norm, _F32, "norm", (1,)), (clock, torch.int64, "clock", (4,)), (device_rate, _F32, "device_rate", (1,))):
-        if t is not None:
-            _check(t, dtype, name, size)
-    options = ll_adamw_options(rate, betas[0], betas[1], eps, decay, max_norm, 0 if step is None else step, seed & 0xFFFFFFFF)
-    rc = (_lib or lib()).ll_adamw(tensors.array, len(tensors), options, _ptr(norm), _ptr(clock), _ptr(device_rate), _stream(stream))
+    if norm is not None:
+        _check(norm, _F32, "norm", (1,))
+    if clock is not None:
+        _check(clock, torch.int64, "clock", (4,))
+    if device_rate is not None:
+        _check(device_rate, _F32, "device_rate", (1,))
+    o = tensors.options
+    o.rate, (o.beta1, o.beta2), o.eps, o.decay, o.max_norm, o.step, o.seed = rate, betas, eps, decay, max_norm, step or 0, seed & 0xFFFFFFFF
+    rc = (_lib or lib()).ll_adamw(tensors.address, len(tensors.grads), tensors.options_address, None if norm is None else norm.data_ptr(),
+                                  None if clock is None else clock.data_ptr(), None if device_rate is None else device_rate.data_ptr(), _stream(stream))
     if rc != LL_OK:
         raise LLError(rc, "ll_adamw")

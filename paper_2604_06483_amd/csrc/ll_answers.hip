@@ -66,6 +66,38 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t r
   return r;
 }
 
+// Before the first product: the rows padded, the tokens' logits (before the temperature; 0 without a token), and what P starts from, as in
+// ll_distill_lists_kernel.  One token a row, so a workgroup shares a row, and has all of it in flight at once.
+__global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p, float* __restrict__ z, float* __restrict__ ref, uint16_t* __restrict__ panel,
+                                                                int64_t lda) {
+  __shared__ float part[4];
+  const int64_t row = blockIdx.x;
+  const int id = p.ids[row];
+  const bool valid = id >= 0 && id < p.V;
+  const uint4* const a = reinterpret_cast<const uint4*>(p.rows + row * p.d);
+  const uint4* const w = reinterpret_cast<const uint4*>(p.W + (valid ? (int64_t)id * p.d : 0));
+  float s[2] = {0.f, 0.f};
+#pragma unroll 4
+  for (int c = threadIdx.x; c < p.d / 8; c += 256) {
+    const uint4 x = a[c], y = w[c];
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      s[0] = fmaf(bf16_lo(xs[q]), bf16_lo(ys[q]), s[0]);
+      s[1] = fmaf(bf16_hi(xs[q]), bf16_hi(ys[q]), s[1]);
+    }
+    if (panel != nullptr) reinterpret_cast<uint4*>(panel + row * lda)[c] = x;
+  }
+  if (panel != nullptr && (int)threadIdx.x < lda / 8 - p.d / 8) reinterpret_cast<uint4*>(panel + row * lda)[p.d / 8 + threadIdx.x] = make_uint4(0, 0, 0, 0);
+  const float sum = wave_sum(s[0] + s[1]);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  const float logit = valid ? (part[0] + part[1]) + (part[2] + part[3]) : 0.f, most = logit * p.to_log2;
+  z[row] = logit;
+  ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
+}
+
 // A row a workgroup: its log-probability and what its gradient is made of.  terms.a is the gradient's factor without c, terms.factor with it
 // (a preference's comes later: ll_preference_pairs_kernel), terms.b the own token's part, (p - 1) 2^(lse2 - base), whose place in P is 0.  Tiles
 // of P are brought to one base as in ll_distill_rows_kernel.
@@ -362,7 +394,7 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
       return LL_OK;
     }
   } else {
-    hipLaunchKernelGGL(ll_distill_lists_kernel, dim3(p.n), p.list_threads(), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
+    hipLaunchKernelGGL(ll_answers_tokens_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
                        p.panel(), l.lda);
     LL_HIP_CHECK(hipGetLastError());
     LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());

@@ -52,6 +52,25 @@ __device__ __forceinline__ bool gather_same(int id, bool valid, int k, int lane,
   return first;
 }
 
+// Before the first product: the rows padded, the listed tokens' logits, and the largest in powers of two, to the nearest whole one (of a row
+// without any: 0).  What P is relative to is always whole: to change it then changes exponents only, and rounds nothing again.
+__global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref,
+                                                                uint16_t* __restrict__ panel, int64_t lda) {
+  __shared__ float z[LIST_MAX];
+  pad_row(p.rows, blockIdx.x, p.d, panel, lda);
+  list_logits(p, blockIdx.x, z);
+  const int lane = threadIdx.x;
+  if (lane >= 64) return;
+  const int64_t row = blockIdx.x, e = row * p.k + lane;
+  float most = NEG_BIG;
+  if (lane < p.k) {
+    z_out[e] = z[lane];
+    if (p.ids[e] >= 0 && p.ids[e] < p.V) most = z[lane] * p.to_log2;
+  }
+  most = wave_max(most);
+  if (lane == 0) ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
+}
+
 // A row's teacher, by a wavefront, one lane an entry: t = softmax of the scores / temperature over the entries that there are.
 struct Teacher {
   bool valid, some;     // the lane's entry is one; the row has one

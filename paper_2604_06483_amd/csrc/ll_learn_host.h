@@ -41,25 +41,6 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   return r;
 }
 
-// Before the first product: the rows padded, the listed tokens' logits, and the largest in powers of two, to the nearest whole one (of a row
-// without any: 0).  What P is relative to is always whole: to change it then changes exponents only, and rounds nothing again.
-__global__ __launch_bounds__(1024) void ll_distill_lists_kernel(const ListArgs p, float* __restrict__ z_out, float* __restrict__ ref,
-                                                                uint16_t* __restrict__ panel, int64_t lda) {
-  __shared__ float z[LIST_MAX];
-  pad_row(p.rows, blockIdx.x, p.d, panel, lda);
-  list_logits(p, blockIdx.x, z);
-  const int lane = threadIdx.x;
-  if (lane >= 64) return;
-  const int64_t row = blockIdx.x, e = row * p.k + lane;
-  float most = NEG_BIG;
-  if (lane < p.k) {
-    z_out[e] = z[lane];
-    if (p.ids[e] >= 0 && p.ids[e] < p.V) most = z[lane] * p.to_log2;
-  }
-  most = wave_max(most);
-  if (lane == 0) ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
-}
-
 // A row of P brought to one base, by a workgroup of 256 threads (see ll_distill_rows_kernel).
 __device__ __forceinline__ void tiles_to_base(uint16_t* at, int64_t ldp, const float* __restrict__ moved, float base) {
   for (int64_t c = 8 * (int)threadIdx.x; c < ldp; c += 8 * 256) {

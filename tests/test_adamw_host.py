@@ -25,8 +25,12 @@ def options(**kw):
     return LL.ll_adamw_options(*[o[n] for n, _ in LL.ll_adamw_options._fields_])
 
 
+def at(x):
+    return None if x is None else ctypes.addressof(x)
+
+
 def step(list_=None, count=2, opt=None, norm=None, clock=None, device_rate=None):
-    return LL.lib().ll_adamw(list_, count, opt, norm, clock, device_rate, None)
+    return LL.lib().ll_adamw(at(list_), count, at(opt), norm, clock, device_rate, None)
 
 
 def test_the_structs_are_the_headers():
@@ -66,7 +70,7 @@ def test_arguments():
 
 
 def test_norm():
-    call = LL.lib().ll_grad_norm
+    call = lambda list_, *a: LL.lib().ll_grad_norm(at(list_), *a)  # noqa: E731
     need = LL.lib().ll_grad_norm_workspace_bytes(2)
     assert need > 0 and need % 256 == 0 and LL.lib().ll_grad_norm_workspace_bytes(-1) == 0
     assert LL.lib().ll_grad_norm_workspace_bytes(1000) > need
