@@ -283,6 +283,8 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
   __shared__ float shared_ref, shared_c;
   const int row = blockIdx.y, rows = gridDim.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int of_wave = POLICY ? row : wave;
+  FewColumns columns;
+  columns.load(p, row);
   if (POLICY ? wave == 0 : wave < rows) {
     const RowStats stats = join_stats(r.stats + of_wave, r.parts, lane, r.stride);
     const int id = r.ids[of_wave];
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
     scale[i] = part.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(part.x - shared_ref);
   }
   __syncthreads();
-  few_join_columns(p, row, shared_c != 0.f ? -r.inv_t * shared_c : 0.f, scale, share, id_of);
+  columns.join(p, row, shared_c != 0.f ? -r.inv_t * shared_c : 0.f, scale, share, id_of);
 }
 
 // ---------------------------------------------------------------------------------------

@@ -208,6 +208,8 @@ __global__ __launch_bounds__(256) void ll_learn_few_join_kernel(const FewJoinArg
   const ListArgs& l = p.f.list;
   const int row = blockIdx.y, k = l.k, lane = threadIdx.x & 63;
   const float temperature = p.f.temperature;
+  FewColumns columns;
+  columns.load(p, row);
   if (threadIdx.x < 64) {
     const int e = row * k + lane;
     const int id = lane < k ? l.ids[e] : -1;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void ll_learn_few_join_kernel(const FewJoinArg
     }
     __syncthreads();
   }
-  few_join_columns(p, row, shared_factor, DISTILL ? scale : nullptr, share, id_of);
+  columns.join(p, row, shared_factor, DISTILL ? scale : nullptr, share, id_of);
 }
 
 }  // namespace

@@ -81,49 +81,64 @@ struct FewJoinArgs {
   float* loss;
   uint16_t* out;
 };
-// The parts' sums joined, and the listed tokens' rows of W: block (64 columns, row), sixteen runs of the parts and of the list side by side.
-// scale: what each part is multiplied by, or nullptr (1); share and id_of: the list's entries (id below 0: none); all three in LDS.
-__device__ __forceinline__ void few_join_columns(const FewJoinArgs& p, int row, float factor, const float* scale, const float* share, const int* id_of) {
-  __shared__ float4 red[16][16];
-  const ListArgs& l = p.f.list;
-  const int k = l.k;
-  const int col = threadIdx.x & 15, run = threadIdx.x >> 4, c = blockIdx.x * 64 + col * 4;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (c < l.d && factor != 0.f) {
-    const float* from = p.f.sums + (int64_t)row * l.d + c;
-    const int64_t stride = (int64_t)p.stride * l.d;
-#pragma unroll 8
-    for (int i = run; i < p.parts; i += 16) {
-      const float4 x = *reinterpret_cast<const float4*>(from + i * stride);
-      const float by = scale != nullptr ? scale[i] : 1.f;
-      s.x = fmaf(by, x.x, s.x);
-      s.y = fmaf(by, x.y, s.y);
-      s.z = fmaf(by, x.z, s.z);
-      s.w = fmaf(by, x.w, s.w);
-    }
-    for (int i = run; i < k; i += 16) {
-      if (id_of[i] < 0) continue;
-      const uint2 w = *reinterpret_cast<const uint2*>(l.W + (int64_t)id_of[i] * l.d + c);
-      const float by = share[i];
-      s.x = fmaf(by, bf16_lo(w.x), s.x);
-      s.y = fmaf(by, bf16_hi(w.x), s.y);
-      s.z = fmaf(by, bf16_lo(w.y), s.z);
-      s.w = fmaf(by, bf16_hi(w.y), s.w);
-    }
-  }
-  red[run][col] = s;
-  __syncthreads();
-  if (run != 0 || c >= l.d) return;
+// The parts' sums joined, and the listed tokens' rows of W: block (64 columns, row), sixteen runs of the parts and of the list side by side.  What
+// a thread adds is asked for first and waits in registers for what it is multiplied by.
+struct FewColumns {
+  static constexpr int RUNS = 16, MOST = FEW_LEARN_STREAMS / RUNS;
+  float4 x[MOST];
+  static __device__ __forceinline__ int column() { return blockIdx.x * 64 + (threadIdx.x & 15) * 4; }
+
+  __device__ __forceinline__ void load(const FewJoinArgs& p, int row) {
+    const int run = threadIdx.x >> 4, c = column(), d = p.f.list.d;
+    const float* from = p.f.sums + (int64_t)row * d + (c < d ? c : 0);
+    const int64_t stride = (int64_t)p.stride * d;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) {
-    const float4 x = red[i][col];
-    s.x += x.x;
-    s.y += x.y;
-    s.z += x.z;
-    s.w += x.w;
+    for (int j = 0; j < MOST; ++j) {
+      const int i = run + RUNS * j;
+      x[j] = *reinterpret_cast<const float4*>(from + (i < p.parts ? i : 0) * stride);
+    }
   }
-  *reinterpret_cast<uint2*>(p.out + (int64_t)row * l.d + c) = make_uint2(pack_bf16(factor * s.x, factor * s.y), pack_bf16(factor * s.z, factor * s.w));
-}
+  // scale: what each part is multiplied by, or nullptr (1); share and id_of: the list's entries (id below 0: none); all three in LDS.
+  __device__ __forceinline__ void join(const FewJoinArgs& p, int row, float factor, const float* scale, const float* share, const int* id_of) {
+    __shared__ float4 red[RUNS][16];
+    const ListArgs& l = p.f.list;
+    const int col = threadIdx.x & 15, run = threadIdx.x >> 4, c = column();
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < l.d && factor != 0.f) {
+#pragma unroll
+      for (int j = 0; j < MOST; ++j) {
+        const int i = run + RUNS * j;
+        if (i >= p.parts) continue;
+        const float by = scale != nullptr ? scale[i] : 1.f;
+        s.x = fmaf(by, x[j].x, s.x);
+        s.y = fmaf(by, x[j].y, s.y);
+        s.z = fmaf(by, x[j].z, s.z);
+        s.w = fmaf(by, x[j].w, s.w);
+      }
+      for (int i = run; i < l.k; i += RUNS) {
+        if (id_of[i] < 0) continue;
+        const uint2 w = *reinterpret_cast<const uint2*>(l.W + (int64_t)id_of[i] * l.d + c);
+        const float by = share[i];
+        s.x = fmaf(by, bf16_lo(w.x), s.x);
+        s.y = fmaf(by, bf16_hi(w.x), s.y);
+        s.z = fmaf(by, bf16_lo(w.y), s.z);
+        s.w = fmaf(by, bf16_hi(w.y), s.w);
+      }
+    }
+    red[run][col] = s;
+    __syncthreads();
+    if (run != 0 || c >= l.d) return;
+#pragma unroll
+    for (int i = 1; i < RUNS; ++i) {
+      const float4 y = red[i][col];
+      s.x += y.x;
+      s.y += y.y;
+      s.z += y.z;
+      s.w += y.w;
+    }
+    *reinterpret_cast<uint2*>(p.out + (int64_t)row * l.d + c) = make_uint2(pack_bf16(factor * s.x, factor * s.y), pack_bf16(factor * s.z, factor * s.w));
+  }
+};
 
 // ---------------------------------------------------------------------------------------
 // Host
