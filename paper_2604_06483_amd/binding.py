@@ -673,34 +673,36 @@ def ll_preference(rows, W_U, ids, offsets, *, ref_logp=None, weight=None, beta=0
 class TensorList:
     """The tensors that a step is about, as ll_grad_norm and ll_adamw take them, checked and marshalled once: `grads` alone for the norm; for a
     step also `params`, `m` and `v` (fp32; or m in float8_e4m3fn and v in float8_e5m2 with fp32 `m_scale` and `v_scale`, one for LL_STATE_BLOCK
-    elements) and, where fp32 parameters have one, a bf16 copy each (`copies`; None: none).  The tensors are kept, and worked on in place.
+    elements) and, where fp32 parameters have one, a bf16 copy each (`copies`; None: none).  Their memory is kept, and worked on in place: of a
+    tensor that is given other memory later (by `.data =`, say) it is still the old.  All on one device.
     """
 
     def __init__(self, grads, params=None, m=None, v=None, m_scale=None, v_scale=None, copies=None):
         kinds = {"params": params, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies}
-        self.grads = list(grads)
+        kept = lambda of: [x.detach() if isinstance(x, _Tensor) else x for x in of]
+        self.grads = kept(grads)
         count = len(self.grads)
         for name, of in kinds.items():
-            of = [None] * count if of is None else list(of)
+            of = [None] * count if of is None else kept(of)
             if len(of) != count:
                 raise ValueError(f"{name}: {len(of)} tensors, expected {count}")
             setattr(self, name, of)
         self.whole = params is not None
         if self.whole and (m is None or v is None):
             raise ValueError("a step needs m and v")
-        self.device = self.grads[0].device if count else torch.device("cuda")
+        self.device = None
         self.array, self.options = (ll_tensor * max(count, 1))(), ll_adamw_options()
         self.address, self.options_address = ctypes.addressof(self.array), ctypes.addressof(self.options)
         written = set()
         for i, g in enumerate(self.grads):
             t = self.array[i]
-            t.n, t.grad = g.numel(), g.data_ptr()
             t.flags = self._grad_flag(g, f"grads[{i}]")
+            t.n, t.grad = g.numel(), g.data_ptr()
             if not self.whole:
                 continue
             p = self.params[i]
-            _check(p, p.dtype if p.dtype in (_F32, _BF16) else _F32, f"params[{i}]", g.shape)
-            eight = self.m[i].dtype == torch.float8_e4m3fn
+            _check(p, _BF16 if isinstance(p, _Tensor) and p.dtype == _BF16 else _F32, f"params[{i}]", g.shape)
+            eight = isinstance(self.m[i], _Tensor) and self.m[i].dtype == torch.float8_e4m3fn
             _check(self.m[i], torch.float8_e4m3fn if eight else _F32, f"m[{i}]", g.shape)
             _check(self.v[i], torch.float8_e5m2 if eight else _F32, f"v[{i}]", g.shape)
             blocks = (t.n + LL_STATE_BLOCK - 1) // LL_STATE_BLOCK
@@ -713,34 +715,39 @@ class TensorList:
                 if p.dtype != _F32:
                     raise ValueError(f"copies[{i}]: only fp32 parameters have one")
                 _check(self.copies[i], _BF16, f"copies[{i}]", g.shape)
-            t.param, t.m, t.v, t.m_scale, t.v_scale, t.copy = (_ptr(x) for x in (p, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i], self.copies[i]))
+            mine = [p, self.m[i], self.v[i], self.m_scale[i], self.v_scale[i], self.copies[i]]
+            t.param, t.m, t.v, t.m_scale, t.v_scale, t.copy = at = [_ptr(x) for x in mine]
             t.flags |= (LL_TENSOR_PARAM_BF16 if p.dtype == _BF16 else 0) | (LL_TENSOR_STATE_8BIT if eight else 0)
-            for x in (t.param, t.m, t.v, t.copy):
-                if t.n and x in written:
+            for x, a in zip(mine, at):
+                if x is None:
+                    continue
+                if x.device != self.device:
+                    raise ValueError(f"tensor {i}: on {x.device}, the first on {self.device}")
+                if a and a in written:
                     raise ValueError(f"tensor {i}: the same memory is in the list twice")
-                written.add(x) if x else None
+                written.add(a)
+        self.device = torch.device("cuda") if self.device is None else self.device
 
-    @staticmethod
-    def _grad_flag(g, name):
-        if isinstance(g, _Tensor) and g.dtype == _BF16:
-            _check(g, _BF16, name)
-            return LL_TENSOR_GRAD_BF16
-        _check(g, _F32, name)
-        return 0
+    def _grad_flag(self, g, name):
+        bf16 = isinstance(g, _Tensor) and g.dtype == _BF16
+        _check(g, _BF16 if bf16 else _F32, name)
+        if self.device is None:
+            self.device = g.device
+        elif g.device != self.device:
+            raise ValueError(f"{name}: on {g.device}, the first on {self.device}")
+        return LL_TENSOR_GRAD_BF16 if bf16 else 0
 
     def set_grads(self, grads):
         """Other gradients of the same shapes (a backward pass that made new tensors)."""
-        grads = list(grads)
+        grads = [g.detach() if isinstance(g, _Tensor) else g for g in grads]
         if len(grads) != len(self.grads):
             raise ValueError(f"grads: {len(grads)} tensors, expected {len(self.grads)}")
+        flags = [self._grad_flag(g, f"grads[{i}]") for i, g in enumerate(grads)]
         for i, (g, old) in enumerate(zip(grads, self.grads)):
-            if g is old:
-                continue
-            flag = self._grad_flag(g, f"grads[{i}]")
             if g.shape != old.shape:
                 raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, expected {tuple(old.shape)}")
-            self.array[i].grad = g.data_ptr()
-            self.array[i].flags = (self.array[i].flags & ~LL_TENSOR_GRAD_BF16) | flag
+        for t, g, flag in zip(self.array, grads, flags):        # (all of them or none)
+            t.grad, t.flags = g.data_ptr(), (t.flags & ~LL_TENSOR_GRAD_BF16) | flag
         self.grads = grads
 
     def __len__(self):

@@ -17,6 +17,14 @@
 
 namespace {
 
+// What a row's gradient is made of: factor (P's product with W_U + own W_id).
+struct AnswerTerms {
+  float rest;               // what 32 bits leave of the log-probability
+  float unit;               // the factor without c
+  float own;                // the own token's part, (p - 1) 2^(lse2 - base)
+  float factor;             // unit c; 0: the row takes no part
+};
+
 struct PolicyArgs {
   const float* advantage;
   const float* old_logp;    // or nullptr: the log-probability itself
@@ -34,7 +42,7 @@ struct AnswerArgs {
   int V;
   float to_log2, inv_t;
   float* logp;
-  RowTerms* terms;            // or nullptr: no gradient
+  AnswerTerms* terms;            // or nullptr: no gradient
   // the products' P; nullptr with few rows, whose sums are relative to lse2
   uint16_t* P;
   int64_t ldp;
@@ -65,6 +73,14 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t r
   if (p.weight != nullptr && p.weight[row] == 0.f) r.c = 0.f;  // (whatever the row holds)
   return r;
 }
+
+// A token's log-probability in powers of two, in 64 bits: a score's small log-ratios are differences of these, and the last bit of 32 at their
+// size would be most of a short answer's error.  The reference and the sum's exponent come off before a logarithm is taken, at the size of 1.
+__device__ __forceinline__ double log2_p(float z, float to_log2, const RowStats& r) {
+  const float rest = __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(r.sum));          // of [1/2, 1)
+  return (((double)z * (double)to_log2 - (double)r.ref) - (double)__builtin_amdgcn_frexp_expf(r.sum)) - (double)rest;
+}
+constexpr double LN2_64 = 0.69314718055994530942;
 
 // Before the first product: the rows padded, the tokens' logits (before the temperature; 0 without a token), and what P starts from, as in
 // ll_distill_lists_kernel.  One token a row, so a workgroup shares a row, and has all of it in flight at once.
@@ -98,9 +114,8 @@ __global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p
   ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
 }
 
-// A row a workgroup: its log-probability and what its gradient is made of.  terms.a is the gradient's factor without c, terms.factor with it
-// (a preference's comes later: ll_preference_pairs_kernel), terms.b the own token's part, (p - 1) 2^(lse2 - base), whose place in P is 0.  Tiles
-// of P are brought to one base as in ll_distill_rows_kernel.
+// A row a workgroup: its log-probability and its terms (a preference's factor comes later: ll_preference_pairs_kernel).  The own token's place in
+// P is made 0.  Tiles of P are brought to one base as in ll_distill_rows_kernel.
 template <bool POLICY>
 __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p) {
   __shared__ float shared_base;
@@ -113,22 +128,22 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
     const RowStats r = join_stats(p.stride == 1 ? p.stats + row * p.parts : p.stats + row, p.parts, lane, p.stride);
     id = p.ids[row];
     const bool valid = id >= 0 && id < p.V;
-    const float l = fmaf(p.z[row], p.to_log2, -r.lse2);
+    const double l = log2_p(p.z[row], p.to_log2, r), logp = l * LN2_64;
     bool other = false;
     if (p.P != nullptr)
       for (int i = lane; i < p.parts; i += 64) other |= p.stats[row * p.parts + i].x != p.ref[row];
     other = __builtin_amdgcn_ballot_w64(other) != 0;
     const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : p.ref[row];
     PolicyTerm t = {0.f, 0.f};
-    if (POLICY && valid) t = policy_term(p.policy, row, l * LN2);
+    if (POLICY && valid) t = policy_term(p.policy, row, (float)logp);
     live = valid && (!POLICY || t.c != 0.f);
     if (lane == 0) {
-      p.logp[row] = valid ? l * LN2 : NAN;
+      p.logp[row] = valid ? (float)logp : NAN;
       if (POLICY) p.policy.loss[row] = t.loss;
       if (p.terms != nullptr) {
         const float unit = -p.inv_t * (p.P == nullptr ? 1.f : __builtin_amdgcn_exp2f(base - r.lse2));
-        const float own = __builtin_amdgcn_exp2f(l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
-        p.terms[row] = {r.lse2, unit, own, POLICY && live ? unit * t.c : 0.f};
+        const float own = __builtin_amdgcn_exp2f((float)l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
+        p.terms[row] = {(float)(logp - (double)(float)logp), unit, own, POLICY && live ? unit * t.c : 0.f};
       }
       shared_moved = live && other;
       shared_base = base;
@@ -155,7 +170,7 @@ struct PairArgs {
   float beta, smoothing;
   float* loss;
   float* score;             // [pairs, 2]
-  RowTerms* terms;          // or nullptr: no gradient
+  AnswerTerms* terms;          // or nullptr: no gradient
 };
 
 // Rows of a sequence: [begin, end), brought into [0, N) whatever the offsets say.
@@ -205,7 +220,7 @@ __device__ __forceinline__ double group_total(double x, double* red) {
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
   const double sum = (red[0] + red[1]) + (red[2] + red[3]);
-  __syncthreads();
+  __syncthreads();                             // (`red` is free again)
   return sum;
 }
 
@@ -213,46 +228,47 @@ __device__ __forceinline__ double group_total(double x, double* red) {
 // row's c.  Offsets that are out of order or out of range are brought into it: no row outside [0, N) is touched.
 __global__ __launch_bounds__(256) void ll_preference_pairs_kernel(const PairArgs p) {
   __shared__ double red[4];
-  const int64_t pair = blockIdx.x;
-  Sequence rows[2];
-  double score[2], length[2];
+  for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) {
+    Sequence rows[2];
+    double score[2], length[2];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    rows[side] = sequence_of(p, 2 * pair + side);
-    double sum = 0., count = 0.;
-    for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256) {
-      if (p.ids[r] < 0 || p.ids[r] >= p.V) continue;
-      sum += (double)p.logp[r] - (p.ref_logp != nullptr ? (double)p.ref_logp[r] : 0.);
-      count += 1.;
+    for (int side = 0; side < 2; ++side) {
+      rows[side] = sequence_of(p, 2 * pair + side);
+      double sum = 0., count = 0.;
+      for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256) {
+        if (p.ids[r] < 0 || p.ids[r] >= p.V) continue;
+        sum += (double)p.logp[r] + (p.terms != nullptr ? (double)p.terms[r].rest : 0.) - (p.ref_logp != nullptr ? (double)p.ref_logp[r] : 0.);
+        count += 1.;
+      }
+      sum = group_total(sum, red);
+      count = group_total(count, red);
+      length[side] = p.mean && count > 1. ? count : 1.;
+      score[side] = sum / length[side];
     }
-    sum = group_total(sum, red);
-    count = group_total(count, red);
-    length[side] = p.mean && count > 1. ? count : 1.;
-    score[side] = sum / length[side];
-  }
-  const PairTerm t = pair_term(p, score);
-  if (threadIdx.x == 0) {
-    p.loss[pair] = t.loss;
-    p.score[2 * pair] = (float)score[0];
-    p.score[2 * pair + 1] = (float)score[1];
-  }
-  if (p.terms == nullptr) return;
+    const PairTerm t = pair_term(p, score);
+    if (threadIdx.x == 0) {
+      p.loss[pair] = t.loss;
+      p.score[2 * pair] = (float)score[0];
+      p.score[2 * pair + 1] = (float)score[1];
+    }
+    if (p.terms == nullptr) continue;
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const float c = pair_c(p, pair, t.slope, length[side], side);
-    for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256)
-      if (p.ids[r] >= 0 && p.ids[r] < p.V) p.terms[r].factor = c != 0.f ? p.terms[r].a * c : 0.f;
+    for (int side = 0; side < 2; ++side) {
+      const float c = pair_c(p, pair, t.slope, length[side], side);
+      for (int64_t r = rows[side].begin + (int)threadIdx.x; r < rows[side].end; r += 256)
+        if (p.ids[r] >= 0 && p.ids[r] < p.V) p.terms[r].factor = c != 0.f ? p.terms[r].unit * c : 0.f;
+    }
   }
 }
 
 // The slices' sums joined, in order, and the own token's part; a row that takes no part gets zeros whatever W holds.
 __global__ __launch_bounds__(256) void ll_answers_join_kernel(const float* __restrict__ part, int splits, int rows, int d, const int32_t* __restrict__ ids,
-                                                              const uint16_t* __restrict__ W, const RowTerms* __restrict__ terms,
+                                                              const uint16_t* __restrict__ W, const AnswerTerms* __restrict__ terms,
                                                               uint16_t* __restrict__ out) {
   const int64_t row = blockIdx.y;
   const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (c >= d) return;
-  const RowTerms t = terms[row];
+  const AnswerTerms t = terms[row];
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (t.factor != 0.f) {                       // (so the row has a token)
     const uint2 w = *reinterpret_cast<const uint2*>(W + (int64_t)ids[row] * d + c);
@@ -264,8 +280,8 @@ __global__ __launch_bounds__(256) void ll_answers_join_kernel(const float* __res
       s.z += x.z;
       s.w += x.w;
     }
-    s = make_float4(t.factor * fmaf(t.b, bf16_lo(w.x), s.x), t.factor * fmaf(t.b, bf16_hi(w.x), s.y), t.factor * fmaf(t.b, bf16_lo(w.y), s.z),
-                    t.factor * fmaf(t.b, bf16_hi(w.y), s.w));
+    s = make_float4(t.factor * fmaf(t.own, bf16_lo(w.x), s.x), t.factor * fmaf(t.own, bf16_hi(w.x), s.y), t.factor * fmaf(t.own, bf16_lo(w.y), s.z),
+                    t.factor * fmaf(t.own, bf16_hi(w.y), s.w));
   }
   *reinterpret_cast<uint2*>(out + row * d + c) = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
@@ -279,7 +295,7 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
   __shared__ float scale[FEW_LEARN_STREAMS];
   __shared__ float share[1];
   __shared__ int id_of[1];
-  __shared__ float logp[FEW_MOST];
+  __shared__ double logp[FEW_MOST];
   __shared__ float shared_ref, shared_c;
   const int row = blockIdx.y, rows = gridDim.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int of_wave = POLICY ? row : wave;
@@ -289,7 +305,7 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
     const RowStats stats = join_stats(r.stats + of_wave, r.parts, lane, r.stride);
     const int id = r.ids[of_wave];
     if (lane == 0) {
-      logp[POLICY ? 0 : wave] = id >= 0 && id < r.V ? fmaf(r.z[of_wave], r.to_log2, -stats.lse2) * LN2 : NAN;
+      logp[POLICY ? 0 : wave] = id >= 0 && id < r.V ? log2_p(r.z[of_wave], r.to_log2, stats) * LN2_64 : (double)NAN;
       if (of_wave == row) {
         shared_ref = stats.lse2;
         shared_c = 0.f;
@@ -303,15 +319,15 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
   if (POLICY) {
     if (threadIdx.x == 0) {
       PolicyTerm t = {0.f, 0.f};
-      if (valid) t = policy_term(r.policy, row, logp[0]);
+      if (valid) t = policy_term(r.policy, row, (float)logp[0]);
       shared_c = t.c;
       if (writes) {
-        r.logp[row] = logp[0];
+        r.logp[row] = (float)logp[0];
         r.policy.loss[row] = t.loss;
       }
     }
   } else {
-    if (threadIdx.x == 0 && writes) r.logp[row] = logp[row];
+    if (threadIdx.x == 0 && writes) r.logp[row] = (float)logp[row];
     for (int64_t pair = threadIdx.x; pair < q.pairs; pair += 256) {
       Sequence of[2];
       double score[2], length[2];
@@ -321,7 +337,7 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
         double sum = 0., count = 0.;
         for (int64_t i = of[side].begin; i < of[side].end; ++i) {
           if (q.ids[i] < 0 || q.ids[i] >= q.V) continue;
-          sum += (double)logp[i] - (q.ref_logp != nullptr ? (double)q.ref_logp[i] : 0.);
+          sum += logp[i] - (q.ref_logp != nullptr ? (double)q.ref_logp[i] : 0.);
           count += 1.;
         }
         length[side] = q.mean && count > 1. ? count : 1.;
@@ -365,13 +381,13 @@ AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
   a.total = a.l.total;
   if (needs == FORWARD) return a;
   a.terms = a.total;
-  a.total = align_up(a.total + (size_t)(s->N > 0 ? s->N : 1) * sizeof(RowTerms), 256);
+  a.total = align_up(a.total + (size_t)(s->N > 0 ? s->N : 1) * sizeof(AnswerTerms), 256);
   return a;
 }
 
 // The first product of a pass and its rows' terms; POLICY: and losses.  Of few rows with a gradient, all there is.
 template <bool POLICY>
-int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids, float temperature, float* logp, RowTerms* terms,
+int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids, float temperature, float* logp, AnswerTerms* terms,
                 const PolicyArgs& policy, const PairArgs& pairs, void* out) {
   const LearnPlan& l = a.l;
   AnswerArgs r = {};
@@ -416,12 +432,14 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
 }
 
 // The gradient of a pass from its sums.
-int answer_join(const Pass& p, const AnswerPlan& a, const float* sums, const int32_t* ids, const RowTerms* terms, uint16_t* out) {
+int answer_join(const Pass& p, const AnswerPlan& a, const float* sums, const int32_t* ids, const AnswerTerms* terms, uint16_t* out) {
   hipLaunchKernelGGL(ll_answers_join_kernel, dim3((p.shape->d + 1023) / 1024, p.n), dim3(256), 0, p.stream, sums, a.l.back_splits, p.n, p.shape->d, ids,
                      p.W, terms, out);
   LL_HIP_CHECK(hipGetLastError());
   return LL_OK;
 }
+
+constexpr int MOST_PAIRS = 1 << 16;   // workgroups that take pairs in turn
 
 bool finite(float x) { return x - x == 0.f; }
 
@@ -448,7 +466,7 @@ int ll_policy(const ll_shape* shape, void* workspace, size_t workspace_bytes, co
   return for_passes(shape, a.l, workspace, rows, W_U, temperature, 1, stream, [&](const Pass& p, int64_t r0) -> int {
     const auto from = [&](const float* x) { return x != nullptr ? x + r0 : nullptr; };
     const PolicyArgs policy = {advantage + r0, from(old_logp), kl != 0.f ? from(ref_logp) : nullptr, from(weight), out_loss + r0, clip_low, clip_high, kl};
-    RowTerms* const terms = grad ? at<RowTerms>(workspace, a.terms) + r0 : nullptr;
+    AnswerTerms* const terms = grad ? at<AnswerTerms>(workspace, a.terms) + r0 : nullptr;
     LL_TRY(answer_rows<true>(p, a, workspace, ids + r0, temperature, out_logp + r0, terms, policy, PairArgs{}, out_grad));
     if (!grad || a.l.few) return LL_OK;
     float* const sums = at<float>(workspace, a.l.part);
@@ -478,11 +496,11 @@ int ll_preference(const ll_shape* shape, void* workspace, size_t workspace_bytes
     if (out_logp == nullptr) return LL_EINVAL;
     LL_TRY(check(shape, workspace, workspace_bytes, a.total, rows, W_U, temperature, ids));
   }
-  RowTerms* const terms = grad && shape->N > 0 ? at<RowTerms>(workspace, a.terms) : nullptr;
+  AnswerTerms* const terms = grad && shape->N > 0 ? at<AnswerTerms>(workspace, a.terms) : nullptr;
   const PairArgs q = {ids, offsets, out_logp, ref_logp, weight, shape->N, n_pairs, shape->V, form, mean, beta, smoothing, out_loss, out_score, terms};
   const auto pairs = [&]() -> int {
     if (n_pairs == 0) return LL_OK;
-    hipLaunchKernelGGL(ll_preference_pairs_kernel, dim3((unsigned)n_pairs), dim3(256), 0, (hipStream_t)stream, q);
+    hipLaunchKernelGGL(ll_preference_pairs_kernel, dim3(n_pairs < MOST_PAIRS ? n_pairs : MOST_PAIRS), dim3(256), 0, (hipStream_t)stream, q);
     LL_HIP_CHECK(hipGetLastError());
     return LL_OK;
   };

@@ -14,7 +14,8 @@ __device__ __forceinline__ void pad_row(const uint16_t* __restrict__ rows, int64
         8 * c < d ? reinterpret_cast<const uint4*>(rows + row * d)[c] : make_uint4(0, 0, 0, 0);
 }
 struct RowStats {
-  float lse2, t;   // log2 of the sum of 2^x; sum of p (x - lse2), x = z log2 e: minus the entropy, in powers of two
+  float lse2, t;     // log2 of the sum of 2^x; sum of p (x - lse2), x = z log2 e: minus the entropy, in powers of two
+  float ref, sum;    // that sum is 2^ref sum
 };
 // A row's parts, `stride` apart, joined by a wavefront.
 __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats, int parts, int lane, int stride = 1) {
@@ -36,8 +37,8 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   s = wave_sum(s);
   t = wave_sum(t);
   const float log_s = __builtin_amdgcn_logf(s);
-  RowStats r = {m + log_s, t / s - log_s};
-  if (wave_sum(nan ? 1.f : 0.f) > 0.f) r.lse2 = r.t = NAN;
+  RowStats r = {m + log_s, t / s - log_s, m, s};
+  if (wave_sum(nan ? 1.f : 0.f) > 0.f) r.lse2 = r.t = r.sum = NAN;
   return r;
 }
 

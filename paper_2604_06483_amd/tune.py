@@ -209,15 +209,28 @@ class AdamW(torch.optim.Optimizer):
         """The parameters' TensorList, kept from step to step, with this step's gradients."""
         kept = self._lists.get(key)
         states = [self.state[p] for p in params]
-        same = kept is not None and len(kept) == len(params) and all(a is b for a, b in zip(kept.params, params)) and all(
-            kept.m[i] is s["m"] for i, s in enumerate(states))
-        if same:
+        copies = [self.copies.get(p) for p in params]
+        # (the list keeps its tensors' memory: what begins where one of them does is that one, unless it has been given other memory)
+        at = lambda x: None if x is None else x.data_ptr()
+        if kept is not None and len(kept) == len(params) and all(
+                at(p) == at(q) and p.dtype == q.dtype and at(s["m"]) == at(m) and at(s["v"]) == at(v) and at(c) == at(k)
+                for p, q, s, m, v, c, k in zip(params, kept.params, states, kept.m, kept.v, copies, kept.copies)):
             kept.set_grads(grads)
             return kept
         pick = lambda name: [s.get(name) for s in states]
-        kept = LL.TensorList(grads, params, pick("m"), pick("v"), pick("m_scale"), pick("v_scale"), [self.copies.get(p) for p in params])
-        self._lists[key] = kept
+        kept = self._lists[key] = LL.TensorList(grads, params, pick("m"), pick("v"), pick("m_scale"), pick("v_scale"), copies)
         return kept
+
+    @staticmethod
+    def _whole(g):
+        """A gradient as the library takes it: dense, contiguous, from a multiple of 16 bytes on."""
+        if g.layout != torch.strided:
+            raise ValueError(f"a gradient is {g.layout}: only dense ones")
+        g = g.contiguous()
+        return g if g.data_ptr() % 16 == 0 else g.clone()
+
+    def __getstate__(self):
+        return dict(super().__getstate__(), max_norm=self.max_norm, bits=self.bits, seed=self.seed, norm=None, copies=self.copies, _lists={})
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -234,17 +247,17 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad is not None:
                     by_step.setdefault(self._state(p)["step"], []).append(p)
             for turn, (done, params) in enumerate(by_step.items()):
-                calls.append((group, done + 1, self._list((at, turn), params, [p.grad.contiguous() for p in params])))
+                calls.append((group, done + 1, params, self._list((at, turn), params, [self._whole(p.grad) for p in params])))
         if not calls:
             return loss
         self.norm = None
         if self.max_norm is not None:
-            one = calls[0][2] if len(calls) == 1 else LL.TensorList([g for _, _, tensors in calls for g in tensors.grads])
+            one = calls[0][3] if len(calls) == 1 else LL.TensorList([g for *_, tensors in calls for g in tensors.grads])
             self.norm = LL.ll_grad_norm(one)
-        for turn, (group, step, tensors) in enumerate(calls):
+        for turn, (group, step, params, tensors) in enumerate(calls):
             LL.ll_adamw(tensors, step, rate=float(group["lr"]), betas=group["betas"], eps=group["eps"], decay=group["weight_decay"], norm=self.norm,
                         max_norm=float("inf") if self.max_norm is None else self.max_norm, seed=self.seed + turn)
-            for p in tensors.params:
+            for p in params:
                 self.state[p]["step"] = step
                 torch.autograd.graph.increment_version(p)
         return loss

@@ -187,6 +187,20 @@ def test_more_pairs_than_threads(N):
     assert int((score != 0).sum()) == 2 and not grad[N - 1].any()
 
 
+def test_more_pairs_than_workgroups():
+    """70 000 pairs, all empty but the first and the last."""
+    N, d, V, P = 40, 64, 300, 70000
+    say(f"preference, {P} pairs")
+    a, W, ids, g = case(N, d, V, seed=10)
+    offsets = torch.full((2 * P + 1,), 20, dtype=torch.int32)
+    offsets[0], offsets[1], offsets[-2], offsets[-1] = 0, 11, 33, N
+    dev = [x.to(DEV) for x in (a, W, ids)]
+    loss, score, _, grad = LL.ll_preference(*dev, offsets.to(DEV))
+    few = LL.ll_preference(*dev, torch.tensor([0, 11, 20, 33, N], dtype=torch.int32, device=DEV))
+    assert torch.equal(loss[[0, -1]], few[0]) and torch.equal(score[[0, -1]], few[1]) and torch.equal(grad, few[3])
+    assert not score[1:-1].any() and float((loss[1:-1] - math.log(2)).abs().max()) < 1e-6
+
+
 @pytest.mark.parametrize("N,d,V", [(2, 2560, 3000), (4, 1024, 900)])
 def test_few_rows_take_two_launches(N, d, V):
     say(f"answers in two launches N={N}")

@@ -1,4 +1,6 @@
 """What autograd is told of the calls that learn from answers, and the optimiser's book-keeping, with the calls themselves in torch (no GPU needed)."""
+import copy
+
 import pytest
 import torch
 
@@ -105,8 +107,8 @@ class List:
 
     def __init__(self, grads, params=None, m=None, v=None, m_scale=None, v_scale=None, copies=None):
         List.made += 1
-        self.grads, self.params, self.m, self.v, self.copies = list(grads), params, m, v, copies
-        self.m_scale, self.v_scale = m_scale, v_scale
+        kept = lambda of: None if of is None else [None if x is None else x.detach() for x in of]  # noqa: E731
+        self.grads, self.params, self.m, self.v, self.copies = kept(grads), kept(params), kept(m), kept(v), kept(copies)
 
     def set_grads(self, grads):
         self.grads = list(grads)
@@ -176,6 +178,41 @@ def test_states_survive_being_saved(steps, bits, dtype):
     b.grad = a.grad
     other.step()
     assert [s for s, _, _ in steps] == [1, 2]
+
+
+def test_memory_that_a_parameter_no_longer_has_is_not_stepped(steps):
+    a = torch.nn.Parameter(torch.ones(3))
+    opt = tune.AdamW([a], lr=0.5)
+    a.grad = torch.ones(3)
+    opt.step()
+    old = a.data
+    a.data = torch.full((3,), 7.0)                        # (as moving a model does)
+    opt.step()
+    assert torch.equal(a.detach(), torch.full((3,), 6.5)) and torch.equal(old, torch.full((3,), 0.5)) and List.made == 2
+
+
+def test_a_copied_optimiser_goes_on(steps):
+    a = torch.nn.Parameter(torch.ones(3))
+    opt = tune.AdamW([a], lr=0.5, bits=8, max_norm=2.0, seed=4)
+    a.grad = torch.ones(3)
+    opt.step()
+    b, other = copy.deepcopy((a, opt))
+    b.grad = torch.ones(3)
+    other.step()
+    assert [s for s, _, _ in steps] == [1, 2] and steps[1][2]["max_norm"] == 2.0 and steps[1][2]["seed"] == 4
+    assert torch.equal(b.detach(), torch.zeros(3)) and torch.equal(a.detach(), torch.full((3,), 0.5))
+
+
+def test_gradients_that_are_no_whole_rows(steps, monkeypatch):
+    """Transposed, and from the middle of a buffer: a copy; sparse: an error."""
+    a, b = torch.nn.Parameter(torch.zeros(3, 2)), torch.nn.Parameter(torch.zeros(5))
+    a.grad, b.grad = torch.arange(6.0).reshape(2, 3).T, torch.arange(9.0)[1:6]
+    opt = tune.AdamW([a, b], lr=1.0)
+    opt.step()
+    assert torch.equal(a.detach(), -a.grad) and torch.equal(b.detach(), -b.grad)
+    a.grad = torch.zeros(3, 2).to_sparse()
+    with pytest.raises(ValueError, match="dense"):
+        opt.step()
 
 
 def test_refusals():
