@@ -27,7 +27,7 @@ constexpr int STEP_TENSORS = 48;               // of one launch: their list is t
 constexpr int NORM_TENSORS = 160;
 constexpr int NORM_GROUPS = 2048;              // workgroups of a launch, and their partial sums
 constexpr int NORM_UNIT = 1024;                // elements, by a wavefront; four of them in flight
-constexpr int NORM_ALONE = 128;                // units that one workgroup takes by itself
+constexpr int NORM_ALONE = 128;                // units that one workgroup takes by itself (66: 6.2 us, two launches 10.1; 132: 9.0 | 8.7 to 9.9; 264: 11.9 | 8.8 to 9.9)
 
 // ---- numbers ------------------------------------------------------------------------------------
 // A permutation of 32-bit words: PCG's RXS-M-XS output function over its own multiplier and increment (M. O'Neill, 2014), used as a hash

@@ -170,3 +170,51 @@ def test_a_second_derivative_is_refused():
         (grad,) = torch.autograd.grad(factor * value, rows, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             grad.float().sum().backward()
+
+
+def test_gradients_in_a_graph():
+    """Losses and gradients of both captured once, on inputs that are replaced between the replays: the eager ones each time."""
+    say("autograd of answers in a graph")
+    rows, W, ids, g = answers(60, 128, 700, seed=2)
+    A, factor = torch.randn((60,), generator=g).to(DEV), torch.tensor([1.0, 2.0], device=DEV)
+    offsets = torch.tensor([0, 20, 31, 31, 50], dtype=torch.int32, device=DEV)
+    held = rows.clone().requires_grad_()
+
+    def both(x):
+        a = torch.autograd.grad(tune.policy(x, W, ids, A)[0].sum(), x)[0]
+        b = torch.autograd.grad((factor * tune.preference(x, W, ids, offsets)[0]).sum(), x)[0]
+        return a, b
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both(held)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        out = both(held)
+    for turn in range(3):
+        with torch.no_grad():
+            held.copy_(torch.roll(rows, turn, 0))
+            factor.mul_(2.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(out, both(held.detach().clone().requires_grad_())):
+            assert torch.equal(x, y), turn
+
+
+def test_a_step_on_another_stream():
+    say("optimiser on another stream")
+    a, b = (torch.nn.Parameter(torch.ones((1000,), device=DEV)) for _ in range(2))
+    one, two = tune.AdamW([a], lr=0.1, max_norm=1.0), tune.AdamW([b], lr=0.1, max_norm=1.0)
+    s = torch.cuda.Stream()
+    for t in range(3):
+        a.grad = torch.full((1000,), 0.5 + t, device=DEV)
+        b.grad = a.grad.clone()
+        one.step()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            two.step()
+        torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(a.detach(), b.detach())
