@@ -600,6 +600,16 @@ def ll_preference_workspace_bytes(N: int, d: int, V: int, pairs: int) -> int:
     return int(lib().ll_preference_workspace_bytes(ll_shape(N, d, V), pairs))
 
 
+def _here(device, stream, *others):
+    """All tensors on one device, and that the one that the call goes to: a kernel would read the others' addresses as its own."""
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and on {t.device}")
+    index = (None if _device is None else _device()) if stream is None else stream.device.index
+    if index is not None and device.index is not None and index != device.index:
+        raise ValueError(f"the tensors are on {device}, the call goes to device {index}")
+
+
 def _each(t, dtype, name, N, stream):
     """One value a row, in the rows' own leading shape or flat."""
     if t is None:
@@ -629,6 +639,7 @@ def ll_policy(rows, W_U, ids, advantage, old_logp=None, *, ref_logp=None, weight
     r2, i2, N, d, V = _answer_rows(rows, W_U, ids, stream)
     A, old, ref, w = (_each(t, _F32, name, N, stream) for t, name in ((advantage, "advantage"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weight, "weight")))
     dev = rows.device
+    _here(dev, stream, W_U, i2, A, old, ref, w, workspace)
     loss, logp = _empty((N,), _F32, dev, stream), _empty((N,), _F32, dev, stream)
     out = _like(r2, stream) if grad else None
     ws = _workspace(workspace, lambda: ll_policy_workspace_bytes(N, d, V) if grad else ll_logp_workspace_bytes(N, d, V, 1), dev, stream)
@@ -658,6 +669,7 @@ def ll_preference(rows, W_U, ids, offsets, *, ref_logp=None, weight=None, beta=0
     P = offsets.shape[0] // 2
     ref, w = _each(ref_logp, _F32, "ref_logp", N, stream), _each(weight, _F32, "weight", P, stream)
     dev = rows.device
+    _here(dev, stream, W_U, i2, offsets, ref, w, workspace)
     loss, score, logp = _empty((P,), _F32, dev, stream), _empty((P, 2), _F32, dev, stream), _empty((N,), _F32, dev, stream)
     out = _like(r2, stream) if grad else None
     ws = _workspace(workspace, lambda: ll_preference_workspace_bytes(N, d, V, P) if grad else ll_logp_workspace_bytes(N, d, V, 1), dev, stream)
@@ -762,6 +774,7 @@ def ll_grad_norm(tensors, *, workspace=None, stream=None, out=None):
     """Norm of all gradients of a TensorList (or of a sequence of fp32 and bf16 tensors): [1] fp32, on the GPU."""
     if not isinstance(tensors, TensorList):
         tensors = TensorList(tensors)
+    _here(tensors.device, stream, workspace, out)
     ws = _workspace(workspace, lambda: ll_grad_norm_workspace_bytes(tensors), tensors.device, stream)
     if out is None:
         out = _empty((1,), _F32, tensors.device, stream)
@@ -788,6 +801,7 @@ def ll_adamw(tensors, step=None, *, rate=1e-3, betas=(0.9, 0.999), eps=1e-8, dec
         _check(clock, torch.int64, "clock", (4,))
     if device_rate is not None:
         _check(device_rate, _F32, "device_rate", (1,))
+    _here(tensors.device, stream, norm, clock, device_rate)
     o = tensors.options
     o.rate, (o.beta1, o.beta2), o.eps, o.decay, o.max_norm, o.step, o.seed = rate, betas, eps, decay, max_norm, step or 0, seed & 0xFFFFFFFF
     rc = (_lib or lib()).ll_adamw(tensors.address, len(tensors.grads), tensors.options_address, None if norm is None else norm.data_ptr(),

@@ -7,8 +7,7 @@
 // The row's own token is left out of P and its whole part, p - 1, which outweighs all others', joins the sums in fp32: rounded into P it would
 // be most of the gradient's error (rms, of the gradient: 0.0026 with it in P, 0.0017 without, which is the result's own rounding).
 // What is new is c.  Nothing of it is needed before the second product's sums are rounded, where it is a factor of the row, so that the logits
-// are formed once: with the log-probabilities and their gradient as two
-// calls there is a third product.  Whole calls, us, ll_policy | ll_logp, the loss in torch, ll_logp_grad: 1 row, d = 4096, V = 128256 175 | 364; 111,
+// are formed once: with the log-probabilities and their gradient as two calls there is a third product.  Whole calls, us, ll_policy | ll_logp, the loss in torch, ll_logp_grad: 1 row, d = 4096, V = 128256 175 | 364; 111,
 // 1608, 50257 97 | 161; 1500, 4096, 128256 2193 | 3190 (1.44 PFLOP/s; the vendor's bare product of that shape 1.28); 6000, 2560, 151936 6546 | 9510.
 //
 // A policy's c is the row's own.  A preference's is known when every row of its pair has been through W_U.  Up to one pass of rows the
@@ -43,7 +42,7 @@ struct AnswerArgs {
   int V;
   float to_log2, inv_t;
   float* logp;
-  AnswerTerms* terms;            // or nullptr: no gradient
+  AnswerTerms* terms;         // or nullptr: no gradient
   // the products' P; nullptr with few rows, whose sums are relative to lse2
   uint16_t* P;
   int64_t ldp;
@@ -171,7 +170,7 @@ struct PairArgs {
   float beta, smoothing;
   float* loss;
   float* score;             // [pairs, 2]
-  AnswerTerms* terms;          // or nullptr: no gradient
+  AnswerTerms* terms;       // or nullptr: no gradient
 };
 
 // Rows of a sequence: [begin, end), brought into [0, N) whatever the offsets say.
