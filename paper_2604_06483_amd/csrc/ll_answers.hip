@@ -47,8 +47,8 @@ struct AnswerArgs {
   uint16_t* P;
   int64_t ldp;
   const float* ref;
-  const float* moved;
-  int tiles;
+  const float* moved;         // [rows, tiles]: what the exponents of a tile of `width` ids are relative to
+  int tiles, width;
   PolicyArgs policy;
 };
 
@@ -114,6 +114,120 @@ __global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p
   ref[row] = fabsf(most) < 1e30f ? rintf(most) : 0.f;
 }
 
+// The first product where the vocabulary is too short for the direct-to-LDS kernel (ll_learn_gemm.hip): its tiles of 256 ids leave compute units
+// without one, and each that has one waits for a stage of 64 columns after the other (9 x 3024 x 19314: 76 workgroups, 56 us for 117 MB).
+// Here a workgroup has 16 VT ids and 16 RT rows, and its four wavefronts a quarter of the columns each, so that there are several times as
+// many workgroups and every wavefront has 4 (VT + RT) loads of 16 bytes a lane in flight, with nothing to wait for but its own.  W's and the rows'
+// fragments come straight from memory (a load is 16 rows' 64 bytes, the next the other half of their lines); the rows are read where they are,
+// whatever d.  The quarters are joined through LDS, in one order, and wavefront j makes statistics and exponentials of row tile j as LearnEpilogue
+// does, with a reference for each workgroup's ids.
+struct ShortArgs {
+  const uint16_t* rows;
+  const uint16_t* W;
+  const float* ref;
+  float4* stats;            // [n, tiles]
+  float* moved;             // [n, tiles]
+  uint16_t* P;
+  int64_t ldp;
+  int n, d, V, tiles;
+  float to_log2;
+};
+
+template <int VT, int RT>
+__global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs p) {
+  constexpr int STEPS = 4;                     // of 32 columns, in flight together
+  constexpr float MOST = 60.f;
+  __shared__ f32x4 quarter[4][VT][RT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  const int tile = blockIdx.x, v0 = tile * 16 * VT, r0 = blockIdx.y * 16 * RT;
+  const uint16_t* w_at[VT];
+  const uint16_t* a_at[RT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t) w_at[t] = p.W + (int64_t)min(v0 + 16 * t + m, p.V - 1) * p.d + 8 * g;
+#pragma unroll
+  for (int j = 0; j < RT; ++j) a_at[j] = p.rows + (int64_t)min(r0 + 16 * j + m, p.n - 1) * p.d + 8 * g;
+  f32x4 acc[VT][RT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto take = [&](const bf16x8 (&w)[VT], const bf16x8 (&a)[RT]) {
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[t], a[j], acc[t][j], 0, 0, 0);
+  };
+  const int steps = (p.d + 31) / 32, each = (steps + 3) / 4, end = min((wave + 1) * each, steps), whole = min(end, p.d / 32);
+  int s = wave * each;
+  for (; s + STEPS <= whole; s += STEPS) {
+    bf16x8 w[STEPS][VT], a[STEPS][RT];
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+#pragma unroll
+      for (int t = 0; t < VT; ++t) w[u][t] = *reinterpret_cast<const bf16x8*>(w_at[t] + 32 * (s + u));
+#pragma unroll
+      for (int j = 0; j < RT; ++j) a[u][j] = *reinterpret_cast<const bf16x8*>(a_at[j] + 32 * (s + u));
+    }
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) take(w[u], a[u]);
+  }
+  for (; s < end; ++s) {                       // columns past the row's end: 0 on both sides (0 times an infinity would not do)
+    const bool in = 32 * s + 8 * g < p.d;
+    bf16x8 w[VT], a[RT];
+#pragma unroll
+    for (int t = 0; t < VT; ++t) w[t] = in ? *reinterpret_cast<const bf16x8*>(w_at[t] + 32 * s) : bf16x8{};
+#pragma unroll
+    for (int j = 0; j < RT; ++j) a[j] = in ? *reinterpret_cast<const bf16x8*>(a_at[j] + 32 * s) : bf16x8{};
+    take(w, a);
+  }
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) quarter[wave][t][j][lane] = acc[t][j];
+  __syncthreads();
+  if (wave >= RT) return;
+  // ids v0 + 16 t + 4 g + i of row r0 + 16 wave + m
+  const int row = r0 + 16 * wave + m, last = p.V - 1 - v0 - 4 * g;
+  const float ref = p.ref[min(row, p.n - 1)];
+  float x[VT][4], most = NEG_BIG;
+#pragma unroll
+  for (int t = 0; t < VT; ++t) {
+    const f32x4 z = (quarter[0][t][wave][lane] + quarter[1][t][wave][lane]) + (quarter[2][t][wave][lane] + quarter[3][t][wave][lane]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[t][i] = z[i] * p.to_log2;
+      most = 16 * t + i <= last ? fmaxf(most, x[t][i]) : most;
+    }
+  }
+  const auto larger = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
+  const auto add = [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
+  most = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(most), larger), larger));      // the row's four lanes
+  const float base = most - ref > MOST ? ceilf(most) : ref;
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < VT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[t][i] = 16 * t + i <= last ? __builtin_amdgcn_exp2f(x[t][i] - base) : 0.f;
+      sum += x[t][i];
+    }
+  sum = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(sum), add), add));
+  if (row >= p.n) return;
+  if (g == 0) {
+    p.stats[(int64_t)row * p.tiles + tile] = make_float4(base, sum, 0.f, 0.f);
+    p.moved[(int64_t)row * p.tiles + tile] = base;
+  }
+  uint16_t* const to = p.P + row * p.ldp + (v0 & ~31) + 8 * g;      // (see place_in_p)
+  if constexpr (VT == 1) {
+    *reinterpret_cast<uint2*>(to + 4 * ((v0 >> 4) & 1)) = make_uint2(pack_bf16(x[0][0], x[0][1]), pack_bf16(x[0][2], x[0][3]));
+  } else {
+#pragma unroll
+    for (int t = 0; t < VT; t += 2)
+      *reinterpret_cast<uint4*>(to + 16 * t) = make_uint4(pack_bf16(x[t][0], x[t][1]), pack_bf16(x[t][2], x[t][3]), pack_bf16(x[t + 1][0], x[t + 1][1]),
+                                                         pack_bf16(x[t + 1][2], x[t + 1][3]));
+  }
+}
+
 // A row a workgroup: its log-probability and its terms (a preference's factor comes later: ll_preference_pairs_kernel).  The own token's place in
 // P is made 0.  Tiles of P are brought to one base as in ll_distill_rows_kernel.
 template <bool POLICY>
@@ -153,7 +267,7 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
   __syncthreads();
   uint16_t* const at = p.P + row * p.ldp;
   if (shared_moved) {
-    tiles_to_base(at, p.ldp, p.moved + row * p.tiles, shared_base);
+    tiles_to_base(at, p.ldp, p.moved + row * p.tiles, shared_base, p.width);
     __syncthreads();
   }
   if (threadIdx.x == 0 && live) at[place_in_p(id)] = 0;
@@ -369,20 +483,51 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
 struct AnswerPlan {
   LearnPlan l;
   bool keep;                // the sums of all passes are joined behind the last
-  size_t terms, total;
+  int id_tiles, row_tiles;  // of 16, a workgroup of ll_answers_logits_kernel; id_tiles 0: the direct-to-LDS kernel
+  int parts;                // of a row's statistics
+  size_t stats, moved, terms, total;
 };
+
+// Whether ll_answers_logits_kernel is the faster one, by the tiles of 256 ids that the direct-to-LDS kernel would have.  Whole calls, us, through that
+// kernel | this one: d = 4096, V = 4000 (16 tiles), 16 rows 48 | 30, 64 53 | 45, 200 102 | 67, 400 110 | 100, 800 105 | 160; V = 8000 (32), 16 rows 53 | 39, 64
+// 59 | 54, 200 109 | 99, 400 119 | 165; V = 16 000 (63), 16 rows 83 | 64, 64 93 | 91, 100 101 | 103, 200 126 | 175; V = 32 000 (125), 16 rows 114 | 114, 64
+// 125 | 132; V = 50 257 (197), 16 rows 164 | 189; d = 8192, V = 4000, 16 rows 80 | 42, 400 180 | 166; d = 512, V = 4000, 16 rows 27 | 26, 400 47 | 42, 800
+// 46 | 49.  (It reads the rows again for every 64 ids, which is what bounds it with many of both.)
+bool few_ids(int rows, int tiles) { return tiles <= 100 && rows * tiles <= 6400; }
 
 AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
   AnswerPlan a = {};
   a.l = plan_for(s, 1, needs, 1);
-  const int64_t passes = (s->N + a.l.pass_rows - 1) / a.l.pass_rows;
+  const int64_t N = s->N > 0 ? s->N : 1, passes = (N + a.l.pass_rows - 1) / a.l.pass_rows;
   a.keep = pairs && needs == BACKWARD && passes > 1;
   if (a.keep) a.l = plan_for(s, 1, needs, passes);
+  a.parts = a.l.splits;
+  a.stats = a.l.stats;
+  a.moved = a.l.moved;
   a.total = a.l.total;
-  if (needs == FORWARD) return a;
-  a.terms = a.total;
-  a.total = align_up(a.total + (size_t)(s->N > 0 ? s->N : 1) * sizeof(AnswerTerms), 256);
+  const auto take = [&](size_t bytes) {
+    const size_t at = a.total;
+    a.total = align_up(a.total + bytes, 256);
+    return at;
+  };
+  // (the losses alone have ll_logp's workspace, and its kernel)
+  if (needs == BACKWARD && !a.l.few && few_ids(a.l.pass_rows, a.l.tiles)) {
+    const int blocks = (a.l.pass_rows + 63) / 64, ids = (int)a.l.ldp / 16;
+    a.row_tiles = ((a.l.pass_rows + blocks - 1) / blocks + 15) / 16;
+    a.id_tiles = ids / 4 * blocks >= NUM_CU ? 4 : ids / 2 * blocks >= NUM_CU ? 2 : 1;
+    a.parts = ids / a.id_tiles;
+    a.stats = take((size_t)a.l.pass_rows * a.parts * sizeof(float4));
+    a.moved = take((size_t)a.l.pass_rows * a.parts * sizeof(float));
+  }
+  if (needs == BACKWARD) a.terms = take((size_t)N * sizeof(AnswerTerms));
   return a;
+}
+
+using ShortKernel = void (*)(const ShortArgs);
+ShortKernel short_kernel(int id_tiles, int row_tiles) {
+  return with_row_tiles(row_tiles, [&](auto rt) -> ShortKernel {
+    return id_tiles == 4 ? ll_answers_logits_kernel<4, rt()> : id_tiles == 2 ? ll_answers_logits_kernel<2, rt()> : ll_answers_logits_kernel<1, rt()>;
+  });
 }
 
 // The first product of a pass and its rows' terms; POLICY: and losses.  Of few rows with a gradient, all there is.
@@ -412,18 +557,28 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
       return LL_OK;
     }
   } else {
+    const bool short_of_ids = a.id_tiles != 0;
     hipLaunchKernelGGL(ll_answers_tokens_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
-                       p.panel(), l.lda);
+                       short_of_ids ? nullptr : p.panel(), l.lda);
     LL_HIP_CHECK(hipGetLastError());
-    LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());
-    r.parts = l.splits;
+    r.stats = at<float4>(ws, a.stats);
+    r.parts = a.parts;
     r.stride = 1;
     if (terms != nullptr) {
       r.P = at<uint16_t>(ws, l.P);
       r.ldp = l.ldp;
       r.ref = at<float>(ws, l.ref);
-      r.moved = at<float>(ws, l.moved);
-      r.tiles = l.tiles;
+      r.moved = at<float>(ws, a.moved);
+      r.tiles = short_of_ids ? a.parts : l.tiles;
+      r.width = short_of_ids ? 16 * a.id_tiles : BM;
+    }
+    if (short_of_ids) {
+      const ShortArgs q = {p.rows, p.W, at<float>(ws, l.ref), at<float4>(ws, a.stats), at<float>(ws, a.moved), r.P, l.ldp, p.n, p.shape->d, p.shape->V,
+                           a.parts, p.to_log2};
+      hipLaunchKernelGGL(short_kernel(a.id_tiles, a.row_tiles), dim3(a.parts, (p.n + 16 * a.row_tiles - 1) / (16 * a.row_tiles)), dim3(256), 0, p.stream, q);
+      LL_HIP_CHECK(hipGetLastError());
+    } else {
+      LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());
     }
   }
   hipLaunchKernelGGL(ll_answers_rows_kernel<POLICY>, dim3(p.n), dim3(r.P != nullptr ? 256 : 64), 0, p.stream, r);

@@ -42,13 +42,15 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   return r;
 }
 
-// A row of P brought to one base, by a workgroup of 256 threads (see ll_distill_rows_kernel).
-__device__ __forceinline__ void tiles_to_base(uint16_t* at, int64_t ldp, const float* __restrict__ moved, float base) {
+// A row of P brought to one base, by a workgroup of 256 threads (see ll_distill_rows_kernel).  width: of a tile that has a reference of its own, 16 ids
+// or a multiple; eight places hold four ids of each half of 32 (see place_in_p).
+__device__ __forceinline__ void tiles_to_base(uint16_t* at, int64_t ldp, const float* __restrict__ moved, float base, int width = BM) {
   for (int64_t c = 8 * (int)threadIdx.x; c < ldp; c += 8 * 256) {
     const uint4 q = *reinterpret_cast<const uint4*>(at + c);
-    const float by = __builtin_amdgcn_exp2f(moved[c / BM] - base);
+    const int64_t id = c & ~(int64_t)31;
+    const float by = __builtin_amdgcn_exp2f(moved[id / width] - base), and_by = __builtin_amdgcn_exp2f(moved[(id + 16) / width] - base);
     *reinterpret_cast<uint4*>(at + c) = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
-                                                   pack_bf16(bf16_lo(q.z) * by, bf16_hi(q.z) * by), pack_bf16(bf16_lo(q.w) * by, bf16_hi(q.w) * by));
+                                                   pack_bf16(bf16_lo(q.z) * and_by, bf16_hi(q.z) * and_by), pack_bf16(bf16_lo(q.w) * and_by, bf16_hi(q.w) * and_by));
   }
 }
 

@@ -17,7 +17,11 @@ DEV = "cuda:0"
 # few rows of every width that they are dealt by; less than a tile, ragged, one pass and several, the gradient in one slice
 SIZES = [(1, 8, 1), (1, 64, 5), (2, 72, 257), (3, 328, 1000), (4, 1024, 900), (2, 2048, 700), (4, 4096, 600), (4, 8192, 1000), (2, 16384, 500),
          (3, 16384, 300), (5, 2504, 5001), (64, 256, 4096), (257, 128, 3001), (300, 1608, 2050), (33, 2560, 20000), (17, 200, 70000),
-         (600, 520, 60), (2048, 1024, 300), (2100, 64, 777), (4500, 72, 300)]
+         (600, 520, 60), (2048, 1024, 300), (2100, 64, 777), (4500, 72, 300),
+         # short vocabularies: 16, 32 and 64 ids a workgroup with one to four tiles of rows, one block of rows and several
+         (20, 136, 10000), (48, 72, 20001), (64, 264, 9000), (200, 40, 5000), (7, 24, 25000), (33, 1000, 4300), (16, 2048, 17000), (390, 96, 4096),
+         # and ones that are not
+         (70, 328, 26000), (300, 136, 30000), (4500, 72, 2000)]
 
 
 def case(N, d, V, seed=0):
@@ -219,10 +223,11 @@ def test_one_long_pair_over_several_passes():
     check_preference(a, W, ids, torch.tensor([0, 2600, N], dtype=torch.int32), None, None, 0.02, 0.0, "logistic", True, 1.0)
 
 
-def test_rows_far_from_the_token():
+@pytest.mark.parametrize("V", [2000, 12000, 20000, 30000])
+def test_rows_far_from_the_token(V):
     """A token 2^-150 as likely as the most likely one: the exponentials' reference moves, and the loss is as large as it is."""
-    N, d, V = 40, 64, 2000
-    say("policy and preference of impossible tokens")
+    N, d = 40, 64
+    say(f"policy and preference of impossible tokens V={V}")
     g = torch.Generator().manual_seed(3)
     W = torch.randn((V, d), generator=g).to(torch.bfloat16)
     a = (2.0 * W[torch.randint(0, V, (N,), generator=g)].float()).to(torch.bfloat16)
@@ -233,6 +238,23 @@ def test_rows_far_from_the_token():
     for rows in (N, 3):
         check_policy(a[:rows], W, ids[:rows], A[:rows], None, None, None, 0.2, 0.2, 0.0, 1.0)
         check_preference(a[:rows], W, ids[:rows], torch.tensor([0, 1, rows], dtype=torch.int32), None, None, 0.01, 0.0, "logistic", False, 1.0)
+
+
+def test_infinities_of_an_unembedding_stay_in_their_own_ids():
+    """Rows of W_U that hold an infinity or NaN in the last columns, beside a d that ends inside a step of 32: what they add is theirs, and where
+    every row is 0 there they add nothing but NaN to nobody's logit."""
+    say("infinities beside the end of a row")
+    for V in (3000, 30000):
+        d = 40
+        g = torch.Generator().manual_seed(5)
+        a, W = torch.randn((20, d), generator=g).to(torch.bfloat16), torch.randn((V, d), generator=g).to(torch.bfloat16)
+        ids = torch.randint(1, V, (20,), generator=g).to(torch.int32)
+        A = torch.ones((20,))
+        clean = LL.ll_policy(*[x.to(DEV) for x in (a, W, ids, A)])
+        big = torch.cat([W, torch.full((8, d), float("inf"), dtype=torch.bfloat16)])      # rows behind the vocabulary, right behind its last
+        got = LL.ll_policy(a.to(DEV), big.to(DEV)[:V], ids.to(DEV), A.to(DEV))
+        for x, y in zip(clean, got):
+            assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("N,d,V", [(4, 512, 900), (70, 328, 1000), (2100, 64, 777)])

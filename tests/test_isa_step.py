@@ -39,6 +39,6 @@ def test_norm(step):
 
 def test_answers(tmp_path):
     kernels = {n: m for n, m in metadata(T.assembly("ll_answers", tmp_path)).items() if "ll_answers" in n or "ll_preference" in n}
-    assert len(kernels) == 7
+    assert len(kernels) == 7 + 12                 # (16, 32 and 64 ids with one to four tiles of rows)
     for name, m in kernels.items():
-        assert m["vgpr"] <= 128 and m["scratch"] == 0 and m["spill"] == 0, (name, m)
+        assert m["vgpr"] <= (256 if "logits" in name else 128) and m["scratch"] == 0 and m["spill"] == 0, (name, m)
