@@ -46,7 +46,7 @@ struct AnswerArgs {
   // the products' P; nullptr with few rows, whose sums are relative to lse2
   uint16_t* P;
   int64_t ldp;
-  const float* ref;
+  const float* ref;           // [rows], or nullptr: 0
   const float* moved;         // [rows, tiles]: what the exponents of a tile of `width` ids are relative to
   int tiles, width;
   PolicyArgs policy;
@@ -119,12 +119,14 @@ __global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p
 // Here a workgroup has 16 VT ids and 16 RT rows, and its four wavefronts a quarter of the columns each, so that there are several times as
 // many workgroups and every wavefront has 4 (VT + RT) loads of 16 bytes a lane in flight, with nothing to wait for but its own.  W's and the rows'
 // fragments come straight from memory (a load is 16 rows' 64 bytes, the next the other half of their lines); the rows are read where they are,
-// whatever d.  The quarters are joined through LDS, in one order, and wavefront j makes statistics and exponentials of row tile j as LearnEpilogue
-// does, with a reference for each workgroup's ids.
+// whatever d.  The quarters are joined through LDS, in one order, and wavefront j makes statistics and exponentials of row tile j.  They are relative
+// to 0, which is as good as any reference within 60 powers of two of the largest logit; a workgroup whose ids are further off takes its own largest, a
+// whole number (see LearnEpilogue).  The row's token is met on the way: its logit goes to z, and its place in P is 0.
 struct ShortArgs {
   const uint16_t* rows;
   const uint16_t* W;
-  const float* ref;
+  const int32_t* ids;
+  float* z;
   float4* stats;            // [n, tiles]
   float* moved;             // [n, tiles]
   uint16_t* P;
@@ -187,8 +189,7 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
   __syncthreads();
   if (wave >= RT) return;
   // ids v0 + 16 t + 4 g + i of row r0 + 16 wave + m
-  const int row = r0 + 16 * wave + m, last = p.V - 1 - v0 - 4 * g;
-  const float ref = p.ref[min(row, p.n - 1)];
+  const int row = r0 + 16 * wave + m, last = p.V - 1 - v0 - 4 * g, own = p.ids[min(row, p.n - 1)] - v0 - 4 * g;
   float x[VT][4], most = NEG_BIG;
 #pragma unroll
   for (int t = 0; t < VT; ++t) {
@@ -197,12 +198,13 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
     for (int i = 0; i < 4; ++i) {
       x[t][i] = z[i] * p.to_log2;
       most = 16 * t + i <= last ? fmaxf(most, x[t][i]) : most;
+      if (16 * t + i == own && own <= last && row < p.n) p.z[row] = z[i];
     }
   }
   const auto larger = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
   const auto add = [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
   most = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(most), larger), larger));      // the row's four lanes
-  const float base = most - ref > MOST ? ceilf(most) : ref;
+  const float base = fabsf(most) > MOST && most > NEG_BIG ? ceilf(most) : 0.f;     // (NEG_BIG: no id, or no number)
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < VT; ++t)
@@ -210,6 +212,7 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
     for (int i = 0; i < 4; ++i) {
       x[t][i] = 16 * t + i <= last ? __builtin_amdgcn_exp2f(x[t][i] - base) : 0.f;
       sum += x[t][i];
+      if (16 * t + i == own) x[t][i] = 0.f;
     }
   sum = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(sum), add), add));
   if (row >= p.n) return;
@@ -243,11 +246,12 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
     id = p.ids[row];
     const bool valid = id >= 0 && id < p.V;
     const double l = log2_p(p.z[row], p.to_log2, r), logp = l * LN2_64;
+    const float ref = p.ref != nullptr ? p.ref[row] : 0.f;
     bool other = false;
     if (p.P != nullptr)
-      for (int i = lane; i < p.parts; i += 64) other |= p.stats[row * p.parts + i].x != p.ref[row];
+      for (int i = lane; i < p.parts; i += 64) other |= p.stats[row * p.parts + i].x != ref;
     other = __builtin_amdgcn_ballot_w64(other) != 0;
-    const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : p.ref[row];
+    const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : ref;
     PolicyTerm t = {0.f, 0.f};
     if (POLICY && valid) t = policy_term(p.policy, row, (float)logp);
     live = valid && (!POLICY || t.c != 0.f);
@@ -489,10 +493,10 @@ struct AnswerPlan {
 };
 
 // Whether ll_answers_logits_kernel is the faster one, by the tiles of 256 ids that the direct-to-LDS kernel would have.  Whole calls, us, through that
-// kernel | this one: d = 4096, V = 4000 (16 tiles), 16 rows 48 | 30, 64 53 | 45, 200 102 | 67, 400 110 | 100, 800 105 | 160; V = 8000 (32), 16 rows 53 | 39, 64
-// 59 | 54, 200 109 | 99, 400 119 | 165; V = 16 000 (63), 16 rows 83 | 64, 64 93 | 91, 100 101 | 103, 200 126 | 175; V = 32 000 (125), 16 rows 114 | 114, 64
-// 125 | 132; V = 50 257 (197), 16 rows 164 | 189; d = 8192, V = 4000, 16 rows 80 | 42, 400 180 | 166; d = 512, V = 4000, 16 rows 27 | 26, 400 47 | 42, 800
-// 46 | 49.  (It reads the rows again for every 64 ids, which is what bounds it with many of both.)
+// kernel | this one: d = 4096, V = 4000 (16 tiles), 16 rows 48 | 27, 64 53 | 42, 200 102 | 64, 400 110 | 97, 800 105 | 157; V = 8000 (32), 16 rows 53 | 36, 64
+// 59 | 51, 200 109 | 96, 400 119 | 162; V = 16 000 (63), 16 rows 83 | 61, 64 93 | 88, 100 101 | 100, 200 126 | 172; V = 32 000 (125), 16 rows 114 | 111, 64
+// 125 | 129; V = 50 257 (197), 16 rows 164 | 186; d = 8192, V = 4000, 16 rows 80 | 39, 400 180 | 160; d = 512, V = 4000, 16 rows 27 | 23, 400 47 | 39, 800
+// 46 | 46.  (It reads the rows again for every 64 ids, which is what bounds it with many of both.)
 bool few_ids(int rows, int tiles) { return tiles <= 100 && rows * tiles <= 6400; }
 
 AnswerPlan answer_plan(const ll_shape* s, bool pairs, Needs needs) {
@@ -557,27 +561,25 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
       return LL_OK;
     }
   } else {
-    const bool short_of_ids = a.id_tiles != 0;
-    hipLaunchKernelGGL(ll_answers_tokens_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref),
-                       short_of_ids ? nullptr : p.panel(), l.lda);
-    LL_HIP_CHECK(hipGetLastError());
     r.stats = at<float4>(ws, a.stats);
     r.parts = a.parts;
     r.stride = 1;
     if (terms != nullptr) {
       r.P = at<uint16_t>(ws, l.P);
       r.ldp = l.ldp;
-      r.ref = at<float>(ws, l.ref);
       r.moved = at<float>(ws, a.moved);
-      r.tiles = short_of_ids ? a.parts : l.tiles;
-      r.width = short_of_ids ? 16 * a.id_tiles : BM;
+      r.tiles = a.id_tiles != 0 ? a.parts : l.tiles;
+      r.width = a.id_tiles != 0 ? 16 * a.id_tiles : BM;
     }
-    if (short_of_ids) {
-      const ShortArgs q = {p.rows, p.W, at<float>(ws, l.ref), at<float4>(ws, a.stats), at<float>(ws, a.moved), r.P, l.ldp, p.n, p.shape->d, p.shape->V,
+    if (a.id_tiles != 0) {
+      const ShortArgs q = {p.rows, p.W, ids, at<float>(ws, l.z), at<float4>(ws, a.stats), at<float>(ws, a.moved), r.P, l.ldp, p.n, p.shape->d, p.shape->V,
                            a.parts, p.to_log2};
       hipLaunchKernelGGL(short_kernel(a.id_tiles, a.row_tiles), dim3(a.parts, (p.n + 16 * a.row_tiles - 1) / (16 * a.row_tiles)), dim3(256), 0, p.stream, q);
       LL_HIP_CHECK(hipGetLastError());
     } else {
+      r.ref = at<float>(ws, l.ref);
+      hipLaunchKernelGGL(ll_answers_tokens_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref), p.panel(), l.lda);
+      LL_HIP_CHECK(hipGetLastError());
       LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());
     }
   }
