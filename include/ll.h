@@ -377,7 +377,8 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
  *   clip_low   0 to 1;  clip_high  0 or more, infinity: no bound;  kl  finite, not negative
  *   out_loss, out_logp  fp32 [N];  out_grad  bf16 [N, d] = weight[r] d out_loss[r] / d rows[r, :], or NULL: the losses alone, for about half the
  *              time; the workspace may then be of ll_logp_workspace_bytes(shape, 1)
- * A ratio on the border of the clipping counts as inside.
+ * A ratio on the border of the clipping counts as inside.  The gradient keeps its digits where p is next to 1: it is made of the other tokens' sum.
+ * (Log-probabilities beside a gradient are made of it too, and may differ from the losses' alone by the rounding of the logits.)
  *
  * ll_preference: the loss of pairs of answers of which the first is preferred.  Sequence i is rows offsets[i] to offsets[i + 1] - 1, the pairs are
  * sequences 2 j (preferred) and 2 j + 1;

@@ -5,7 +5,8 @@
 //
 // Both products are those of distillation (ll_learn.hip): the first leaves P = 2^(x - base) behind it in bf16, the second multiplies P by W_U.
 // The row's own token is left out of P and its whole part, p - 1, which outweighs all others', joins the sums in fp32: rounded into P it would
-// be most of the gradient's error (rms, of the gradient: 0.0026 with it in P, 0.0017 without, which is the result's own rounding).
+// be most of the gradient's error (rms, of the gradient: 0.0026 with it in P, 0.0017 without, which is the result's own rounding).  p - 1 is the
+// others' sum over the whole, negated, and the first product keeps that sum by itself: with p next to 1 the difference is rounding.
 // What is new is c.  Nothing of it is needed before the second product's sums are rounded, where it is a factor of the row, so that the logits
 // are formed once: with the log-probabilities and their gradient as two calls there is a third product.  Whole calls, us, ll_policy | ll_logp, the loss in torch, ll_logp_grad: 1 row, d = 4096, V = 128256 175 | 364; 111,
 // 1608, 50257 97 | 161; 1500, 4096, 128256 2193 | 3190 (1.44 PFLOP/s; the vendor's bare product of that shape 1.28); 6000, 2560, 151936 6546 | 9510.
@@ -81,9 +82,13 @@ __device__ __forceinline__ double log2_p(float z, float to_log2, const RowStats&
   return (((double)z * (double)to_log2 - (double)r.ref) - (double)__builtin_amdgcn_frexp_expf(r.sum)) - (double)rest;
 }
 constexpr double LN2_64 = 0.69314718055994530942;
+// The log-probability itself, beside a gradient: above a half from the others' part, of which it has every digit.
+__device__ __forceinline__ double log_p(float z, float to_log2, const RowStats& r) {
+  return r.t < 0.5f * r.sum ? (double)log1pf(-r.t / r.sum) : log2_p(z, to_log2, r) * LN2_64;
+}
 
-// Before the first product: the rows padded, the tokens' logits (before the temperature; 0 without a token), and what P starts from, as in
-// ll_distill_lists_kernel.  One token a row, so a workgroup shares a row, and has all of it in flight at once.
+// Before the first product: the rows padded, the tokens' logits (before the temperature; 0 without a token; with a gradient the product's own take
+// their place), and what P starts from, as in ll_distill_lists_kernel.  One token a row, so a workgroup shares a row, and has all of it in flight at once.
 __global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p, float* __restrict__ z, float* __restrict__ ref, uint16_t* __restrict__ panel,
                                                                 int64_t lda) {
   __shared__ float part[4];
@@ -121,7 +126,7 @@ __global__ __launch_bounds__(256) void ll_answers_tokens_kernel(const ListArgs p
 // fragments come straight from memory (a load is 16 rows' 64 bytes, the next the other half of their lines); the rows are read where they are,
 // whatever d.  The quarters are joined through LDS, in one order, and wavefront j makes statistics and exponentials of row tile j.  They are relative
 // to 0, which is as good as any reference within 60 powers of two of the largest logit; a workgroup whose ids are further off takes its own largest, a
-// whole number (see LearnEpilogue).  The row's token is met on the way: its logit goes to z, and its place in P is 0.
+// whole number (see LearnEpilogue).  The row's token is met on the way: its logit goes to z, its place in P is 0, and the sum without it is kept.
 struct ShortArgs {
   const uint16_t* rows;
   const uint16_t* W;
@@ -196,8 +201,8 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
     const f32x4 z = (quarter[0][t][wave][lane] + quarter[1][t][wave][lane]) + (quarter[2][t][wave][lane] + quarter[3][t][wave][lane]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[t][i] = z[i] * p.to_log2;
-      most = 16 * t + i <= last ? fmaxf(most, x[t][i]) : most;
+      x[t][i] = z[i];
+      most = 16 * t + i <= last ? fmaxf(most, z[i] * p.to_log2) : most;
       if (16 * t + i == own && own <= last && row < p.n) p.z[row] = z[i];
     }
   }
@@ -205,19 +210,21 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
   const auto add = [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); };
   most = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(most), larger), larger));      // the row's four lanes
   const float base = fabsf(most) > MOST && most > NEG_BIG ? ceilf(most) : 0.f;     // (NEG_BIG: no id, or no number)
-  float sum = 0.f;
+  float sum = 0.f, others = 0.f;
 #pragma unroll
   for (int t = 0; t < VT; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[t][i] = 16 * t + i <= last ? __builtin_amdgcn_exp2f(x[t][i] - base) : 0.f;
+      x[t][i] = 16 * t + i <= last ? __builtin_amdgcn_exp2f(fmaf(x[t][i], p.to_log2, -base)) : 0.f;
       sum += x[t][i];
       if (16 * t + i == own) x[t][i] = 0.f;
+      others += x[t][i];
     }
   sum = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(sum), add), add));
+  others = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(others), add), add));
   if (row >= p.n) return;
   if (g == 0) {
-    p.stats[(int64_t)row * p.tiles + tile] = make_float4(base, sum, 0.f, 0.f);
+    p.stats[(int64_t)row * p.tiles + tile] = make_float4(base, sum, others, 0.f);
     p.moved[(int64_t)row * p.tiles + tile] = base;
   }
   uint16_t* const to = p.P + row * p.ldp + (v0 & ~31) + 8 * g;      // (see place_in_p)
@@ -231,21 +238,19 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
   }
 }
 
-// A row a workgroup: its log-probability and its terms (a preference's factor comes later: ll_preference_pairs_kernel).  The own token's place in
-// P is made 0.  Tiles of P are brought to one base as in ll_distill_rows_kernel.
+// A row a workgroup: its log-probability and its terms (a preference's factor comes later: ll_preference_pairs_kernel).  Tiles of P are brought to
+// one base as in ll_distill_rows_kernel.
 template <bool POLICY>
 __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p) {
   __shared__ float shared_base;
   __shared__ int shared_moved;
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x & 63;
-  int id = -1;
-  bool live = false;
   if (threadIdx.x < 64) {
-    const RowStats r = join_stats(p.stride == 1 ? p.stats + row * p.parts : p.stats + row, p.parts, lane, p.stride);
-    id = p.ids[row];
+    const RowStats r = join_stats<true>(p.stride == 1 ? p.stats + row * p.parts : p.stats + row, p.parts, lane, p.stride);
+    const int id = p.ids[row];
     const bool valid = id >= 0 && id < p.V;
-    const double l = log2_p(p.z[row], p.to_log2, r), logp = l * LN2_64;
+    const double logp = p.P != nullptr ? log_p(p.z[row], p.to_log2, r) : log2_p(p.z[row], p.to_log2, r) * LN2_64;
     const float ref = p.ref != nullptr ? p.ref[row] : 0.f;
     bool other = false;
     if (p.P != nullptr)
@@ -254,13 +259,13 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
     const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : ref;
     PolicyTerm t = {0.f, 0.f};
     if (POLICY && valid) t = policy_term(p.policy, row, (float)logp);
-    live = valid && (!POLICY || t.c != 0.f);
+    const bool live = valid && (!POLICY || t.c != 0.f);
     if (lane == 0) {
       p.logp[row] = valid ? (float)logp : NAN;
       if (POLICY) p.policy.loss[row] = t.loss;
       if (p.terms != nullptr) {
         const float unit = -p.inv_t * (p.P == nullptr ? 1.f : __builtin_amdgcn_exp2f(base - r.lse2));
-        const float own = __builtin_amdgcn_exp2f((float)l + (r.lse2 - base)) - __builtin_amdgcn_exp2f(r.lse2 - base);
+        const float own = -r.t * __builtin_amdgcn_exp2f(r.ref - base);
         p.terms[row] = {(float)(logp - (double)(float)logp), unit, own, POLICY && live ? unit * t.c : 0.f};
       }
       shared_moved = live && other;
@@ -269,12 +274,7 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
   }
   if (p.P == nullptr) return;
   __syncthreads();
-  uint16_t* const at = p.P + row * p.ldp;
-  if (shared_moved) {
-    tiles_to_base(at, p.ldp, p.moved + row * p.tiles, shared_base, p.width);
-    __syncthreads();
-  }
-  if (threadIdx.x == 0 && live) at[place_in_p(id)] = 0;
+  if (shared_moved) tiles_to_base(p.P + row * p.ldp, p.ldp, p.moved + row * p.tiles, shared_base, p.width);
 }
 
 struct PairArgs {
@@ -420,14 +420,14 @@ __global__ __launch_bounds__(256) void ll_answers_few_join_kernel(const FewJoinA
   FewColumns columns;
   columns.load(p, row);
   if (POLICY ? wave == 0 : wave < rows) {
-    const RowStats stats = join_stats(r.stats + of_wave, r.parts, lane, r.stride);
+    const RowStats stats = join_stats<true>(r.stats + of_wave, r.parts, lane, r.stride);
     const int id = r.ids[of_wave];
     if (lane == 0) {
-      logp[POLICY ? 0 : wave] = id >= 0 && id < r.V ? log2_p(r.z[of_wave], r.to_log2, stats) * LN2_64 : (double)NAN;
+      logp[POLICY ? 0 : wave] = id >= 0 && id < r.V ? log_p(r.z[of_wave], r.to_log2, stats) : (double)NAN;
       if (of_wave == row) {
         shared_ref = stats.lse2;
         shared_c = 0.f;
-        share[0] = -1.f;
+        share[0] = -stats.t * __builtin_amdgcn_exp2f(stats.ref - stats.lse2);
         id_of[0] = id < r.V ? id : -1;
       }
     }
@@ -551,7 +551,7 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
   r.policy = policy;
   if (l.few) {
     FewJoinArgs j = {};
-    LL_TRY(terms != nullptr ? p.few<EXPS>(ids, j.f) : p.few<STATS>(ids, j.f));
+    LL_TRY(terms != nullptr ? p.few<OTHERS>(ids, j.f) : p.few<STATS>(ids, j.f));
     j.parts = r.parts = l.few_parts;
     j.stride = r.stride = l.few_rows;
     j.out = (uint16_t*)out;
@@ -580,7 +580,7 @@ int answer_rows(const Pass& p, const AnswerPlan& a, void* ws, const int32_t* ids
       r.ref = at<float>(ws, l.ref);
       hipLaunchKernelGGL(ll_answers_tokens_kernel, dim3(p.n), dim3(256), 0, p.stream, p.list(ids), at<float>(ws, l.z), at<float>(ws, l.ref), p.panel(), l.lda);
       LL_HIP_CHECK(hipGetLastError());
-      LL_TRY(terms != nullptr ? p.logits<EXPS>() : p.logits<STATS>());
+      LL_TRY(terms != nullptr ? p.logits<OTHERS>(ids) : p.logits<STATS>());
     }
   }
   hipLaunchKernelGGL(ll_answers_rows_kernel<POLICY>, dim3(p.n), dim3(r.P != nullptr ? 256 : 64), 0, p.stream, r);

@@ -13,8 +13,8 @@ constexpr int STAGE_K = 64;                // columns (backwards: ids) of a stag
 constexpr size_t LEARN_LDS = 160 << 10;    // what they take of LDS
 constexpr float LN2 = 0.6931471805599453f;
 
-// Statistics only; and the exponentials; dz where the statistics are known.
-enum LearnWhat { STATS, EXPS, GRAD };
+// Statistics only; and the exponentials; dz where the statistics are known; the exponentials and sums without the row's own token.
+enum LearnWhat { STATS, EXPS, GRAD, OTHERS };
 constexpr float MASKED = -1024.f;  // an exponent that stands for a column past the vocabulary: 2^l is 0, and l times whatever a gradient is no infinity
 
 struct RowTerms {   // of a row's dz: with l = z log2 e - lse2, dz = 2^l (a + b l); its gradient is `factor` times P's product, zeros where that is 0
@@ -28,6 +28,7 @@ struct LearnArgs : GemmArgs {
   const RowTerms* terms;   // [rows]
   int64_t ldp;
   float to_log2;        // log2(e) / T
+  float* z;             // OTHERS: [rows], the logit of the row's token (`target`)
 };
 
 struct LearnBackArgs : BackArgs {

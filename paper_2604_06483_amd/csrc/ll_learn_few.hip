@@ -67,7 +67,7 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
 }
 
 template <int WHAT, int N, int NC, int GROUPS>
-__global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const FewLearnArgs p) {
+__device__ __forceinline__ void few_rows(const FewLearnArgs& p) {
   constexpr int R = few_learn_rows(N, NC), M = R * N, STEP = GROUPS * R;
   const int tpr = GROUPS > 1 ? FEW_LEARN_THREADS / GROUPS : blockDim.x;      // threads to a row of W
   constexpr int WAVES = GROUPS > 1 ? FEW_LEARN_THREADS / GROUPS / 64 : FEW_LEARN_THREADS / 64;   // of a group, at most
@@ -105,6 +105,7 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
       if (n < p.n && c < n8) a[n][i] = reinterpret_cast<const uint4*>(l.rows + (int64_t)n * l.d)[c];
     }
   const int value = lane >> VALUE_BIT, my_n = value / R, my_r = value % R;
+  const int own = WHAT == OTHERS && my_n < p.n ? l.ids[my_n] : -1;     // OTHERS: one token a row, as in ll_learn_gemm.hip
   float ref = NEG_BIG, s = 0.f, t = 0.f, term_a = 0.f, term_b = 0.f;   // of the lane's own value
   if (WHAT == GRAD) {
     ref = shared_terms[my_n].lse2;
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
       const auto most = [](uint32_t u, uint32_t v) { return __float_as_uint(fmaxf(__uint_as_float(u), __uint_as_float(v))); };
       const float m = __uint_as_float(over_bits<VALUE_BIT, log2_of(R)>(__float_as_uint(inside ? x : NEG_BIG), most));
       const float to_ref = m - ref > 24.f ? m : ref, before = ref - to_ref, keep = __builtin_amdgcn_exp2f(before);
-      t = keep * fmaf(before, s, t);
+      t = keep * (WHAT == OTHERS ? t : fmaf(before, s, t));
       s *= keep;
       ref = to_ref;
 #pragma unroll
@@ -229,6 +230,10 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
     }
     s += prob;
     if (WHAT == STATS) t = fmaf(prob, e, t);
+    if (WHAT == OTHERS) {
+      prob = step * STEP + group * R + my_r == own ? 0.f : prob;
+      t += prob;
+    }
     return WHAT == GRAD ? prob * fmaf(term_b, e, term_a) : prob;
   };
   if constexpr (N <= 2) {   // few instructions beside the read: one step after the other
@@ -312,7 +317,7 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
             const float before = q.x - m, keep = __builtin_amdgcn_exp2f(before);
             if (q.y == 0.f) continue;
             sum_s = fmaf(keep, q.y, sum_s);
-            sum_t += keep * fmaf(before, q.y, q.z);
+            sum_t += keep * (WHAT == OTHERS ? q.z : fmaf(before, q.y, q.z));
           }
           p.stats[part * N + n] = make_float4(m, sum_s, sum_t, 0.f);
         }
@@ -331,6 +336,22 @@ __global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const F
   }
 }
 
+template <int WHAT, int N, int NC, int GROUPS>
+__global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_kernel(const FewLearnArgs p) {
+  few_rows<WHAT, N, NC, GROUPS>(p);
+}
+
+template <int N, int NC, int GROUPS>
+__global__ __launch_bounds__(FEW_LEARN_THREADS) void ll_learn_few_others_kernel(const FewLearnArgs p) {
+  few_rows<OTHERS, N, NC, GROUPS>(p);
+}
+
+template <int WHAT, int N, int NC, int GROUPS>
+constexpr FewLearnKernel few_kernel() {
+  if constexpr (WHAT == OTHERS) return ll_learn_few_others_kernel<N, NC, GROUPS>;
+  else return ll_learn_few_kernel<WHAT, N, NC, GROUPS>;
+}
+
 }  // namespace
 
 namespace ll {
@@ -339,13 +360,13 @@ FewLearnKernel few_learn_kernel(LearnWhat what, int rows, int chunks, int groups
   const auto pick = [&](auto w, auto n) -> FewLearnKernel {
     constexpr int WHAT = w(), N = n();
     if constexpr (N <= 4) {
-      if (groups == 8) return ll_learn_few_kernel<WHAT, N, 1, 8>;
-      if (groups == 4) return ll_learn_few_kernel<WHAT, N, 1, 4>;
-      if (groups == 2) return ll_learn_few_kernel<WHAT, N, 1, 2>;
+      if (groups == 8) return few_kernel<WHAT, N, 1, 8>();
+      if (groups == 4) return few_kernel<WHAT, N, 1, 4>();
+      if (groups == 2) return few_kernel<WHAT, N, 1, 2>();
     }
-    if (chunks == 1) return ll_learn_few_kernel<WHAT, N, 1, 1>;
-    if (chunks == 2) return ll_learn_few_kernel<WHAT, N, 2, 1>;
-    if constexpr (N <= 2) return ll_learn_few_kernel<WHAT, N, 4, 1>;
+    if (chunks == 1) return few_kernel<WHAT, N, 1, 1>();
+    if (chunks == 2) return few_kernel<WHAT, N, 2, 1>();
+    if constexpr (N <= 2) return few_kernel<WHAT, N, 4, 1>();
     return nullptr;
   };
   const auto of = [&](auto w) -> FewLearnKernel {
@@ -357,6 +378,7 @@ FewLearnKernel few_learn_kernel(LearnWhat what, int rows, int chunks, int groups
     return nullptr;
   };
   if (what == STATS) return of(std::integral_constant<int, STATS>{});
+  if (what == OTHERS) return of(std::integral_constant<int, OTHERS>{});
   if (what == EXPS) return of(std::integral_constant<int, EXPS>{});
   return of(std::integral_constant<int, GRAD>{});
 }

@@ -8,7 +8,11 @@ namespace {
 
 static_assert(DK == STAGE_K && (size_t)SLOTS * SLOT_BYTES == LEARN_LDS, "as the host takes them");
 
-// STATS: statistics only; EXPS: and the exponentials; GRAD: dz where the statistics are known.
+// STATS: statistics only; EXPS: and the exponentials; GRAD: dz where the statistics are known; OTHERS: as EXPS, with the row's own token left
+// out of P and out of the sum, and its exponential beside that: what a gradient needs is p - 1 of that token, and where p is next to 1 a
+// difference of sums that are rounded by themselves holds nothing of it (1 - p = 1e-4 at d = 4096: 19 % off).  A row tile has two forms, with and
+// without a token of one of its 16 rows in it, and the first looks for it 32 columns at a time.  ll_policy and ll_preference, us, without any of this |
+// with | with the first form alone: 1500 x 4096 x 128256 2224 | 2229 | 2247; 6000 x 2560 x 151936 6653 | 6666 | 6739; 348 x 1608 x 50257 161 | 162 | 167.
 //
 // Exponents are relative to a reference that is no maximum: with fp32's range a sum of 2^(x - ref) does as well for any ref that is
 // not far from it, and so does bf16 for the exponentials, so that a tile takes one look at its accumulators and not two.  The reference
@@ -21,10 +25,12 @@ struct LearnEpilogue {
   struct State {   // of the lane's rows, 16 j + lane % 16 of the wavefront's; s and t over the vocabulary that the lane has seen
     float ref[RT], s[RT], t[RT];
     RowTerms terms[WHAT == GRAD ? RT : 1];
+    int own[WHAT == OTHERS ? RT : 1];
   };
+  static constexpr bool TO_P = WHAT == EXPS || WHAT == OTHERS;
   static constexpr bool RELOAD_FRAGMENTS = WHAT == STATS && RT == 4, OWN_U = false, BACK = false, PAST_CACHES = PAST, HALVES_APART = true;
   static constexpr int ROWS = 64 * RT, ROW_TILES = RT;
-  static constexpr float MOST = WHAT == EXPS ? 0x1p60f : 0x1p16f;
+  static constexpr float MOST = TO_P ? 0x1p60f : 0x1p16f;
   static __device__ __forceinline__ bool skip(const GemmArgs&) { return false; }
   static __device__ __forceinline__ int row_of(int my_row, int j) { return my_row - (threadIdx.x & 63) + 16 * j + (threadIdx.x & 15); }
   static __device__ __forceinline__ void init(State& st, const GemmArgs& args, int my_row, int) {
@@ -32,9 +38,10 @@ struct LearnEpilogue {
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
       const int row = min(row_of(my_row, j), p.rows - 1);
-      st.ref[j] = WHAT == EXPS ? p.ref[row] : NEG_BIG;
+      st.ref[j] = TO_P ? p.ref[row] : NEG_BIG;
       st.s[j] = st.t[j] = 0.f;
       if (WHAT == GRAD) st.terms[j] = p.terms[row];
+      if (WHAT == OTHERS) st.own[j] = p.target[row] < p.V ? p.target[row] : -1;
     }
   }
   template <class ACC>
@@ -46,22 +53,36 @@ struct LearnEpilogue {
   }
   // Whether column q of the lane's eight of columns 32 u .. is in the vocabulary.
   static __device__ __forceinline__ bool inside(int u, int q, int last) { return 16 * (2 * u + (q >> 2)) + (q & 3) <= last; }
-  // One row tile, eight values at a time: what they add to the sums, and what goes to P.  WHOLE: all columns are in the vocabulary.
-  template <bool WHOLE, class ACC>
-  static __device__ __forceinline__ float2 sums_of_tile(const ACC& acc, const State& st, int j, int last, float c, uint4* to, bool present) {
+  // One row tile, eight values at a time: what they add to the sums, and what goes to P.  WHOLE: all columns are in the vocabulary.  MEETS: own is the
+  // lane's column of its row's token, or none.
+  template <bool WHOLE, bool MEETS, class ACC>
+  static __device__ __forceinline__ float2 sums_of_tile(const ACC& acc, const State& st, int j, int last, float c, uint4* to, bool present, int own, float& logit) {
     float s = 0.f, t = 0.f;
     const float ref = WHAT == GRAD ? st.terms[j].lse2 : st.ref[j];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      float x[8];
+      float x[8], z[8];
+      const float before = s;
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        float l = fmaf(acc_read(acc[2 * u + (q >> 2)][j][q & 3]), c, -ref);
+        z[q] = acc_read(acc[2 * u + (q >> 2)][j][q & 3]);
+        float l = fmaf(z[q], c, -ref);
         if (!WHOLE) l = inside(u, q, last) ? l : MASKED;
         x[q] = __builtin_amdgcn_exp2f(l);
         if (WHAT == GRAD) x[q] *= fmaf(st.terms[j].b, l, st.terms[j].a);
         else s += x[q];
         if (WHAT == STATS) t = fmaf(x[q], l, t);
+      }
+      if (MEETS && __builtin_amdgcn_ballot_w64((own >> 5) == u) != 0) {
+        s = before;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const bool mine = 16 * (2 * u + (q >> 2)) + (q & 3) == own;
+          t = mine ? x[q] : t;
+          logit = mine ? z[q] : logit;
+          x[q] = mine ? 0.f : x[q];
+          s += x[q];
+        }
       }
       if (WHAT != STATS && present)
         to[4 * u] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
@@ -79,9 +100,19 @@ struct LearnEpilogue {
       const int row = row_of(my_row, j);
       const bool present = row < p.rows;
       uint4* const to = reinterpret_cast<uint4*>(p.P + row * p.ldp + v0 + 8 * g);
-      float2 add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
+      int own = -1;
+      if (WHAT == OTHERS) {
+        own = st.own[j] - v0 - 4 * g;             // (no token: -1, and so below 0)
+        if ((own & 15) >= 4) own = -1;            // (another lane's)
+      }
+      const bool meets = WHAT == OTHERS && __builtin_amdgcn_ballot_w64(own >= 0 && own < BM) != 0;
+      float logit = 0.f;
+      float2 add;
+      if (meets) add = sums_of_tile<WHOLE, WHAT == OTHERS>(acc, st, j, last, c, to, present, own, logit);
+      else add = sums_of_tile<WHOLE, false>(acc, st, j, last, c, to, present, own, logit);
       if (WHAT == GRAD) continue;
-      if (__builtin_amdgcn_ballot_w64(add.x > MOST) != 0) {
+      const auto large = [&] { return add.x > MOST || (WHAT == OTHERS && add.y > MOST); };
+      if (__builtin_amdgcn_ballot_w64(large()) != 0) {
         float m = NEG_BIG;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -96,17 +127,18 @@ struct LearnEpilogue {
         const auto any = [](uint32_t a, uint32_t b) { return a | b; };
         // the four lanes of a row together
         m = __uint_as_float(with_lane_xor<32>(with_lane_xor<16>(__float_as_uint(m), most), most)) * c;
-        const bool move = with_lane_xor<32>(with_lane_xor<16>(add.x > MOST ? 1u : 0u, any), any) != 0;
-        if (WHAT == EXPS) m = ceilf(m);   // (whole, as it was)
+        const bool move = with_lane_xor<32>(with_lane_xor<16>(large() ? 1u : 0u, any), any) != 0;
+        if (TO_P) m = ceilf(m);   // (whole, as it was)
         const float to_ref = move ? fmaxf(m, st.ref[j]) : st.ref[j], before = st.ref[j] - to_ref, keep = __builtin_amdgcn_exp2f(before);
-        st.t[j] = keep * fmaf(before, st.s[j], st.t[j]);
+        st.t[j] = keep * (WHAT == OTHERS ? st.t[j] : fmaf(before, st.s[j], st.t[j]));
         st.s[j] *= keep;
         st.ref[j] = to_ref;
-        add = sums_of_tile<WHOLE>(acc, st, j, last, c, to, present);
+        add = sums_of_tile<WHOLE, WHAT == OTHERS>(acc, st, j, last, c, to, present, own, logit);
       }
+      if (WHAT == OTHERS && own >= 0 && own < BM && present) p.z[row] = logit;
       st.s[j] += add.x;
       st.t[j] += add.y;
-      if (WHAT == EXPS && g == 0 && present) p.moved[(int64_t)row * p.tiles + v0 / BM] = st.ref[j];
+      if (TO_P && g == 0 && present) p.moved[(int64_t)row * p.tiles + v0 / BM] = st.ref[j];
     }
   }
   // The four lanes of a row have one reference.
@@ -118,7 +150,8 @@ struct LearnEpilogue {
     for (int j = 0; j < RT; ++j) {
       const int row = row_of(my_row, j);
       const float s = four(st.s[j]), t = four(st.t[j]);
-      if (row < p.rows && (threadIdx.x & 63) < 16) p.stats[(int64_t)row * p.splits + split] = make_float4(st.ref[j], s, t, 0.f);
+      if (row < p.rows && (threadIdx.x & 63) < 16)
+        p.stats[(int64_t)row * p.splits + split] = WHAT == OTHERS ? make_float4(st.ref[j], s + t, s, 0.f) : make_float4(st.ref[j], s, t, 0.f);
     }
   }
 };
@@ -128,6 +161,13 @@ __global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1))
 void ll_learn_logits_kernel(const LearnArgs p) {
   extern __shared__ __align__(16) unsigned char smem[];
   lens_gemm_dma<LearnEpilogue<WHAT, RT, PAST>, TAIL>(p, smem);
+}
+
+template <bool TAIL, int RT, bool PAST>
+__global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void ll_learn_others_kernel(const LearnArgs p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  lens_gemm_dma<LearnEpilogue<OTHERS, RT, PAST>, TAIL>(p, smem);
 }
 
 // dA = dz W over one slice of the vocabulary: the tile as it is, for ll_learn_join_kernel, or rounded where the slice is the whole.  A
@@ -192,6 +232,8 @@ LearnKernel learn_kernel(LearnWhat what, bool ragged, bool past_caches, int row_
              : past_caches ? ll_learn_logits_kernel<w(), false, rt(), true>
                            : ll_learn_logits_kernel<w(), false, rt(), false>;
     };
+    if (what == OTHERS) return ragged ? ll_learn_others_kernel<true, rt(), false> : past_caches ? ll_learn_others_kernel<false, rt(), true>
+                                                                                                : ll_learn_others_kernel<false, rt(), false>;
     if (what == STATS) return form(std::integral_constant<int, STATS>{});
     if (what == EXPS) return form(std::integral_constant<int, EXPS>{});
     return form(std::integral_constant<int, GRAD>{});

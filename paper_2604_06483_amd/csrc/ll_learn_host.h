@@ -17,7 +17,8 @@ struct RowStats {
   float lse2, t;     // log2 of the sum of 2^x; sum of p (x - lse2), x = z log2 e: minus the entropy, in powers of two
   float ref, sum;    // that sum is 2^ref sum
 };
-// A row's parts, `stride` apart, joined by a wavefront.
+// A row's parts, `stride` apart, joined by a wavefront.  OTHERS: they hold sums without the row's token, and so does t, relative to 2^ref.
+template <bool OTHERS = false>
 __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats, int parts, int lane, int stride = 1) {
   float m = NEG_BIG;
   bool nan = false;
@@ -32,12 +33,12 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
     const float4 q = stats[(int64_t)i * stride];
     const float by = q.x - m, e = __builtin_amdgcn_exp2f(by);
     s += q.y > 0.f ? e * q.y : 0.f;
-    t += q.y > 0.f ? e * fmaf(by, q.y, q.z) : 0.f;
+    t += q.y > 0.f ? e * (OTHERS ? q.z : fmaf(by, q.y, q.z)) : 0.f;
   }
   s = wave_sum(s);
   t = wave_sum(t);
   const float log_s = __builtin_amdgcn_logf(s);
-  RowStats r = {m + log_s, t / s - log_s, m, s};
+  RowStats r = {m + log_s, OTHERS ? t : t / s - log_s, m, s};
   if (wave_sum(nan ? 1.f : 0.f) > 0.f) r.lse2 = r.t = r.sum = NAN;
   return r;
 }
@@ -341,7 +342,7 @@ struct Pass {
   uint16_t* panel() const { return l.lda != shape->d ? at<uint16_t>(ws, l.panel) : nullptr; }
 
   template <LearnWhat WHAT>
-  int logits() const {
+  int logits(const int32_t* ids = nullptr) const {   // ids: OTHERS'
     LearnArgs p = {};
     p.A = panel() != nullptr ? panel() : rows;
     p.W = W;
@@ -362,6 +363,8 @@ struct Pass {
       p.moved = at<float>(ws, l.moved);
       p.ref = at<float>(ws, l.ref);
       p.terms = at<RowTerms>(ws, l.terms);
+      p.target = ids;
+      p.z = at<float>(ws, l.z);
     }
     const LearnKernel kernel = learn_kernel(WHAT, l.lda != shape->d, past_caches(), l.row_tiles);
     const size_t lds = LEARN_LDS;

@@ -356,3 +356,50 @@ def test_on_another_stream_and_in_a_batch():
     turned = a.view(4, 6, d).transpose(0, 1)
     got = LL.ll_policy(turned, W, ids.view(4, 6).T.contiguous(), A.view(4, 6).T.contiguous())
     assert torch.equal(got[2].transpose(0, 1).reshape(N, d), want[2])
+
+
+def sure_case(N, d, V, temperature):
+    """Every row next to certain of its token: 1 - p from some 5e-2 down to 1e-6 and less."""
+    _, W, ids, _ = inputs(N, d, V, 1, seed=21)
+    ids = ids[:, 0].clone()
+    own = W[ids.long()].float()
+    gap = torch.linspace(3.0, 20.0, N)[:, None]
+    return (own / (own * own).sum(1, keepdim=True) * ((math.log(V) + gap) * temperature)).to(torch.bfloat16), W, ids
+
+
+@pytest.mark.parametrize("N,d,V", [(1, 520, 3000), (4, 328, 5000), (3, 2560, 9000), (2, 8192, 2000),              # few rows
+                                   (20, 328, 4000), (70, 1024, 9000), (300, 136, 6001),                           # a short vocabulary
+                                   (40, 328, 30000), (300, 1024, 30000), (700, 264, 30001), (2100, 64, 30000)])   # and none
+@pytest.mark.parametrize("temperature", [1.0, 0.5])
+def test_tokens_that_the_model_is_sure_of(N, d, V, temperature):
+    """What is left of such a row's gradient is small, and has its digits all the same: the others' p is off by 2 ez (their logits and the sum),
+    by two roundings to bf16 and by some units of 2^-24, of itself; p - 1 is their sum; the result is rounded once.  So is l, which is 1 - p."""
+    say(f"sure of its tokens N={N} d={d} V={V} T={temperature}")
+    a, W, ids = sure_case(N, d, V, temperature)
+    r, w, n = f64(a), f64(W), ids.numpy()
+    ez = logit_error(r, w, temperature)
+    lp, _ = _log_softmax(r, w, temperature)
+    p = np.exp(lp)
+    np.put_along_axis(p, n[:, None], 0.0, 1)
+    rest = p.sum(1)
+    # (the inputs are as meant: the other logits spread by (ln V + 20) / sqrt d, 3.8 at d = 64, whose half square, 7, comes off the 20)
+    assert rest.max() < 0.3 and (N == 1 or rest.min() < 1e-5)
+    off = 2 * 2.0 ** -8 + 4 * ez + 2.0 ** -16
+    part = off * (p @ np.abs(w) + rest[:, None] * np.abs(w[n])) / temperature
+    unit = -(p @ w - rest[:, None] * w[n]) / temperature                  # d l / d row
+    A = torch.linspace(-1.0, 1.5, N) if N > 1 else torch.ones(1)
+    weight = 1 / torch.from_numpy(rest).float()
+    loss, logp, grad = LL.ll_policy(a.to(DEV), W.to(DEV), ids.to(DEV), A.to(DEV), weight=weight.to(DEV), temperature=temperature)
+    offsets = torch.tensor([0, N // 2, N], dtype=torch.int32)
+    ploss, score, plogp, pgrad = LL.ll_preference(a.to(DEV), W.to(DEV), ids.to(DEV), offsets.to(DEV), temperature=temperature)
+    l = np.log1p(-rest)
+    for got in (logp, plogp):
+        bad = np.abs(f64(got) - l) - ((4 * ez + 2.0 ** -18) * rest + 2.0 ** -23 * np.abs(l))
+        assert np.all(bad <= 0), float(bad.max())
+    h = 0.1 * (l[:N // 2].sum() - l[N // 2:].sum())
+    c = np.where(np.arange(N) < N // 2, -0.1, 0.1) / (1 + math.exp(h))
+    for got, by in ((grad, f64(A) * -f64(weight)), (pgrad, c)):
+        ref = by[:, None] * unit
+        bound = 2.0 ** -8 * np.abs(ref) + np.abs(by)[:, None] * part + 1e-37
+        bad = ~(np.abs(f64(got) - ref) <= bound)
+        assert not bad.any(), (int(bad.sum()), float(np.nanmax(np.abs(f64(got) - ref) / bound)))

@@ -42,3 +42,14 @@ def test_answers(tmp_path):
     assert len(kernels) == 7 + 12                 # (16, 32 and 64 ids with one to four tiles of rows)
     for name, m in kernels.items():
         assert m["vgpr"] <= (256 if "logits" in name else 128) and m["scratch"] == 0 and m["spill"] == 0, (name, m)
+
+
+def test_products_that_keep_the_others_sum(tmp_path):
+    kernels = {n: m for n, m in metadata(T.assembly("ll_learn_gemm", tmp_path)).items() if "ll_learn_others_kernel" in n}
+    assert len(kernels) == 12                     # one to four row tiles, of whole stages through and past the caches and of ragged ones
+    for name, m in kernels.items():
+        assert m["vgpr"] <= 512 and m["scratch"] == 0 and m["spill"] == 0, (name, m)
+    kernels = {n: m for n, m in metadata(T.assembly("ll_learn_few", tmp_path)).items() if "ll_learn_few_others_kernel" in n}
+    assert len(kernels) == 6 + 6 + 5
+    for name, m in kernels.items():
+        assert m["vgpr"] <= 256 and m["scratch"] == 0 and m["spill"] == 0, (name, m)
