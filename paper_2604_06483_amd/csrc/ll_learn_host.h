@@ -43,13 +43,20 @@ __device__ __forceinline__ RowStats join_stats(const float4* __restrict__ stats,
   return r;
 }
 
+// What brings a tile of P, relative to `moved`, to the row's base.  A tile that adds to the row's sum has a reference at most 60 powers of two above the
+// sum; one past the vocabulary, or of ids that have no probability, holds zeros relative to anything, and 0 times infinity is none.  (NaN passes.)
+__device__ __forceinline__ float tile_to_base(float moved, float base) {
+  const float up = moved - base;
+  return __builtin_amdgcn_exp2f(up > 127.f ? 127.f : up);
+}
+
 // A row of P brought to one base, by a workgroup of 256 threads (see ll_distill_rows_kernel).  width: of a tile that has a reference of its own, 16 ids
 // or a multiple; eight places hold four ids of each half of 32 (see place_in_p).
 __device__ __forceinline__ void tiles_to_base(uint16_t* at, int64_t ldp, const float* __restrict__ moved, float base, int width = BM) {
   for (int64_t c = 8 * (int)threadIdx.x; c < ldp; c += 8 * 256) {
     const uint4 q = *reinterpret_cast<const uint4*>(at + c);
     const int64_t id = c & ~(int64_t)31;
-    const float by = __builtin_amdgcn_exp2f(moved[id / width] - base), and_by = __builtin_amdgcn_exp2f(moved[(id + 16) / width] - base);
+    const float by = tile_to_base(moved[id / width], base), and_by = tile_to_base(moved[(id + 16) / width], base);
     *reinterpret_cast<uint4*>(at + c) = make_uint4(pack_bf16(bf16_lo(q.x) * by, bf16_hi(q.x) * by), pack_bf16(bf16_lo(q.y) * by, bf16_hi(q.y) * by),
                                                    pack_bf16(bf16_lo(q.z) * and_by, bf16_hi(q.z) * and_by), pack_bf16(bf16_lo(q.w) * and_by, bf16_hi(q.w) * and_by));
   }
