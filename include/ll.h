@@ -390,7 +390,8 @@ int ll_distill(const ll_shape* shape, void* workspace, size_t workspace_bytes, c
  *
  *   offsets    int32 [2 n_pairs + 1], device, ascending, within [0, N]; a sequence may be empty (score 0).  Others make losses and gradients
  *              unspecified, but nothing outside the tensors is read or written
- *   ref_logp   fp32 [N] or NULL (0);  weight  fp32 [n_pairs] or NULL (1): of the pair, in the gradient; 0: none, whatever the pair holds
+ *   ref_logp   fp32 [N] or NULL (0); an infinite one makes its score infinite, and the loss is its limit;  weight  fp32 [n_pairs] or NULL (1): of the
+ *              pair, in the gradient; 0: none, whatever the pair holds
  *   beta       positive, finite;  smoothing  0 to 1/2, 0 but for the logistic form
  *   out_loss   fp32 [n_pairs];  out_score  fp32 [n_pairs, 2];  out_logp  fp32 [N]
  *   out_grad   bf16 [N, d] or NULL, as above; rows of no sequence get zeros

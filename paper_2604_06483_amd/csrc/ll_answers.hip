@@ -314,7 +314,8 @@ __device__ __forceinline__ PairTerm pair_term(const PairArgs& p, const double (&
     const float e = expf(-fabsf(h)), soft = log1pf(e);
     const float to = 1.f / (1.f + e), from = e / (1.f + e);        // sigmoids of |h| and of -|h|
     const float up = h > 0.f ? to : from, down = h > 0.f ? from : to;
-    t.loss = (1.f - p.smoothing) * (soft + fmaxf(-h, 0.f)) + p.smoothing * (soft + fmaxf(h, 0.f));
+    t.loss = (1.f - p.smoothing) * (soft + fmaxf(-h, 0.f));
+    if (p.smoothing != 0.f) t.loss = fmaf(p.smoothing, soft + fmaxf(h, 0.f), t.loss);       // (0 times an infinite h is no 0)
     t.slope = p.smoothing * up - (1.f - p.smoothing) * down;
     if (h != h) t.loss = t.slope = h;
   } else if (p.form == LL_PREFERENCE_HINGE) {
