@@ -694,6 +694,7 @@ class TensorList:
         kept = lambda of: [x.detach() if isinstance(x, _Tensor) else x for x in of]
         self.grads = kept(grads)
         count = len(self.grads)
+        self.sizes = []
         for name, of in kinds.items():
             of = [None] * count if of is None else kept(of)
             if len(of) != count:
@@ -710,6 +711,7 @@ class TensorList:
             t = self.array[i]
             t.flags = self._grad_flag(g, f"grads[{i}]")
             t.n, t.grad = g.numel(), g.data_ptr()
+            self.sizes.append(g.shape)
             if not self.whole:
                 continue
             p = self.params[i]
@@ -750,16 +752,17 @@ class TensorList:
         return LL_TENSOR_GRAD_BF16 if bf16 else 0
 
     def set_grads(self, grads):
-        """Other gradients of the same shapes (a backward pass that made new tensors)."""
+        """Other gradients of the same shapes (a backward pass that made new tensors).  None in a gradient's place lets its memory go: the list is then
+        refused by the calls until there is another."""
         grads = [g.detach() if isinstance(g, _Tensor) else g for g in grads]
         if len(grads) != len(self.grads):
             raise ValueError(f"grads: {len(grads)} tensors, expected {len(self.grads)}")
-        flags = [self._grad_flag(g, f"grads[{i}]") for i, g in enumerate(grads)]
-        for i, (g, old) in enumerate(zip(grads, self.grads)):
-            if g.shape != old.shape:
-                raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, expected {tuple(old.shape)}")
+        flags = [0 if g is None else self._grad_flag(g, f"grads[{i}]") for i, g in enumerate(grads)]
+        for i, (g, size) in enumerate(zip(grads, self.sizes)):
+            if g is not None and g.shape != size:
+                raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, expected {tuple(size)}")
         for t, g, flag in zip(self.array, grads, flags):        # (all of them or none)
-            t.grad, t.flags = g.data_ptr(), (t.flags & ~LL_TENSOR_GRAD_BF16) | flag
+            t.grad, t.flags = _ptr(g), (t.flags & ~LL_TENSOR_GRAD_BF16) | flag
         self.grads = grads
 
     def __len__(self):

@@ -206,7 +206,7 @@ class AdamW(torch.optim.Optimizer):
         return s
 
     def _list(self, key, params, grads):
-        """The parameters' TensorList, kept from step to step, with this step's gradients."""
+        """The parameters' TensorList, kept from step to step, with this step's gradients (which it lets go with the step)."""
         kept = self._lists.get(key)
         states = [self.state[p] for p in params]
         copies = [self.copies.get(p) for p in params]
@@ -240,16 +240,28 @@ class AdamW(torch.optim.Optimizer):
                 loss = closure()
         if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("a captured step would repeat one step number: capture ll_adamw with a clock")
-        calls = []
+        try:
+            self._step()
+        finally:
+            # (kept, this step's gradients would stand in memory beside those of the next backward pass)
+            for tensors in self._lists.values():
+                tensors.set_grads([None] * len(tensors))
+        return loss
+
+    def _step(self):
+        calls, used = [], set()
         for at, group in enumerate(self.param_groups):
             by_step = {}                                  # (parameters that were without a gradient at times have done fewer steps)
             for p in group["params"]:
                 if p.grad is not None:
                     by_step.setdefault(self._state(p)["step"], []).append(p)
             for turn, (done, params) in enumerate(by_step.items()):
+                used.add((at, turn))
                 calls.append((group, done + 1, params, self._list((at, turn), params, [self._whole(p.grad) for p in params])))
+        # (a group whose parameters are at one step again needs one list; one that had no gradients keeps its own)
+        self._lists = {key: kept for key, kept in self._lists.items() if key in used or (key[0], 0) not in used}
         if not calls:
-            return loss
+            return
         self.norm = None
         if self.max_norm is not None:
             one = calls[0][3] if len(calls) == 1 else LL.TensorList([g for *_, tensors in calls for g in tensors.grads])
@@ -260,7 +272,6 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 self.state[p]["step"] = step
                 torch.autograd.graph.increment_version(p)
-        return loss
 
     def load_state_dict(self, state_dict):
         """As torch's, which would bring every state to its parameter's type: here they keep their own."""
