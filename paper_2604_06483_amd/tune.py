@@ -103,10 +103,10 @@ class _Preference(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, W_U, ids, offsets, weight, options):
         loss, score, logp, grad = LL.ll_preference(rows, W_U, ids, offsets, weight=weight, grad=ctx.needs_input_grad[0], **options)
-        ctx.save_for_backward(grad, loss if ctx.needs_input_grad[4] else None, offsets)
+        ctx.save_for_backward(grad, loss.reshape(weight.shape) if ctx.needs_input_grad[4] else None, offsets)
         ctx.mark_non_differentiable(score, logp)
         ctx.set_materialize_grads(False)
-        return loss if weight is None else (weight * loss).masked_fill(weight == 0, 0.0), score, logp
+        return loss if weight is None else (weight.reshape(-1) * loss).masked_fill(weight.reshape(-1) == 0, 0.0), score, logp
 
     @staticmethod
     @once_differentiable
@@ -123,7 +123,7 @@ class _Preference(torch.autograd.Function):
             inside = pair < g_loss.shape[0]
             by = torch.where(inside, torch.cat([g_loss, g_loss.new_zeros((1,))])[pair], 0.0)
             d_rows = (by[:, None] * flat).to(grad.dtype).reshape(grad.shape)
-        return d_rows, None, None, None, None if loss is None else g_loss * loss, None
+        return d_rows, None, None, None, None if loss is None else g_loss.reshape(loss.shape) * loss, None
 
 
 def _no_gradient(**tensors):
