@@ -53,7 +53,8 @@ struct AnswerArgs {
   PolicyArgs policy;
 };
 
-// Loss of a sampled token and what it gains by the token's log-probability.  A ratio on the border of the clipping counts as inside.
+// Loss of a sampled token and what it gains by the token's log-probability.  A ratio on the border of the clipping counts as inside; an advantage of 0
+// has no loss, whatever the ratio, but that of a row that holds no number.
 struct PolicyTerm {
   float loss, c;
 };
@@ -63,8 +64,9 @@ __device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs& p, int64_t r
   const float most = 1.f + p.high, least = 1.f - p.low;
   const bool clipped = A > 0.f ? ratio > most : ratio < least;
   PolicyTerm r;
-  r.loss = A == 0.f ? 0.f : -A * (clipped ? (A > 0.f ? most : least) : ratio);   // (an advantage of 0 has no loss, whatever the ratio)
+  r.loss = A == 0.f ? 0.f : -A * (clipped ? (A > 0.f ? most : least) : ratio);
   r.c = A == 0.f || clipped ? 0.f : -A * ratio;
+  if (logp != logp) r.loss = r.c = logp;
   if (p.ref_logp != nullptr) {
     const float q = p.ref_logp[row] - logp, e = expm1f(q);     // e^q - 1 keeps its digits where the two policies are near
     r.loss = fmaf(p.kl, e - q, r.loss);
