@@ -44,8 +44,7 @@ struct AnswerArgs {
   float to_log2, inv_t;
   float* logp;
   AnswerTerms* terms;         // or nullptr: no gradient
-  // the products' P; nullptr with few rows, whose sums are relative to lse2
-  uint16_t* P;
+  uint16_t* P;                // the products', where there are terms; else nullptr
   int64_t ldp;
   const float* ref;           // [rows], or nullptr: 0
   const float* moved;         // [rows, tiles]: what the exponents of a tile of `width` ids are relative to
@@ -258,7 +257,7 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
     if (p.P != nullptr)
       for (int i = lane; i < p.parts; i += 64) other |= p.stats[row * p.parts + i].x != ref;
     other = __builtin_amdgcn_ballot_w64(other) != 0;
-    const float base = p.P == nullptr ? r.lse2 : other ? rintf(r.lse2) : ref;
+    const float base = other ? rintf(r.lse2) : ref;
     PolicyTerm t = {0.f, 0.f};
     if (POLICY && valid) t = policy_term(p.policy, row, (float)logp);
     const bool live = valid && (!POLICY || t.c != 0.f);
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(256) void ll_answers_rows_kernel(const AnswerArgs p
       p.logp[row] = valid ? (float)logp : NAN;
       if (POLICY) p.policy.loss[row] = t.loss;
       if (p.terms != nullptr) {
-        const float unit = -p.inv_t * (p.P == nullptr ? 1.f : __builtin_amdgcn_exp2f(base - r.lse2));
+        const float unit = -p.inv_t * __builtin_amdgcn_exp2f(base - r.lse2);
         const float own = -r.t * __builtin_amdgcn_exp2f(r.ref - base);
         p.terms[row] = {(float)(logp - (double)(float)logp), unit, own, POLICY && live ? unit * t.c : 0.f};
       }
