@@ -195,7 +195,8 @@ __global__ __launch_bounds__(256) void ll_answers_logits_kernel(const ShortArgs 
   __syncthreads();
   if (wave >= RT) return;
   // ids v0 + 16 t + 4 g + i of row r0 + 16 wave + m
-  const int row = r0 + 16 * wave + m, last = p.V - 1 - v0 - 4 * g, own = p.ids[min(row, p.n - 1)] - v0 - 4 * g;
+  const int row = r0 + 16 * wave + m, last = p.V - 1 - v0 - 4 * g, id = p.ids[min(row, p.n - 1)];
+  const int own = (id >= 0 ? id : -1) - v0 - 4 * g;                // (no token: below 0 or past the vocabulary's last, whatever the id)
   float x[VT][4], most = NEG_BIG;
 #pragma unroll
   for (int t = 0; t < VT; ++t) {

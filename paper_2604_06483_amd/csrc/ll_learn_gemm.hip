@@ -41,7 +41,7 @@ struct LearnEpilogue {
       st.ref[j] = TO_P ? p.ref[row] : NEG_BIG;
       st.s[j] = st.t[j] = 0.f;
       if (WHAT == GRAD) st.terms[j] = p.terms[row];
-      if (WHAT == OTHERS) st.own[j] = p.target[row] < p.V ? p.target[row] : -1;
+      if (WHAT == OTHERS) st.own[j] = (uint32_t)p.target[row] < (uint32_t)p.V ? p.target[row] : -1;
     }
   }
   template <class ACC>
