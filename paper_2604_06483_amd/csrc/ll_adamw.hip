@@ -227,14 +227,18 @@ struct StepFour {
 #pragma unroll
     for (int i = 0; i < 4; ++i) moments(g[i] * clip, m[i], v[i], p.beta1, p.less1, p.beta2, p.less2);
     // The quotient's last bits are far below the parameter's: the hardware's own root and reciprocal, each within one.  They take subnormal numbers
-    // for 0, which is nothing beside an eps that is large beside their roots.
+    // for 0, which is nothing beside an eps that is large beside their roots.  (1 / eps may be more than 32 bits hold, and an element without a gradient
+    // would be 0 times infinity.)
     if (p.eps >= 1e-10f) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         w[i] = fmaf(-terms.rate * m[i], __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), terms.root, p.eps)), w[i] * terms.keep);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = fmaf(-terms.rate * m[i], 1.f / fmaf(sqrtf(v[i]), terms.root, p.eps), w[i] * terms.keep);
+      for (int i = 0; i < 4; ++i) {
+        const float under = fmaf(sqrtf(v[i]), terms.root, p.eps), by = 1.f / under, up = -terms.rate * m[i];
+        w[i] = by < INFINITY ? fmaf(up, by, w[i] * terms.keep) : fmaf(w[i], terms.keep, up / under);
+      }
     }
     uint32_t words[4];
     if (STATE_8 || PARAM_BF16) {
