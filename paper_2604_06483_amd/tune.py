@@ -207,18 +207,18 @@ class AdamW(torch.optim.Optimizer):
 
     def _list(self, key, params, grads):
         """The parameters' TensorList, kept from step to step, with this step's gradients (which it lets go with the step)."""
-        kept = self._lists.get(key)
         states = [self.state[p] for p in params]
         copies = [self.copies.get(p) for p in params]
         # (the list keeps its tensors' memory: what begins where one of them does is that one, unless it has been given other memory)
         at = lambda x: None if x is None else x.data_ptr()
-        if kept is not None and len(kept) == len(params) and all(
-                at(p) == at(q) and p.dtype == q.dtype and at(s["m"]) == at(m) and at(s["v"]) == at(v) and at(c) == at(k)
-                for p, q, s, m, v, c, k in zip(params, kept.params, states, kept.m, kept.v, copies, kept.copies)):
-            kept.set_grads(grads)
-            return kept
+        where = [(at(p), p.dtype, *(at(s.get(n)) for n in ("m", "v", "m_scale", "v_scale")), at(c)) for p, s, c in zip(params, states, copies)]
+        found = self._lists.get(key)
+        if found is not None and found[0] == where:
+            found[1].set_grads(grads)
+            return found[1]
         pick = lambda name: [s.get(name) for s in states]
-        kept = self._lists[key] = LL.TensorList(grads, params, pick("m"), pick("v"), pick("m_scale"), pick("v_scale"), copies)
+        kept = LL.TensorList(grads, params, pick("m"), pick("v"), pick("m_scale"), pick("v_scale"), copies)
+        self._lists[key] = where, kept
         return kept
 
     @staticmethod
@@ -244,7 +244,7 @@ class AdamW(torch.optim.Optimizer):
             self._step()
         finally:
             # (kept, this step's gradients would stand in memory beside those of the next backward pass)
-            for tensors in self._lists.values():
+            for _, tensors in self._lists.values():
                 tensors.set_grads([None] * len(tensors))
         return loss
 
