@@ -274,8 +274,18 @@ class AdamW(torch.optim.Optimizer):
                 torch.autograd.graph.increment_version(p)
 
     def load_state_dict(self, state_dict):
-        """As torch's, which would bring every state to its parameter's type: here they keep their own."""
-        super().load_state_dict(state_dict)
+        """As torch's, which would bring every state to its parameter's type: here they keep their own.  Hooks before it may give other states, and hooks
+        behind it see those that were loaded."""
+        given = []
+        ours = [self.register_load_state_dict_pre_hook(lambda _, state_dict: given.append(state_dict)),
+                self.register_load_state_dict_post_hook(lambda _: self._take(given[-1]), prepend=True)]
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for hook in ours:
+                hook.remove()
+
+    def _take(self, state_dict):
         theirs = [i for group in state_dict["param_groups"] for i in group["params"]]
         ours = [p for group in self.param_groups for p in group["params"]]
         for i, p in zip(theirs, ours):

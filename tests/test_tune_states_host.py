@@ -23,3 +23,31 @@ def test_a_state_in_other_memory_is_another(steps):  # noqa: F811
         assert List.made == made + 1, name
         opt.step()
         assert List.made == made + 1, name
+
+
+def test_hooks_after_loading_see_the_states_as_they_are(steps):  # noqa: F811
+    a, opt = stepped()
+    b = torch.nn.Parameter(a.detach().clone())
+    other, seen = tune.AdamW([b], bits=8), []
+    other.register_load_state_dict_post_hook(lambda o: seen.append({k: x.dtype for k, x in o.state[b].items() if k != "step"}))
+    other.load_state_dict(opt.state_dict())
+    assert seen == [dict(m=torch.float8_e4m3fn, v=torch.float8_e5m2, m_scale=torch.float32, v_scale=torch.float32)]
+    other.load_state_dict(opt.state_dict())
+    assert len(seen) == 2
+
+
+def test_what_a_hook_before_loading_returns_is_loaded(steps):  # noqa: F811
+    a, opt = stepped()
+    b = torch.nn.Parameter(a.detach().clone())
+    other = tune.AdamW([b], bits=8)
+
+    def forgets(o, given):
+        state = {i: dict(s, step=40, m=torch.zeros(300, dtype=torch.uint8).view(torch.float8_e4m3fn)) for i, s in given["state"].items()}
+        return dict(given, state=state)
+
+    hook = other.register_load_state_dict_pre_hook(forgets)
+    other.load_state_dict(opt.state_dict())
+    assert other.state[b]["step"] == 40 and not other.state[b]["m"].view(torch.uint8).any() and opt.state[a]["step"] == 1
+    hook.remove()
+    other.load_state_dict(opt.state_dict())
+    assert other.state[b]["step"] == 1 and other.state[b]["m"].view(torch.uint8).any()
