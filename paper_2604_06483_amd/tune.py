@@ -272,6 +272,8 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 self.state[p]["step"] = step
                 torch.autograd.graph.increment_version(p)
+                if p in self.copies:
+                    torch.autograd.graph.increment_version(self.copies[p])
 
     def load_state_dict(self, state_dict):
         """As torch's, which would bring every state to its parameter's type: here they keep their own.  Hooks before it may give other states, and hooks

@@ -51,3 +51,13 @@ def test_what_a_hook_before_loading_returns_is_loaded(steps):  # noqa: F811
     hook.remove()
     other.load_state_dict(opt.state_dict())
     assert other.state[b]["step"] == 1 and other.state[b]["m"].view(torch.uint8).any()
+
+
+def test_autograd_knows_that_a_copy_is_another(steps):  # noqa: F811
+    a = torch.nn.Parameter(torch.ones(8))
+    copy = a.detach().bfloat16()
+    opt = tune.AdamW([a], copies={a: copy})
+    a.grad = torch.ones(8)
+    before = copy._version
+    opt.step()
+    assert copy._version > before
