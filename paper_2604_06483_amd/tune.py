@@ -272,7 +272,7 @@ class AdamW(torch.optim.Optimizer):
             for p in params:
                 self.state[p]["step"] = step
                 torch.autograd.graph.increment_version(p)
-                if p in self.copies:
+                if self.copies.get(p) is not None:
                     torch.autograd.graph.increment_version(self.copies[p])
 
     def load_state_dict(self, state_dict):

@@ -56,8 +56,9 @@ def test_what_a_hook_before_loading_returns_is_loaded(steps):  # noqa: F811
 def test_autograd_knows_that_a_copy_is_another(steps):  # noqa: F811
     a = torch.nn.Parameter(torch.ones(8))
     copy = a.detach().bfloat16()
-    opt = tune.AdamW([a], copies={a: copy})
-    a.grad = torch.ones(8)
+    b = torch.nn.Parameter(torch.ones(8))
+    opt = tune.AdamW([a, b], copies={a: copy, b: None})
+    a.grad = b.grad = torch.ones(8)
     before = copy._version
     opt.step()
     assert copy._version > before
