@@ -754,11 +754,18 @@ class TensorList:
     def set_grads(self, grads):
         """Other gradients of the same shapes (a backward pass that made new tensors).  None in a gradient's place lets its memory go: the list is then
         refused by the calls until there is another."""
-        grads = [g.detach() if isinstance(g, _Tensor) else g for g in grads]
+        grads = list(grads)
         if len(grads) != len(self.grads):
             raise ValueError(f"grads: {len(grads)} tensors, expected {len(self.grads)}")
-        flags = [0 if g is None else self._grad_flag(g, f"grads[{i}]") for i, g in enumerate(grads)]
+        if all(g is None for g in grads):
+            self.grads = grads
+            for t in self.array:
+                t.grad = None
+            return
+        grads = [g.detach() if isinstance(g, _Tensor) else g for g in grads]
+        flags = []
         for i, (g, size) in enumerate(zip(grads, self.sizes)):
+            flags.append(0 if g is None else self._grad_flag(g, f"grads[{i}]"))
             if g is not None and g.shape != size:
                 raise ValueError(f"grads[{i}]: shape {tuple(g.shape)}, expected {tuple(size)}")
         for t, g, flag in zip(self.array, grads, flags):        # (all of them or none)

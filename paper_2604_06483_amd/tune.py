@@ -205,13 +205,12 @@ class AdamW(torch.optim.Optimizer):
                 s["m_scale"], s["v_scale"] = zeros(torch.float32, blocks), zeros(torch.float32, blocks)
         return s
 
-    def _list(self, key, params, grads):
+    def _list(self, key, params, states, grads):
         """The parameters' TensorList, kept from step to step, with this step's gradients (which it lets go with the step)."""
-        states = [self.state[p] for p in params]
-        copies = [self.copies.get(p) for p in params]
+        copies = [self.copies.get(p) for p in params] if self.copies else [None] * len(params)
         # (the list keeps its tensors' memory: what begins where one of them does is that one, unless it has been given other memory)
-        at = lambda x: None if x is None else x.data_ptr()
-        where = [(at(p), p.dtype, *(at(s.get(n)) for n in ("m", "v", "m_scale", "v_scale")), at(c)) for p, s, c in zip(params, states, copies)]
+        where = [(p.data_ptr(), p.dtype, [x.data_ptr() for x in s.values() if isinstance(x, torch.Tensor)], None if c is None else c.data_ptr())
+                 for p, s, c in zip(params, states, copies)]
         found = self._lists.get(key)
         if found is not None and found[0] == where:
             found[1].set_grads(grads)
@@ -254,26 +253,29 @@ class AdamW(torch.optim.Optimizer):
             by_step = {}                                  # (parameters that were without a gradient at times have done fewer steps)
             for p in group["params"]:
                 if p.grad is not None:
-                    by_step.setdefault(self._state(p)["step"], []).append(p)
-            for turn, (done, params) in enumerate(by_step.items()):
+                    state = self._state(p)
+                    params, states, grads = by_step.setdefault(state["step"], ([], [], []))
+                    params.append(p)
+                    states.append(state)
+                    grads.append(self._whole(p.grad))
+            for turn, (done, (params, states, grads)) in enumerate(by_step.items()):
                 used.add((at, turn))
-                calls.append((group, done + 1, params, self._list((at, turn), params, [self._whole(p.grad) for p in params])))
+                calls.append((group, done + 1, params, states, self._list((at, turn), params, states, grads)))
         # (a group whose parameters are at one step again needs one list; one that had no gradients keeps its own)
-        self._lists = {key: kept for key, kept in self._lists.items() if key in used or (key[0], 0) not in used}
+        if len(self._lists) > len(used):
+            self._lists = {key: kept for key, kept in self._lists.items() if key in used or (key[0], 0) not in used}
         if not calls:
             return
         self.norm = None
         if self.max_norm is not None:
-            one = calls[0][3] if len(calls) == 1 else LL.TensorList([g for *_, tensors in calls for g in tensors.grads])
+            one = calls[0][-1] if len(calls) == 1 else LL.TensorList([g for *_, tensors in calls for g in tensors.grads])
             self.norm = LL.ll_grad_norm(one)
-        for turn, (group, step, params, tensors) in enumerate(calls):
+        for turn, (group, step, params, states, tensors) in enumerate(calls):
             LL.ll_adamw(tensors, step, rate=float(group["lr"]), betas=group["betas"], eps=group["eps"], decay=group["weight_decay"], norm=self.norm,
                         max_norm=float("inf") if self.max_norm is None else self.max_norm, seed=self.seed + turn)
-            for p in params:
-                self.state[p]["step"] = step
-                torch.autograd.graph.increment_version(p)
-                if self.copies.get(p) is not None:
-                    torch.autograd.graph.increment_version(self.copies[p])
+            for state in states:
+                state["step"] = step
+            torch.autograd.graph.increment_version(params + [c for c in map(self.copies.get, params) if c is not None] if self.copies else params)
 
     def load_state_dict(self, state_dict):
         """As torch's, which would bring every state to its parameter's type: here they keep their own.  Hooks before it may give other states, and hooks
