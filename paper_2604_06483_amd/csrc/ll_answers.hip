@@ -9,7 +9,7 @@
 // others' sum over the whole, negated, and the first product keeps that sum by itself: with p next to 1 the difference is rounding.
 // What is new is c.  Nothing of it is needed before the second product's sums are rounded, where it is a factor of the row, so that the logits
 // are formed once: with the log-probabilities and their gradient as two calls there is a third product.  Whole calls, us, ll_policy | ll_logp, the loss in torch, ll_logp_grad: 1 row, d = 4096, V = 128256 175 | 364; 111,
-// 1608, 50257 97 | 161; 1500, 4096, 128256 2229 | 3190 (1.41 PFLOP/s; the vendor's bare product of that shape 1.28); 6000, 2560, 151936 6666 | 9510.
+// 1608, 50257 104 | 161; 1500, 4096, 128256 2229 | 3190 (1.41 PFLOP/s; the vendor's bare product of that shape 1.28); 6000, 2560, 151936 6666 | 9510.
 //
 // A policy's c is the row's own.  A preference's is known when every row of its pair has been through W_U.  Up to one pass of rows the
 // pairs are joined between the two products; beyond, every pass's sums stay in fp32 (4 d bytes a row and slice of the vocabulary, beside
