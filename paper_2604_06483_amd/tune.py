@@ -182,6 +182,8 @@ class AdamW(torch.optim.Optimizer):
     captured step there is ll_adamw itself with a clock: this class counts on the host, and says so instead of being captured.
     """
 
+    STATES = ("m", "v", "m_scale", "v_scale")
+
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, max_norm=None, bits=32, seed=0, copies=None):
         if bits not in (8, 32):
             raise ValueError(f"bits: {bits}, expected 8 or 32")
@@ -209,14 +211,13 @@ class AdamW(torch.optim.Optimizer):
         """The parameters' TensorList, kept from step to step, with this step's gradients (which it lets go with the step)."""
         copies = [self.copies.get(p) for p in params] if self.copies else [None] * len(params)
         # (the list keeps its tensors' memory: what begins where one of them does is that one, unless it has been given other memory)
-        where = [(p.data_ptr(), p.dtype, [x.data_ptr() for x in s.values() if isinstance(x, torch.Tensor)], None if c is None else c.data_ptr())
+        where = [(p.data_ptr(), p.dtype, [x.data_ptr() for x in map(s.get, self.STATES) if x is not None], None if c is None else c.data_ptr())
                  for p, s, c in zip(params, states, copies)]
         found = self._lists.get(key)
         if found is not None and found[0] == where:
             found[1].set_grads(grads)
             return found[1]
-        pick = lambda name: [s.get(name) for s in states]
-        kept = LL.TensorList(grads, params, pick("m"), pick("v"), pick("m_scale"), pick("v_scale"), copies)
+        kept = LL.TensorList(grads, params, *([s.get(name) for s in states] for name in self.STATES), copies)
         self._lists[key] = where, kept
         return kept
 

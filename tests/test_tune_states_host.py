@@ -1,4 +1,6 @@
 """The optimiser's states: replaced one by one, loaded through torch's hooks, and copies that autograd knows of (no GPU needed)."""
+import copy
+
 import torch
 
 from paper_2604_06483_amd import tune
@@ -23,6 +25,17 @@ def test_a_state_in_other_memory_is_another(steps):  # noqa: F811
         assert List.made == made + 1, name
         opt.step()
         assert List.made == made + 1, name
+    opt.state[a]["average"] = torch.ones(300)             # (a program's own beside them)
+    opt.step()
+    assert List.made == made + 1
+
+
+def test_a_copied_optimiser_loads(steps):  # noqa: F811
+    a, opt = stepped()
+    b, other = copy.deepcopy((a, opt))
+    other.state[b]["step"] = 7
+    other.load_state_dict(opt.state_dict())
+    assert other.state[b]["step"] == 1 and other.state[b]["v"].dtype == torch.float8_e5m2
 
 
 def test_hooks_after_loading_see_the_states_as_they_are(steps):  # noqa: F811
@@ -55,10 +68,10 @@ def test_what_a_hook_before_loading_returns_is_loaded(steps):  # noqa: F811
 
 def test_autograd_knows_that_a_copy_is_another(steps):  # noqa: F811
     a = torch.nn.Parameter(torch.ones(8))
-    copy = a.detach().bfloat16()
+    mine = a.detach().bfloat16()
     b = torch.nn.Parameter(torch.ones(8))
-    opt = tune.AdamW([a, b], copies={a: copy, b: None})
+    opt = tune.AdamW([a, b], copies={a: mine, b: None})
     a.grad = b.grad = torch.ones(8)
-    before = copy._version
+    before = mine._version
     opt.step()
-    assert copy._version > before
+    assert mine._version > before
